@@ -413,6 +413,81 @@ hero_status hero_bf16_attn(const void* q, const int64_t q_strides[4],
                            int64_t B, int64_t H, int64_t Sq, int64_t Skv, int64_t Dh, float scale,
                            hero_mask mask, const int32_t* kv_len, void* out, int64_t ldo, void* stream);
 
+/* ---- a KV cache in 8 bits with a scale for each block of tokens and head ----
+ *
+ * The cache that a 16-bit attention reads (Sec. 2.3: the attention module switched to 16 bits; the SQ codes of the INT8
+ * attention have ONE calibrated scale per tensor and a cache of their own, hero_layer_io).  Here no scale is calibrated:
+ * each is the absmax of a block of `block` tokens of one head, taken as the tokens are written.
+ *
+ *   k, v              codes, HERO_I8 or HERO_F8E4M3 (dt): n_blocks blocks of `block` tokens, H heads of width Dh, given by a base
+ *                     pointer and 4 element strides in the order (block, position in the block, head, channel); the channel
+ *                     stride must be 1, the others multiples of 16 that are not negative.  [n_blocks, H, block, Dh] keeps a head's block
+ *                     in one piece.  The blocks of K and of V lie apart from each other (two views of one buffer will do).
+ *   k_scale, v_scale  f32 [n_blocks, H]: token t of a block stands for codes[t] * scale.  Nothing needs clearing: a write that
+ *                     begins a block (its first position is the block's first) sets its scales, whatever was there.
+ *   block_table       int32 [B, max_blocks] (device): positions [j block, (j + 1) block) of sequence b lie in block block_table[b][j].
+ *                     NULL: in block b max_blocks + j (n_blocks >= B max_blocks then).  An index outside [0, n_blocks) is no block:
+ *                     nothing is written there, its keys are left out of the attention, its positions read as 0.  Sequences may
+ *                     share blocks that are only read; a block that is written belongs to one sequence, once.
+ * Constraints: Dh in {64, 128}; block in {16, 32, 64, 128}; max_blocks * block <= 2^30; H <= 65535; a block's 16 rows
+ * span less than 2^31 elements.  The pointers are device pointers as everywhere; the structure itself is read during the call only. */
+typedef struct {
+    void* k; void* v;
+    float* k_scale; float* v_scale;
+    int64_t k_strides[4]; int64_t v_strides[4];
+    const int32_t* block_table;
+    int64_t B, max_blocks, n_blocks;
+    int32_t H, Dh, block, dt;
+} hero_kv_cache;
+
+/* Quantises this call's K and V rows as it writes them into the cache.  Sequence b holds kv_len[b] tokens WITH this call's;
+ * row s < n (n = new_len[b] clamped to [0, S], or S without new_len) is the token at position kv_len[b] - n + s; positions
+ * outside [0, max_blocks * block) are left out, and rows s >= n are not read.  For every block with a new token, per head, K and V apart:
+ *   a     = max |x| over the block's new tokens
+ *   s_new = max(s_old, a / qmax, 2^-64)          qmax 127 (INT8) or 448 (E4M3), IEEE fp32 division;
+ *                                                s_old = 0 if the block holds no token from before this call
+ *   code  = sat(rne(x / s_new)) or e4m3(x / s_new), saturated          IEEE fp32 division
+ *   and, where s_new > s_old, the tokens from before are coded anew: the code of fl(code s_old) at s_new.
+ * A scale never shrinks while its block fills, so tokens cost their block a new coding only when they raise its largest value.  A NaN or
+ * infinity among the new tokens makes the scale NaN, and what is read from that block and head is NaN until it is begun anew.
+ *   k, v  [B, S, H, Dh] in dt (HERO_BF16 / HERO_F16), base pointer and 4 element strides (batch, token, head, channel);
+ *         channel stride 1, the others multiples of 8 (views into a fused QKV buffer will do).  B is the cache's.
+ *   kv_len int32 [B] (device), required; new_len int32 [B] (device) or NULL: a padded batch.
+ * B == 0, S == 0 or H == 0 is a no-op. */
+hero_status hero_kv_write(const hero_kv_cache* cache, const void* k, const int64_t k_strides[4],
+                          const void* v, const int64_t v_strides[4], hero_dtype dt, int64_t S,
+                          const int32_t* kv_len, const int32_t* new_len, void* stream);
+
+/* Reads positions start[b] + i, 0 <= i < S, back: out[b][i] = code * scale, rounded once to out_dt (HERO_BF16, HERO_F16 or
+ * HERO_F32).  Positions outside [0, min(kv_len[b], max_blocks block)) are left as they were in the output.
+ *   k_out, v_out  [B, S, H, Dh], base pointers and 4 element strides (batch, token, head, channel); channel stride 1, the others
+ *                 multiples of 8.  Either may be NULL (only the other is read).
+ *   start  int32 [B] (device) or NULL (0 for every sequence); kv_len int32 [B] (device), required. */
+hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, const int64_t k_strides[4],
+                         void* v_out, const int64_t v_strides[4], hero_dtype out_dt, int64_t S,
+                         const int32_t* start, const int32_t* kv_len, void* stream);
+
+/* 16-bit attention over the cache, its codes and scales taken apart inside the kernel:
+ *   out[b][i][hq] = softmax_k(scale q[b][i][hq] . K[b][k][h]) V[b][k][h],   K, V = codes * scales,  h = hq / (Hq / H)
+ *   q    [B, Sq, Hq, Dh] in dt (HERO_BF16 / HERO_F16), base pointer and 4 element strides (batch, token, head, channel); channel
+ *        stride 1, the others multiples of 8.  Hq is a multiple of the cache's H: grouped heads share a head of the cache.
+ *   out  [B*Sq, Hq*Dh] in dt, leading dimension ldo (a multiple of 4).
+ *   kv_len int32 [B] (device), required: tokens of each sequence, this call's n queries among them (they are written before).
+ *   new_len int32 [B] (device) or NULL: n = new_len[b] (clamped to [0, Sq]) queries of sequence b, Sq without it.
+ *   mask HERO_MASK_NONE: query i < n sees the keys k < len = min(kv_len[b], max_blocks block);  HERO_MASK_CAUSAL: of those k <= i + len - n.
+ *        (HERO_MASK_PADDING -> HERO_ERR_UNSUPPORTED: new_len says it.)  A query that sees no key, i >= n among them, outputs 0.
+ * The scores, the softmax and all sums are fp32; the probabilities (times the V scale of their block) are rounded to FP16 for
+ * the second product whatever dt is, behind a shift that keeps them normal numbers down to 2^-29 of the row's largest; BF16
+ * queries go through FP16 as well, each row times a power of two (exact down to 2^-29 of the row's largest).
+ * Few rows (Sq * Hq / H) over many keys are split along the keys when `workspace` has room: hero_kv_attn_workspace_bytes(cache,
+ * Hq, Sq) bytes (0: this size is not split), device memory, 256-byte aligned (else HERO_ERR_WORKSPACE).  NULL or smaller: one piece (slower, and
+ * fp32 sums are ordered otherwise).  Pure scratch, nothing is kept between calls: calls that may overlap on the GPU need
+ * their own.  The order of the sums depends on the sizes alone, so results are reproducible. */
+size_t hero_kv_attn_workspace_bytes(const hero_kv_cache* cache, int64_t Hq, int64_t Sq);
+hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, const int64_t q_strides[4], hero_dtype dt,
+                         int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,
+                         void* out, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Model-load-time operators (not on the hot path): the pre-processing phase of the method on the GPU.
  *
  * hero_absmax_cols -- calibration statistic of the static scales (Sec. 2.1: FWQ / SQ scales are

@@ -43,6 +43,12 @@ class LayerIO(C.Structure):
                 ("next_read", vp), ("next_read_bytes", C.c_size_t)]
 
 
+class KvCache(C.Structure):
+    _fields_ = [("k", vp), ("v", vp), ("k_scale", vp), ("v_scale", vp), ("k_strides", i64 * 4), ("v_strides", i64 * 4),
+                ("block_table", vp), ("B", i64), ("max_blocks", i64), ("n_blocks", i64),
+                ("H", C.c_int32), ("Dh", C.c_int32), ("block", C.c_int32), ("dt", C.c_int32)]
+
+
 # The same layout for one call, packed in one go (native alignment): a Structure filled field by field is half of a layer's host time.
 _LAYER_IO = struct.Struct("@qq8Pq3PN")
 assert _LAYER_IO.size == C.sizeof(LayerIO)
@@ -76,6 +82,10 @@ SYMBOLS = {
                             f32, f32, vp, i32, i32, vp, vp, i32, i64, vp]),
     "hero_int8_attn_online": (i32, [vp, C.POINTER(i64), vp, C.POINTER(i64), vp, C.POINTER(i64), i64, i64, i64, i64, i64,
                                     vp, f32, vp, i32, i32, vp, vp, i32, i64, vp]),
+    "hero_kv_write": (i32, [C.POINTER(KvCache), vp, C.POINTER(i64), vp, C.POINTER(i64), i32, i64, vp, vp, vp]),
+    "hero_kv_read": (i32, [C.POINTER(KvCache), vp, C.POINTER(i64), vp, C.POINTER(i64), i32, i64, vp, vp, vp]),
+    "hero_kv_attn_workspace_bytes": (C.c_size_t, [C.POINTER(KvCache), i64, i64]),
+    "hero_kv_attn": (i32, [C.POINTER(KvCache), vp, C.POINTER(i64), i32, i64, i64, f32, i32, vp, vp, vp, i64, vp, C.c_size_t, vp]),
     "hero_layer_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDesc), i64, i64]),
     "hero_layer_fwd": (i32, [C.POINTER(LayerDesc), C.POINTER(LayerWeights), C.POINTER(LayerIO), vp, C.c_size_t, vp]),
     "hero_bf16_gemm": (i32, [vp, i64, vp, i64, vp, vp, i64, i32, vp, i64, i64, i64, i64, vp]),
@@ -109,6 +119,15 @@ def _stream(stream=None):
 def _strides4(t):
     assert t.dim() == 4
     return (i64 * 4)(*t.stride())
+
+
+def _kv_rows(cache, t, S, H):
+    assert tuple(t.shape) == (cache.B, S, H, cache.Dh), "rows of a KV cache are [B, S, heads, Dh]"
+
+
+def _kv_lengths(cache, *tensors):
+    for t in tensors:
+        assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (cache.B,)), "lengths are int32 [B]"
 
 
 class Hero:
@@ -344,6 +363,72 @@ class Hero:
                                      B, H, Sq, Skv, Dh, float(scale), int(mask), _ptr(kv_len), _ptr(out),
                                      out.stride(0), _stream(stream))
         self._check(st)
+        return out
+
+    # ------------------------------------------------------------------ KV cache in 8 bits, a scale per block of tokens and head
+    def kv_cache(self, k, v, k_scale, v_scale, max_blocks=None, batch=None, block_table=None) -> KvCache:
+        """The description of a cache that lies in the given tensors: k, v [n_blocks, block, H, Dh] views (unit channel stride)
+        of int8 or float8_e4m3fn codes, k_scale / v_scale f32 [n_blocks, H], block_table int32 [batch, max_blocks] or None
+        (sequence b owns blocks b * max_blocks ..; batch and max_blocks are then given).  It keeps the tensors alive."""
+        n, block, H, Dh = k.shape
+        if block_table is not None:
+            if block_table.dim() != 2 or block_table.dtype != torch.int32 or not block_table.is_contiguous():
+                raise ValueError("block_table is a contiguous int32 tensor [batch, max_blocks]")
+            if batch not in (None, block_table.shape[0]) or max_blocks not in (None, block_table.shape[1]):
+                raise ValueError("batch and max_blocks are the block table's sizes")
+            batch, max_blocks = block_table.shape
+        if batch is None or max_blocks is None:
+            raise ValueError("a cache without a block table needs batch and max_blocks")
+        if v.shape != k.shape or v.dtype != k.dtype or k.dtype not in (torch.int8, torch.float8_e4m3fn):
+            raise ValueError("k and v are int8 or float8_e4m3fn tensors of one shape [n_blocks, block, H, Dh]")
+        for s in (k_scale, v_scale):
+            if s.dtype != torch.float32 or tuple(s.shape) != (n, H) or not s.is_contiguous():
+                raise ValueError("scales are contiguous float32 tensors [n_blocks, H]")
+        c = KvCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _strides4(k), _strides4(v), _ptr(block_table),
+                    int(batch), int(max_blocks), n, H, Dh, block, _DT[k.dtype])
+        c.tensors = (k, v, k_scale, v_scale, block_table)
+        return c
+
+    def hero_kv_write(self, cache, k, v, kv_len, new_len=None, stream=None):
+        """Quantises k, v [B,S,H,Dh] (bf16 / f16, unit channel stride) into the cache; kv_len int32 [B] counts this call's tokens."""
+        _kv_rows(cache, k, k.shape[1], cache.H)
+        _kv_rows(cache, v, k.shape[1], cache.H)
+        assert k.dtype == v.dtype
+        _kv_lengths(cache, kv_len, new_len)
+        self._check(self.lib.hero_kv_write(cache, _ptr(k), _strides4(k), _ptr(v), _strides4(v), _DT[k.dtype], k.shape[1],
+                                           _ptr(kv_len), _ptr(new_len), _stream(stream)))
+
+    def hero_kv_read(self, cache, S, kv_len, start=None, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
+        """Positions start[b] .. start[b] + S - 1 as [B,S,H,Dh] rows of `dtype`, K and V.  Positions that the sequence does not hold
+        are left as they were in k_out / v_out, and are 0 in outputs made here."""
+        shape = (cache.B, S, cache.H, cache.Dh)
+        if k_out is None or v_out is None:
+            device = kv_len.device
+            k_out = torch.zeros(shape, dtype=dtype if v_out is None else v_out.dtype, device=device) if k_out is None else k_out
+            v_out = torch.zeros(shape, dtype=k_out.dtype, device=device) if v_out is None else v_out
+        _kv_rows(cache, k_out, S, cache.H)
+        _kv_rows(cache, v_out, S, cache.H)
+        assert k_out.dtype == v_out.dtype
+        _kv_lengths(cache, kv_len, start)
+        self._check(self.lib.hero_kv_read(cache, _ptr(k_out), _strides4(k_out), _ptr(v_out), _strides4(v_out), _DT[k_out.dtype], S,
+                                          _ptr(start), _ptr(kv_len), _stream(stream)))
+        return k_out, v_out
+
+    def hero_kv_attn_workspace_bytes(self, cache, Hq, Sq) -> int:
+        return int(self.lib.hero_kv_attn_workspace_bytes(cache, Hq, Sq))
+
+    def hero_kv_attn(self, cache, q, scale, mask, kv_len, new_len=None, out=None, workspace=None, stream=None):
+        """q [B,Sq,Hq,Dh] bf16 / f16 over the cache.  Returns [B*Sq, Hq*Dh] in q's type.  workspace: optional uint8 tensor
+        (hero_kv_attn_workspace_bytes), without which few rows over many keys are not split."""
+        B, Sq, Hq, Dh = q.shape
+        _kv_rows(cache, q, Sq, Hq)
+        _kv_lengths(cache, kv_len, new_len)
+        if out is None:
+            out = torch.empty((B * Sq, Hq * Dh), dtype=q.dtype, device=q.device)
+        assert out.dtype == q.dtype and out.stride(1) == 1
+        self._check(self.lib.hero_kv_attn(cache, _ptr(q), _strides4(q), _DT[q.dtype], Hq, Sq, float(scale), int(mask),
+                                          _ptr(kv_len), _ptr(new_len), _ptr(out), out.stride(0), _ptr(workspace),
+                                          0 if workspace is None else workspace.nbytes, _stream(stream)))
         return out
 
     # ------------------------------------------------------------------ layer

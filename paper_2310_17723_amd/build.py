@@ -28,7 +28,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 
 # extra per-file flags
 EXTRA = {"int8_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-         "bf16_ops.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+         "bf16_ops.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "kv_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def sources():

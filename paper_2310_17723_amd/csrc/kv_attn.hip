@@ -1,0 +1,469 @@
+// 16-bit attention over the block-scaled 8-bit KV cache (hero_kv_attn): scores, softmax and products on the matrix cores in
+// FP16 with fp32 sums, the cache's codes (exact in FP16) and scales taken apart in registers.
+//
+// The mathematics.  With K = ks c_k, V = vs c_v (scales of the key's block and head) and, base 2, a = scale log2(e) ks (q . c_k):
+//   out = sum_k 2^a vs c_v / sum_k 2^a = sum_k 2^b c_v / sum_k 2^b / vs,     b = a + log2 vs
+// so V's scale costs nothing per value: it is the addend of the fma that makes a score an exponent, and its reciprocal weighs a block's
+// share of the denominator.  The running maximum m is that of b; P = 2^(b - m + 15) is what FP16 holds: at most 2^15, and a normal number
+// down to 2^-29 of the row's largest (a long flat tail of small probabilities is not lost).  The denominator is summed before that rounding: a
+// block whose V is small beside the others' has a small P and may still hold most of the weight.  q is made FP16 too: rows of BF16 are
+// multiplied by a power of two that takes their largest value to [2^14, 2^15), which keeps every bit of values down to 2^-29 of it.
+// Rows: the queries of all heads that share a head of the cache, row = token * group + head of the group.
+#include "kv_cache.h"
+
+namespace {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
+constexpr float LIFT = 15.0f;
+
+struct AttnArgs {
+    KvView c;
+    const uint16_t* q; int64_t qs[3];                         // batch, token, head
+    int B, Hq, Sq, group;
+    float scale; int causal;
+    const int32_t *kv_len, *new_len;
+    uint16_t* out; int64_t ldo;
+    int tiles, splits;                                        // tiles of rows; pieces of the keys
+    float* part; float* part_ml;                              // [B][H][rows][splits][Dh], [..][2]: a piece's sum of P c_v; its m, its denominator
+};
+
+// ---- codes -> FP16 ----
+// two codes of INT8 in the bytes that sel picks, as FP16: 0x64xx is 1024 + xx, xx = code + 128
+__device__ __forceinline__ uint32_t i8x2_to_f16(uint32_t hi, uint32_t lo, uint32_t sel) {
+    const uint32_t w = __builtin_amdgcn_perm(hi, lo, sel) ^ 0x64806480u;
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, w) + v2h{(_Float16)-1152.0f, (_Float16)-1152.0f});
+}
+template <bool HI> __device__ __forceinline__ uint32_t f8x2_to_f16(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, HI));
+}
+// eight neighbouring codes
+template <int FMT> __device__ __forceinline__ v8h codes8(uint32_t w0, uint32_t w1) {
+    v4i r;
+    if constexpr (FMT == HERO_I8)
+        r = v4i{(int)i8x2_to_f16(0, w0, 0x0c010c00u), (int)i8x2_to_f16(0, w0, 0x0c030c02u),
+                (int)i8x2_to_f16(0, w1, 0x0c010c00u), (int)i8x2_to_f16(0, w1, 0x0c030c02u)};
+    else r = v4i{(int)f8x2_to_f16<false>(w0), (int)f8x2_to_f16<true>(w0), (int)f8x2_to_f16<false>(w1), (int)f8x2_to_f16<true>(w1)};
+    return __builtin_bit_cast(v8h, r);
+}
+// channels 2 p and 2 p + 1 (of the four in a dword) of two keys: the pair of keys per channel
+template <int FMT, int P> __device__ __forceinline__ void pair_of_keys(uint32_t k0, uint32_t k1, uint32_t& c0, uint32_t& c1) {
+    if constexpr (FMT == HERO_I8) {
+        c0 = i8x2_to_f16(k1, k0, P ? 0x0c060c02u : 0x0c040c00u);
+        c1 = i8x2_to_f16(k1, k0, P ? 0x0c070c03u : 0x0c050c01u);
+    } else {
+        const uint32_t w = __builtin_amdgcn_perm(k1, k0, P ? 0x07030602u : 0x05010400u);
+        c0 = f8x2_to_f16<false>(w);
+        c1 = f8x2_to_f16<true>(w);
+    }
+}
+
+__device__ __forceinline__ float max_of_groups16(float x) {           // over the lanes l, l ^ 16, l ^ 32, l ^ 48
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float sum_of_groups16(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// keys that row's query sees: [0, result)
+__device__ __forceinline__ int keys_seen(const AttnArgs& a, int row, int len, int n) {
+    const int s = row / a.group;
+    if (row >= a.Sq * a.group || s >= n) return 0;
+    return a.causal ? (int)max((int64_t)0, min((int64_t)len, (int64_t)s + 1 + len - n)) : len;
+}
+
+// ------------------------------------------------------------------------------------------
+// Few rows: a wave owns 16 RT rows and 32 keys at a time, its K and V fragments straight from memory into registers (K: a lane's 16
+// channels of its key; V: a lane's 8 (4) channels of 8 keys, paired up by byte permutes), and an online softmax of its own; the NW waves of
+// a workgroup split the keys of its piece and meet in LDS.
+// ------------------------------------------------------------------------------------------
+template <int DH, int FMT, int DT, int RT, int NW>
+__global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
+    constexpr int KS = DH / 32;                // matrix steps over the head's width
+    constexpr int CT = DH / 16;                // tiles of 16 output channels; tile i: channels CT c + i
+    constexpr int VW = DH / 64;                // dwords of V per lane and key
+    constexpr int ROWS = 16 * RT, OLD = DH + 4;
+    __shared__ __attribute__((aligned(16))) float so[NW][16][OLD];
+    __shared__ float sm[NW][ROWS], sl[NW][ROWS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+    int u = blockIdx.x;
+    const int split = u % a.splits; u /= a.splits;
+    const int tile = u % a.tiles; u /= a.tiles;
+    const int h = u % a.c.H, b = u / a.c.H;
+    const int block = 1 << a.c.log2_block;
+    const int len = min(max(a.kv_len[b], 0), a.c.max_blocks << a.c.log2_block);
+    const int n = a.new_len ? min(max(a.new_len[b], 0), a.Sq) : a.Sq;
+    const int row0 = tile * ROWS, nrows = a.Sq * a.group;
+
+    // what the rows see: all of them the keys before `all`, none those from `last` on (a later token sees more, until n)
+    int seen[RT], all, last;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) seen[rt] = keys_seen(a, row0 + rt * 16 + c, len, n);
+    {
+        const int hi_row = min(row0 + ROWS, nrows) - 1;
+        last = max(keys_seen(a, row0, len, n), keys_seen(a, min(hi_row, n * a.group - 1), len, n));
+        if (row0 >= n * a.group) last = 0;
+        all = min(keys_seen(a, row0, len, n), keys_seen(a, hi_row, len, n));
+    }
+    last = __builtin_amdgcn_readfirstlane(last);
+    all = __builtin_amdgcn_readfirstlane(all);
+
+    // queries
+    v8h qf[RT][KS];
+    float rc[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = min(row0 + rt * 16 + c, nrows - 1), s = row / a.group;
+        const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + row - s * a.group) * a.qs[2] + g * 16;
+        v4i raw[KS];
+#pragma unroll
+        for (int t = 0; t < KS; ++t) raw[t] = *reinterpret_cast<const v4i*>(qp + (t >> 1) * 64 + (t & 1) * 8);
+        rc[rt] = fabsf(a.scale) * 1.44269504088896340736f;
+        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0;
+        if constexpr (DT == HERO_F16) {
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                v4i w = raw[t];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] ^= (int)sign;
+                qf[rt][t] = __builtin_bit_cast(v8h, w);
+            }
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int t = 0; t < KS; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = (uint32_t)raw[t][j] & 0x7fff7fffu;
+                    top = max(top, max(w & 0xffffu, w >> 16));
+                }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+            // the power of two that takes the largest value to [2^14, 2^15); 1 where it is no number; at most 2^100
+            const int ex = (int)(top >> 7);                               // biased exponent
+            const int up = ex == 255 ? 0 : min(127 + 14 - ex, 100);
+            const float by = __uint_as_float((uint32_t)(127 + up) << 23);
+            rc[rt] *= __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                v4i w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t x = (uint32_t)raw[t][j] ^ sign;
+                    const v2h y = {(_Float16)(bf16_bits_to_f32(x & 0xffffu) * by), (_Float16)(__uint_as_float(x & 0xffff0000u) * by)};
+                    w[j] = __builtin_bit_cast(int, y);
+                }
+                qf[rt][t] = __builtin_bit_cast(v8h, w);
+            }
+        }
+    }
+
+    v4f o[RT][CT];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -INFINITY; l[rt] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < CT; ++i) o[rt][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    // this piece's keys, in steps of 32
+    const int steps = (last + 31) / 32, per = (steps + a.splits - 1) / a.splits;
+    const int s_end = min((split + 1) * per, steps);
+    v4i kr[2][VW];                               // [half][64 channels]
+    uint32_t vr[8][VW];
+    float ks[2], vs[2];
+    int blk[2];
+    const uint32_t koff = (uint32_t)(c * (int)a.c.k.s_row + g * 16), voff = (uint32_t)(g * 4 * (int)a.c.v.s_row + c * (DH / 16));
+    auto find = [&](int step) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const int key = step * 32 + hf * 16;
+            blk[hf] = key < last ? a.c.block_of(b, key >> a.c.log2_block) : -1;
+        }
+    };
+    auto load = [&](int step) {                  // (a half without a block reads block 0, hidden below)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const int key = step * 32 + hf * 16, at = key & (block - 1);
+            const int64_t bl = max(blk[hf], 0);
+            const uint8_t* const kp = a.c.k.codes + bl * a.c.k.s_block + (int64_t)at * a.c.k.s_row + (int64_t)h * a.c.k.s_head;
+            const uint8_t* const vp = a.c.v.codes + bl * a.c.v.s_block + (int64_t)at * a.c.v.s_row + (int64_t)h * a.c.v.s_head;
+            ks[hf] = a.c.k.scale[bl * a.c.H + h];
+            vs[hf] = a.c.v.scale[bl * a.c.H + h];
+#pragma unroll
+            for (int t = 0; t < VW; ++t) kr[hf][t] = *reinterpret_cast<const v4i*>(kp + koff + t * 64);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (VW == 2) {
+                    const v2i w = *reinterpret_cast<const v2i*>(vp + voff + (uint32_t)j * (uint32_t)a.c.v.s_row);
+                    vr[hf * 4 + j][0] = (uint32_t)w[0]; vr[hf * 4 + j][1] = (uint32_t)w[1];
+                } else vr[hf * 4 + j][0] = *reinterpret_cast<const uint32_t*>(vp + voff + (uint32_t)j * (uint32_t)a.c.v.s_row);
+            }
+        }
+    };
+    int step = split * per + wave;
+    if (step < s_end) { find(step); load(step); }
+    for (; step < s_end; step += NW) {
+        // taken over from the loads, so that the next step's can be issued
+        v8h kf[2][KS];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int t = 0; t < VW; ++t) {
+                kf[hf][2 * t] = codes8<FMT>((uint32_t)kr[hf][t][0], (uint32_t)kr[hf][t][1]);
+                kf[hf][2 * t + 1] = codes8<FMT>((uint32_t)kr[hf][t][2], (uint32_t)kr[hf][t][3]);
+            }
+        const int key0 = step * 32;
+        const bool edge = key0 + 32 > all || blk[0] < 0 || blk[1] < 0;
+        if (edge)                                                         // what lies behind the last key is no code
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool there = key0 + (j >> 2) * 16 + g * 4 + (j & 3) < len && blk[j >> 2] >= 0;
+#pragma unroll
+                for (int t = 0; t < VW; ++t) vr[j][t] = there ? vr[j][t] : 0u;
+            }
+        v8h vf[CT];
+#pragma unroll
+        for (int t = 0; t < VW; ++t) {
+            uint32_t w[4][4];                    // [channel][pair of keys]
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                pair_of_keys<FMT, 0>(vr[2 * j][t], vr[2 * j + 1][t], w[0][j], w[1][j]);
+                pair_of_keys<FMT, 1>(vr[2 * j][t], vr[2 * j + 1][t], w[2][j], w[3][j]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vf[t * 4 + i] = __builtin_bit_cast(v8h, v4i{(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3]});
+        }
+        float kc[2], lv[2], iv[2];
+        int lim[2];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            kc[hf] = ks[hf]; lv[hf] = __builtin_amdgcn_logf(vs[hf]); iv[hf] = 1.0f / vs[hf];
+            lim[hf] = blk[hf] < 0 ? 0 : 0x7fffffff;
+        }
+        if (step + NW < s_end) { find(step + NW); load(step + NW); }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            v4f acc[2];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                acc[hf] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int t = 0; t < KS; ++t) acc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][t], qf[rt][t], acc[hf], 0, 0, 0);
+            }
+            float x[8], top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = fmaf(acc[j >> 2][j & 3], rc[rt] * kc[j >> 2], lv[j >> 2]);
+            if (edge) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int key = key0 + (j >> 2) * 16 + g * 4 + (j & 3);
+                    x[j] = key < min(seen[rt], lim[j >> 2]) ? x[j] : -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
+            top = max_of_groups16(top);
+            const float mn = fmaxf(m[rt], top), ms = mn > -INFINITY ? mn : 0.0f, sub = ms - LIFT;
+            const float resc = __builtin_amdgcn_exp2f(m[rt] - ms);
+            uint32_t p[4];
+            float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const float e0 = __builtin_amdgcn_exp2f(x[j] - sub), e1 = __builtin_amdgcn_exp2f(x[j + 1] - sub);
+                p[j >> 1] = __builtin_bit_cast(uint32_t, v2h{(_Float16)e0, (_Float16)e1});
+                sum[j >> 2] += e0 + e1;
+            }
+            // (a block that a row does not see may have a scale that is NaN)
+            l[rt] = fmaf(l[rt], resc, (sum[0] == 0.0f ? 0.0f : sum[0] * iv[0]) + (sum[1] == 0.0f ? 0.0f : sum[1] * iv[1]));
+            if (__builtin_amdgcn_ballot_w64(mn != m[rt]) != 0) {
+#pragma unroll
+                for (int i = 0; i < CT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[rt][i][r] *= resc;
+            }
+            m[rt] = mn;
+            const v8h pf = __builtin_bit_cast(v8h, v4i{(int)p[0], (int)p[1], (int)p[2], (int)p[3]});
+#pragma unroll
+            for (int i = 0; i < CT; ++i) o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[i], pf, o[rt][i], 0, 0, 0);
+        }
+    }
+
+    // the waves meet: each one's sums at the common maximum, added in the order of the waves
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        l[rt] = sum_of_groups16(l[rt]);
+        if (g == 0) { sm[wave][rt * 16 + c] = m[rt]; sl[wave][rt * 16 + c] = l[rt]; }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        __syncthreads();
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, sm[w][rt * 16 + c]);
+        const float f = M > -INFINITY ? __builtin_amdgcn_exp2f(m[rt] - M) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < CT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) so[wave][c][(g * 4 + r) * CT + i] = o[rt][i][r] * f;
+        __syncthreads();
+        for (int at = tid; at < 16 * (DH / 4); at += 64 * NW) {
+            const int rr = at / (DH / 4), e = (at % (DH / 4)) * 4, row = row0 + rt * 16 + rr;
+            if (row >= nrows) continue;
+            float top = -INFINITY, L = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) top = fmaxf(top, sm[w][rt * 16 + rr]);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float lw = sl[w][rt * 16 + rr];
+                if (!(lw == 0.0f)) L = fmaf(lw, __builtin_amdgcn_exp2f(sm[w][rt * 16 + rr] - top), L);
+            }
+            v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const v4f p = *reinterpret_cast<const v4f*>(&so[w][rr][e]);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sum[t] += p[t];
+            }
+            if (a.splits > 1) {
+                const int64_t pr = (((int64_t)b * a.c.H + h) * nrows + row) * a.splits + split;
+                *reinterpret_cast<v4f*>(a.part + pr * DH + e) = sum;
+                if (e == 0) { a.part_ml[pr * 2] = top; a.part_ml[pr * 2 + 1] = L; }
+            } else {
+                // (a score beyond fp32 has no exponent: NaN; no key: 0)
+                const float inv = top == INFINITY ? __builtin_nanf("") : (L == 0.0f ? 0.0f : 1.0f / L);
+                const int s = row / a.group;
+                uint16_t* const op = a.out + ((int64_t)b * a.Sq + s) * a.ldo + (int64_t)(h * a.group + row - s * a.group) * DH + e;
+                *reinterpret_cast<v2i*>(op) = v2i{(int)pack2_hp<DT>(sum[0] * inv, sum[1] * inv), (int)pack2_hp<DT>(sum[2] * inv, sum[3] * inv)};
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// The pieces of the keys joined: DH / 4 threads per row, added in the order of the pieces.
+// ------------------------------------------------------------------------------------------
+template <int DH, int DT>
+__global__ __launch_bounds__(256) void kv_attn_join_kernel(AttnArgs a) {
+    constexpr int TPR = DH / 4;
+    const int nrows = a.Sq * a.group;
+    const int64_t r = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const int e = (threadIdx.x % TPR) * 4;
+    if (r >= (int64_t)a.B * a.c.H * nrows) return;
+    const float* const ml = a.part_ml + r * a.splits * 2;
+    const float* const p = a.part + r * a.splits * DH + e;
+    float M = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, ml[2 * s]);
+    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    float L = 0.0f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float l = ml[2 * s + 1];
+        if (l == 0.0f) continue;
+        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - M);
+        const v4f x = *reinterpret_cast<const v4f*>(p + (int64_t)s * DH);
+        L = fmaf(l, f, L);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sum[t] = fmaf(x[t], f, sum[t]);
+    }
+    const float inv = M == INFINITY ? __builtin_nanf("") : (L == 0.0f ? 0.0f : 1.0f / L);
+    const int row = (int)(r % nrows), bh = (int)(r / nrows), h = bh % a.c.H, b = bh / a.c.H, s = row / a.group;
+    uint16_t* const op = a.out + ((int64_t)b * a.Sq + s) * a.ldo + (int64_t)(h * a.group + row - s * a.group) * DH + e;
+    *reinterpret_cast<v2i*>(op) = v2i{(int)pack2_hp<DT>(sum[0] * inv, sum[1] * inv), (int)pack2_hp<DT>(sum[2] * inv, sum[3] * inv)};
+}
+
+__global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, int64_t ld) {
+    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < rows * cols) out[(i / cols) * ld + i % cols] = 0;
+}
+
+// How a call is cut: 16 RT rows to a tile, the keys into pieces.
+struct Plan { int rt, tiles, splits; };
+
+Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq) {
+    Plan p;
+    const int64_t rows = Sq * (Hq / c->H);
+    p.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const int64_t tiles = (rows + 16 * p.rt - 1) / (16 * p.rt);
+    p.tiles = (int)tiles;
+    const int64_t units = c->B * c->H * tiles, steps = (c->max_blocks * c->block + 31) / 32;
+    // pieces of 16 steps or more while there are fewer than four workgroups per CU
+    int64_t s = (1024 + units - 1) / units;
+    s = s < steps / 16 ? s : steps / 16;
+    p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    return p;
+}
+
+hero_status check_sizes(const hero_kv_cache* c, int64_t Hq, int64_t Sq) {
+    if (Hq < 0 || Sq < 0 || Hq > 65535 || Sq > (1LL << 30)) return HERO_ERR_SHAPE;
+    if (c->H == 0 ? Hq != 0 : Hq % c->H != 0) return HERO_ERR_SHAPE;
+    if (c->H && Sq * (Hq / c->H) > (1LL << 30)) return HERO_ERR_SHAPE;
+    return HERO_OK;
+}
+
+size_t part_bytes(const hero_kv_cache* c, int64_t Hq, int64_t Sq, int splits) {
+    return splits > 1 ? (size_t)(c->B * Sq * Hq) * splits * (c->Dh + 2) * 4 : 0;
+}
+
+template <int DH, int FMT, int DT>
+hero_status launch(const AttnArgs& a, int rt, int64_t nb, hipStream_t st) {
+    const dim3 grid((unsigned)nb), block(256);
+    if (rt == 1) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 1, 4>), grid, block, 0, st, a);
+    else if (rt == 2) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 2, 4>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 4, 4>), grid, block, 0, st, a);
+    hero_status r = hero_launch_status();
+    if (r != HERO_OK || a.splits == 1) return r;
+    const int64_t rows = (int64_t)a.B * a.c.H * a.Sq * a.group;
+    hipLaunchKernelGGL((kv_attn_join_kernel<DH, DT>), dim3((unsigned)((rows * (DH / 4) + 255) / 256)), dim3(256), 0, st, a);
+    return hero_launch_status();
+}
+
+}  // namespace
+
+extern "C" size_t hero_kv_attn_workspace_bytes(const hero_kv_cache* cache, int64_t Hq, int64_t Sq) {
+    if (kv_check(cache) != HERO_OK || check_sizes(cache, Hq, Sq) != HERO_OK || cache->B == 0 || Hq == 0 || Sq == 0) return 0;
+    return part_bytes(cache, Hq, Sq, plan(cache, Hq, Sq).splits);
+}
+
+extern "C" hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, const int64_t q_strides[4], hero_dtype dt,
+                                    int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,
+                                    void* out, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream) {
+    hero_status r = kv_check(cache);
+    if (r != HERO_OK) return r;
+    if (dt != HERO_BF16 && dt != HERO_F16) return HERO_ERR_UNSUPPORTED;
+    if (mask != HERO_MASK_NONE && mask != HERO_MASK_CAUSAL) return HERO_ERR_UNSUPPORTED;
+    if ((r = check_sizes(cache, Hq, Sq)) != HERO_OK) return r;
+    if (cache->B == 0 || Hq == 0 || Sq == 0) return HERO_OK;
+    if (!out || !kv_len) return HERO_ERR_NULL;
+    if ((r = kv_check_rows(q, q_strides)) != HERO_OK) return r;
+    const int Dh = cache->Dh;
+    if (ldo < Hq * Dh) return HERO_ERR_SHAPE;
+    if (ldo % 4 || !hero_aligned16(out) || ((uintptr_t)kv_len & 3) || ((uintptr_t)new_len & 3)) return HERO_ERR_ALIGN;
+    if (workspace && ((uintptr_t)workspace & 255)) return HERO_ERR_WORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    if (cache->n_blocks == 0 || cache->max_blocks == 0) {                // no key anywhere
+        const int64_t n = cache->B * Sq * Hq * Dh;
+        if ((n + 255) / 256 > 0x7fffffffLL) return HERO_ERR_SHAPE;
+        hipLaunchKernelGGL(kv_attn_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (uint16_t*)out, cache->B * Sq, Hq * Dh, ldo);
+        return hero_launch_status();
+    }
+    Plan p = plan(cache, Hq, Sq);
+    if (!workspace || workspace_bytes < part_bytes(cache, Hq, Sq, p.splits)) p.splits = 1;
+    const int64_t nb = cache->B * cache->H * p.tiles * p.splits;
+    if (nb > 0x7fffffffLL || cache->B * Sq * Hq * (Dh / 4) / 256 > 0x7ffffffeLL) return HERO_ERR_SHAPE;
+    AttnArgs a;
+    a.c = kv_view(cache);
+    a.q = (const uint16_t*)q;
+    for (int t = 0; t < 3; ++t) a.qs[t] = q_strides[t];
+    a.B = (int)cache->B; a.Hq = (int)Hq; a.Sq = (int)Sq; a.group = (int)(Hq / cache->H);
+    a.scale = scale; a.causal = mask == HERO_MASK_CAUSAL; a.kv_len = kv_len; a.new_len = new_len;
+    a.out = (uint16_t*)out; a.ldo = ldo; a.tiles = p.tiles; a.splits = p.splits;
+    a.part = (float*)workspace; a.part_ml = a.part + (p.splits > 1 ? cache->B * Sq * Hq * p.splits * Dh : 0);
+#define HERO_KVA(DH, FMT) (dt == HERO_BF16 ? launch<DH, FMT, HERO_BF16>(a, p.rt, nb, st) : launch<DH, FMT, HERO_F16>(a, p.rt, nb, st))
+    if (cache->dt == HERO_I8) return Dh == 64 ? HERO_KVA(64, HERO_I8) : HERO_KVA(128, HERO_I8);
+    return Dh == 64 ? HERO_KVA(64, HERO_F8E4M3) : HERO_KVA(128, HERO_F8E4M3);
+#undef HERO_KVA
+}
