@@ -29,6 +29,10 @@ struct AttnArgs {
     float* part; float* part_ml;                              // [B][H][rows][splits][Dh], [..][2]: a piece's sum of P c_v; its m, its denominator
 };
 
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {       // v_cvt_pk_f16_f32 (round to nearest even)
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{lo, hi}), v2h));
+}
+
 // ---- codes -> FP16 ----
 // two codes of INT8 in the bytes that sel picks, as FP16: 0x64xx is 1024 + xx, xx = code + 128
 __device__ __forceinline__ uint32_t i8x2_to_f16(uint32_t hi, uint32_t lo, uint32_t sel) {
@@ -66,6 +70,49 @@ __device__ __forceinline__ float max_of_groups16(float x) {           // over th
 __device__ __forceinline__ float sum_of_groups16(float x) {
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
+}
+
+// A row's queries as FP16 (lanes LANES apart hold its other channels), negated for a negative scale, and what a score is to be multiplied by (base 2).
+template <int DT, int N, int LANES>
+__device__ __forceinline__ float queries(const v4i (&raw)[N], float scale, v8h (&qf)[N]) {
+    const float rc = fabsf(scale) * 1.44269504088896340736f;
+    const uint32_t sign = scale < 0.0f ? 0x80008000u : 0;
+    if constexpr (DT == HERO_F16) {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            v4i w = raw[t];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] ^= (int)sign;
+            qf[t] = __builtin_bit_cast(v8h, w);
+        }
+        return rc;
+    } else {
+        uint32_t top = 0;
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w = (uint32_t)raw[t][j] & 0x7fff7fffu;
+                top = max(top, max(w & 0xffffu, w >> 16));
+            }
+#pragma unroll
+        for (int o = LANES; o < 64; o *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        // the power of two that takes the largest value to [2^14, 2^15); 1 where it is no number; at most 2^100
+        const int ex = (int)(top >> 7);                                   // biased exponent
+        const int up = ex == 255 ? 0 : min(127 + 14 - ex, 100);
+        const float by = __uint_as_float((uint32_t)(127 + up) << 23);
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            v4i w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t x = (uint32_t)raw[t][j] ^ sign;
+                w[j] = (int)f16x2(bf16_bits_to_f32(x & 0xffffu) * by, __uint_as_float(x & 0xffff0000u) * by);
+            }
+            qf[t] = __builtin_bit_cast(v8h, w);
+        }
+        return rc * __uint_as_float((uint32_t)(127 - up) << 23);
+    }
 }
 
 // keys that row's query sees: [0, result)
@@ -121,44 +168,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
         v4i raw[KS];
 #pragma unroll
         for (int t = 0; t < KS; ++t) raw[t] = *reinterpret_cast<const v4i*>(qp + (t >> 1) * 64 + (t & 1) * 8);
-        rc[rt] = fabsf(a.scale) * 1.44269504088896340736f;
-        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0;
-        if constexpr (DT == HERO_F16) {
-#pragma unroll
-            for (int t = 0; t < KS; ++t) {
-                v4i w = raw[t];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] ^= (int)sign;
-                qf[rt][t] = __builtin_bit_cast(v8h, w);
-            }
-        } else {
-            uint32_t top = 0;
-#pragma unroll
-            for (int t = 0; t < KS; ++t)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t w = (uint32_t)raw[t][j] & 0x7fff7fffu;
-                    top = max(top, max(w & 0xffffu, w >> 16));
-                }
-            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-            // the power of two that takes the largest value to [2^14, 2^15); 1 where it is no number; at most 2^100
-            const int ex = (int)(top >> 7);                               // biased exponent
-            const int up = ex == 255 ? 0 : min(127 + 14 - ex, 100);
-            const float by = __uint_as_float((uint32_t)(127 + up) << 23);
-            rc[rt] *= __uint_as_float((uint32_t)(127 - up) << 23);
-#pragma unroll
-            for (int t = 0; t < KS; ++t) {
-                v4i w;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t x = (uint32_t)raw[t][j] ^ sign;
-                    const v2h y = {(_Float16)(bf16_bits_to_f32(x & 0xffffu) * by), (_Float16)(__uint_as_float(x & 0xffff0000u) * by)};
-                    w[j] = __builtin_bit_cast(int, y);
-                }
-                qf[rt][t] = __builtin_bit_cast(v8h, w);
-            }
-        }
+        rc[rt] = queries<DT, KS, 16>(raw, a.scale, qf[rt]);
     }
 
     v4f o[RT][CT];
@@ -275,7 +285,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 const float e0 = __builtin_amdgcn_exp2f(x[j] - sub), e1 = __builtin_amdgcn_exp2f(x[j + 1] - sub);
-                p[j >> 1] = __builtin_bit_cast(uint32_t, v2h{(_Float16)e0, (_Float16)e1});
+                p[j >> 1] = f16x2(e0, e1);
                 sum[j >> 2] += e0 + e1;
             }
             // (a block that a row does not see may have a scale that is NaN)
@@ -345,6 +355,296 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
+// Many rows: a workgroup of four waves owns 128 RTW rows, a wave 32 RTW of them; K and V of 64 keys at a time are made FP16 once, on their way
+// into LDS (K by rows, V by channels), three tiles deep, so that one barrier per tile is enough: a tile is written while the one before it is
+// worked on.  Scores are computed transposed (S^T = K Q^T): a lane owns query lane % 32 of each of its RTW row tiles, and the exponentials are
+// the second product's operand as they stand.  The scores of 32 keys are made while the exponentials of the 32 before them are taken.
+// The maximum is raised, and the sums so far rescaled, only when a score exceeds it by SLACK (P stays within FP16's 2^15).
+// LDS holds 16-byte pieces XOR-swizzled by their row: fragment reads (turns of lanes 0-3, 12-15, 20-27 and so on) meet no bank conflict.
+// ------------------------------------------------------------------------------------------
+constexpr float SLACK = 7.0f;
+
+template <int DH, int FMT, int DT, int RTW, int GH>          // GH: groups of keys with scales of their own in 32 keys
+__global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(AttnArgs a) {
+    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, GE = 16 / GH;
+    constexpr int KU = DH / 64;                              // 16-byte units of K per thread and tile
+    __shared__ __attribute__((aligned(1024))) uint8_t sK[NB][64 * KROW], sV[NB][DH * 128];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, ql = lane & 31;
+    int u = blockIdx.x;
+    const int nrows = a.Sq * a.group;
+    // workgroups go round-robin to the XCDs: a head's row tiles to one of them; the last rows (which see the most keys) first
+    const int xcd = u & 7; u >>= 3;
+    const int per_xcd = (a.B * a.c.H + 7) / 8;
+    const int split = u % a.splits; u /= a.splits;
+    const int bh = (u % per_xcd) * 8 + xcd, tile = a.tiles - 1 - u / per_xcd;
+    if (bh >= a.B * a.c.H) return;
+    const int h = bh % a.c.H, b = bh / a.c.H;
+    const int len = min(max(a.kv_len[b], 0), a.c.max_blocks << a.c.log2_block);
+    const int n = a.new_len ? min(max(a.new_len[b], 0), a.Sq) : a.Sq;
+    const int row0 = tile * 128 * RTW, wrow = row0 + wave * 32 * RTW;
+    auto range = [&](int r0, int count, int& all, int& last) {           // of rows [r0, r0 + count): keys that all / any of them see
+        const int r1 = min(r0 + count, nrows) - 1;
+        last = r0 >= n * a.group ? 0 : max(keys_seen(a, r0, len, n), keys_seen(a, min(r1, n * a.group - 1), len, n));
+        all = min(keys_seen(a, r0, len, n), keys_seen(a, r1, len, n));
+        last = __builtin_amdgcn_readfirstlane(last);
+        all = __builtin_amdgcn_readfirstlane(all);
+    };
+    int all, last, wall, wlast;
+    range(row0, 128 * RTW, all, last);
+    range(wrow, 32 * RTW, wall, wlast);
+    int seen[RTW];
+#pragma unroll
+    for (int rt = 0; rt < RTW; ++rt) seen[rt] = keys_seen(a, wrow + rt * 32 + ql, len, n);
+    const int total = (last + 63) / 64, per = (total + a.splits - 1) / a.splits;
+    const int t0 = min(split * per, total), t1 = min(t0 + per, total), wt = min(t1, (wlast + 63) / 64);
+
+    v8h qf[RTW][DS];
+    float rc[RTW];
+#pragma unroll
+    for (int rt = 0; rt < RTW; ++rt) {
+        const int row = min(wrow + rt * 32 + ql, nrows - 1), s = row / a.group;
+        const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + row - s * a.group) * a.qs[2] + hh * 8;
+        v4i raw[DS];
+#pragma unroll
+        for (int t = 0; t < DS; ++t) raw[t] = *reinterpret_cast<const v4i*>(qp + t * 16);
+        rc[rt] = queries<DT, DS, 32>(raw, a.scale, qf[rt]);
+    }
+    v16f o[RTW][CT];
+    float m[RTW], l[RTW];
+#pragma unroll
+    for (int rt = 0; rt < RTW; ++rt) {
+        m[rt] = -INFINITY; l[rt] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[rt][c][r] = 0.0f;
+    }
+
+    // ---- staging.  K: unit = 16 codes of a key; V: unit = 4 channels of the 8 keys that a lane half holds of 16 (0-3, 8-11 / 4-7, 12-15)
+    v4i kr[KU];
+    uint32_t vr[8];
+    const int kch = tid % (DH / 16), krow = tid / (DH / 16);             // of unit 0; unit 1: 32 rows on
+    const int vch = tid % (DH / 4), voct = (tid / (DH / 4)) & 7;         // Dh = 64: the first 128 threads
+    const bool vmine = DH == 128 || tid < 128;
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            const int key = t * 64 + krow + i * 32;
+            const int blk = max(a.c.block_of(b, min(key >> a.c.log2_block, a.c.max_blocks - 1)), 0);
+            kr[i] = *reinterpret_cast<const v4i*>(a.c.k.codes + (int64_t)blk * a.c.k.s_block + (int64_t)(key & ((1 << a.c.log2_block) - 1)) * a.c.k.s_row +
+                                                  (int64_t)h * a.c.k.s_head + kch * 16);
+        }
+        if (vmine) {
+            const int key = t * 64 + (voct >> 1) * 16 + (voct & 1) * 4;
+            const int blk = a.c.block_of(b, min(key >> a.c.log2_block, a.c.max_blocks - 1));
+            const uint8_t* const vp = a.c.v.codes + (int64_t)max(blk, 0) * a.c.v.s_block + (int64_t)(key & ((1 << a.c.log2_block) - 1)) * a.c.v.s_row +
+                                      (int64_t)h * a.c.v.s_head + vch * 4;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) vr[j] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)((j >> 2) * 8 + (j & 3)) * a.c.v.s_row);
+            if (t * 64 + 64 > len || blk < 0)                            // what lies behind the last key is no code
+#pragma unroll
+                for (int j = 0; j < 8; ++j) vr[j] = key + (j >> 2) * 8 + (j & 3) < len && blk >= 0 ? vr[j] : 0u;
+        }
+    };
+    auto stage = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            const int row = krow + i * 32;
+            const int sw = DH == 128 ? row & 15 : (row >> 1) & 7;
+            const v8h x0 = codes8<FMT>((uint32_t)kr[i][0], (uint32_t)kr[i][1]), x1 = codes8<FMT>((uint32_t)kr[i][2], (uint32_t)kr[i][3]);
+            *reinterpret_cast<v8h*>(&sK[buf][row * KROW + ((2 * kch) ^ sw) * 16]) = x0;
+            *reinterpret_cast<v8h*>(&sK[buf][row * KROW + ((2 * kch + 1) ^ sw) * 16]) = x1;
+        }
+        if (vmine) {
+            uint32_t w[4][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                pair_of_keys<FMT, 0>(vr[2 * j], vr[2 * j + 1], w[0][j], w[1][j]);
+                pair_of_keys<FMT, 1>(vr[2 * j], vr[2 * j + 1], w[2][j], w[3][j]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = vch * 4 + i, rr = row >> 1;
+                *reinterpret_cast<v4i*>(&sV[buf][row * 128 + (voct ^ (rr & 7) ^ ((rr >> 3) & 1)) * 16]) = v4i{(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3]};
+            }
+        }
+    };
+
+    // scores of 32 keys (s of tile t in buf)
+    typedef v16f Scores[RTW];
+    auto scores = [&](int buf, int s, Scores& acc) __attribute__((always_inline)) {
+#pragma unroll
+        for (int rt = 0; rt < RTW; ++rt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[rt][r] = 0.0f;
+        const int row = s * 32 + ql, sw = DH == 128 ? row & 15 : (row >> 1) & 7;
+#pragma unroll
+        for (int d = 0; d < DS; ++d) {
+            const v8h kf = *reinterpret_cast<const v8h*>(&sK[buf][row * KROW + ((2 * d + hh) ^ sw) * 16]);
+#pragma unroll
+            for (int rt = 0; rt < RTW; ++rt) acc[rt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[rt][d], acc[rt], 0, 0, 0);
+        }
+    };
+    // their exponentials, and the second product
+    struct Group { float ks, lv, iv; int lim; };
+    auto take = [&](int buf, int t, int s, Scores& acc, const Group (&gr)[GH], bool edge) __attribute__((always_inline)) {
+        float cand[RTW], ck[RTW][GH], lv[GH];
+#pragma unroll
+        for (int g = 0; g < GH; ++g) {
+            lv[g] = gr[g].lv;
+#pragma unroll
+            for (int rt = 0; rt < RTW; ++rt) ck[rt][g] = rc[rt] * gr[g].ks;
+        }
+        if (edge) {                              // the exponents themselves, those of hidden keys (of scales that may be NaN) replaced
+#pragma unroll
+            for (int rt = 0; rt < RTW; ++rt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = t * 64 + s * 32 + (r >> 2) * 8 + hh * 4 + (r & 3);
+                    const float x = fmaf(acc[rt][r], ck[rt][r / GE], lv[r / GE]);
+                    acc[rt][r] = key < min(seen[rt], gr[r / GE].lim) ? x : -INFINITY;
+                }
+#pragma unroll
+            for (int g = 0; g < GH; ++g) {
+                lv[g] = 0.0f;
+#pragma unroll
+                for (int rt = 0; rt < RTW; ++rt) ck[rt][g] = 1.0f;
+            }
+        }
+#pragma unroll
+        for (int rt = 0; rt < RTW; ++rt) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int g = 0; g < GH; ++g) {
+                float x = acc[rt][g * GE];
+#pragma unroll
+                for (int r = 1; r < GE; ++r) x = fmaxf(x, acc[rt][g * GE + r]);
+                top = fmaxf(top, fmaf(x, ck[rt][g], lv[g]));
+            }
+            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            cand[rt] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+        }
+        bool raise = cand[0] > m[0] + SLACK;
+#pragma unroll
+        for (int rt = 1; rt < RTW; ++rt) raise |= cand[rt] > m[rt] + SLACK;
+        if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+#pragma unroll
+            for (int rt = 0; rt < RTW; ++rt) {
+                // (a row by its own scores alone: its result does not depend on the others of its wave)
+                const float mn = cand[rt] > m[rt] + SLACK ? cand[rt] : m[rt], resc = mn > m[rt] ? __builtin_amdgcn_exp2f(m[rt] - mn) : 1.0f;
+                m[rt] = mn;
+                l[rt] *= resc;
+#pragma unroll
+                for (int c = 0; c < CT; ++c)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[rt][c][r] *= resc;
+            }
+        }
+        uint32_t p[RTW][8];
+#pragma unroll
+        for (int rt = 0; rt < RTW; ++rt) {
+            const float sub = (m[rt] > -INFINITY ? m[rt] : 0.0f) - (LIFT - SLACK);
+#pragma unroll
+            for (int g = 0; g < GH; ++g) {
+                const float add = lv[g] - sub;
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = g * GE; r < (g + 1) * GE; r += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(acc[rt][r], ck[rt][g], add));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(acc[rt][r + 1], ck[rt][g], add));
+                    sum += e0 + e1;
+                    p[rt][r >> 1] = f16x2(e0, e1);
+                }
+                l[rt] += sum == 0.0f ? 0.0f : sum * gr[g].iv;
+            }
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const int row = c * 32 + ql, rr = row >> 1;
+                const v8h vf = *reinterpret_cast<const v8h*>(&sV[buf][row * 128 + (((s * 2 + st) * 2 + hh) ^ (rr & 7) ^ ((rr >> 3) & 1)) * 16]);
+#pragma unroll
+                for (int rt = 0; rt < RTW; ++rt) {
+                    const v8h pf = __builtin_bit_cast(v8h, v4i{(int)p[rt][4 * st], (int)p[rt][4 * st + 1], (int)p[rt][4 * st + 2], (int)p[rt][4 * st + 3]});
+                    o[rt][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[rt][c], 0, 0, 0);
+                }
+            }
+    };
+    // the scales of a tile's keys; a group without a block has no keys
+    auto groups = [&](int t, Group (&gr)[2][GH], bool& hole) __attribute__((always_inline)) {
+        hole = false;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int g = 0; g < GH; ++g) {
+                const int key = t * 64 + s * 32 + g * (32 / GH);
+                const int blk = key < last ? a.c.block_of(b, key >> a.c.log2_block) : -1;
+                const int64_t at = (int64_t)max(blk, 0) * a.c.H + h;
+                const float vs = a.c.v.scale[at];
+                gr[s][g].ks = a.c.k.scale[at];
+                gr[s][g].lv = __builtin_amdgcn_logf(vs);
+                gr[s][g].iv = 1.0f / vs;
+                gr[s][g].lim = blk < 0 ? 0 : 0x7fffffff;
+                hole |= blk < 0;
+            }
+    };
+
+    if (t0 < t1) {
+        fetch(t0);
+        stage(t0 % NB);
+        if (t0 + 1 < t1) fetch(t0 + 1);
+    }
+    __syncthreads();
+    Scores acc, next;
+    if (t0 < wt) scores(t0 % NB, 0, acc);
+    for (int t = t0; t < t1; ++t) {
+        const int buf = t % NB, after = (t + 1) % NB;
+        Group gr[2][GH];
+        bool hole;
+        groups(t, gr, hole);
+        const bool edge = t * 64 + 64 > wall || hole;
+        if (t < wt) {
+            scores(buf, 1, next);
+            take(buf, t, 0, acc, gr[0], edge);
+        }
+        if (t + 1 < t1) stage(after);
+        __syncthreads();
+        if (t + 2 < t1) fetch(t + 2);
+        if (t < wt) {
+            if (t + 1 < wt) scores(after, 0, acc);
+            take(buf, t, 1, next, gr[1], edge);
+        }
+    }
+
+#pragma unroll
+    for (int rt = 0; rt < RTW; ++rt) {
+        l[rt] += __shfl_xor(l[rt], 32);
+        const int row = wrow + rt * 32 + ql;
+        if (row >= nrows) continue;
+        if (a.splits > 1) {
+            const int64_t pr = ((int64_t)bh * nrows + row) * a.splits + split;
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<v4f*>(a.part + pr * DH + c * 32 + g * 8 + hh * 4) = v4f{o[rt][c][4 * g], o[rt][c][4 * g + 1], o[rt][c][4 * g + 2], o[rt][c][4 * g + 3]};
+            if (hh == 0) { a.part_ml[pr * 2] = m[rt]; a.part_ml[pr * 2 + 1] = l[rt]; }
+        } else {
+            const float inv = m[rt] == INFINITY ? __builtin_nanf("") : (l[rt] == 0.0f ? 0.0f : 1.0f / l[rt]);
+            const int s = row / a.group;
+            uint16_t* const op = a.out + ((int64_t)b * a.Sq + s) * a.ldo + (int64_t)(h * a.group + row - s * a.group) * DH;
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<v2i*>(op + c * 32 + g * 8 + hh * 4) =
+                        v2i{(int)pack2_hp<DT>(o[rt][c][4 * g] * inv, o[rt][c][4 * g + 1] * inv), (int)pack2_hp<DT>(o[rt][c][4 * g + 2] * inv, o[rt][c][4 * g + 3] * inv)};
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
 // The pieces of the keys joined: DH / 4 threads per row, added in the order of the pieces.
 // ------------------------------------------------------------------------------------------
 template <int DH, int DT>
@@ -380,18 +680,19 @@ __global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, i
     if (i < rows * cols) out[(i / cols) * ld + i % cols] = 0;
 }
 
-// How a call is cut: 16 RT rows to a tile, the keys into pieces.
-struct Plan { int rt, tiles, splits; };
+// How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 128 rtw of that of many; the keys into pieces.
+struct Plan { int rt, rtw, tiles, splits; };
 
 Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq) {
     Plan p;
-    const int64_t rows = Sq * (Hq / c->H);
+    const int64_t rows = Sq * (Hq / c->H), bh = c->B * c->H, steps = (c->max_blocks * c->block + 31) / 32;
     p.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int64_t tiles = (rows + 16 * p.rt - 1) / (16 * p.rt);
-    p.tiles = (int)tiles;
-    const int64_t units = c->B * c->H * tiles, steps = (c->max_blocks * c->block + 31) / 32;
-    // pieces of 16 steps or more while there are fewer than four workgroups per CU
-    int64_t s = (1024 + units - 1) / units;
+    p.rtw = rows > 128 ? 2 : 0;
+    const int64_t tile = p.rtw ? 128 * p.rtw : 16 * p.rt;
+    p.tiles = (int)((rows + tile - 1) / tile);
+    const int64_t units = bh * p.tiles;
+    // pieces of 16 steps or more while there are fewer than four workgroups per CU (one, of many rows)
+    int64_t s = ((p.rtw ? 256 : 1024) + units - 1) / units;
     s = s < steps / 16 ? s : steps / 16;
     p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
     return p;
@@ -409,11 +710,18 @@ size_t part_bytes(const hero_kv_cache* c, int64_t Hq, int64_t Sq, int splits) {
 }
 
 template <int DH, int FMT, int DT>
-hero_status launch(const AttnArgs& a, int rt, int64_t nb, hipStream_t st) {
-    const dim3 grid((unsigned)nb), block(256);
-    if (rt == 1) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 1, 4>), grid, block, 0, st, a);
-    else if (rt == 2) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 2, 4>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 4, 4>), grid, block, 0, st, a);
+hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
+    const dim3 block(256);
+    if (p.rtw) {
+        const dim3 grid((unsigned)(((int64_t)a.B * a.c.H + 7) / 8 * 8 * a.tiles * a.splits));
+        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 2, 2>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 2, 1>), grid, block, 0, st, a);
+    } else {
+        const dim3 grid((unsigned)((int64_t)a.B * a.c.H * a.tiles * a.splits));
+        if (p.rt == 1) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 1, 4>), grid, block, 0, st, a);
+        else if (p.rt == 2) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 2, 4>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 4, 4>), grid, block, 0, st, a);
+    }
     hero_status r = hero_launch_status();
     if (r != HERO_OK || a.splits == 1) return r;
     const int64_t rows = (int64_t)a.B * a.c.H * a.Sq * a.group;
@@ -452,7 +760,7 @@ extern "C" hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, c
     }
     Plan p = plan(cache, Hq, Sq);
     if (!workspace || workspace_bytes < part_bytes(cache, Hq, Sq, p.splits)) p.splits = 1;
-    const int64_t nb = cache->B * cache->H * p.tiles * p.splits;
+    const int64_t nb = (cache->B * cache->H + 7) / 8 * 8 * p.tiles * p.splits;
     if (nb > 0x7fffffffLL || cache->B * Sq * Hq * (Dh / 4) / 256 > 0x7ffffffeLL) return HERO_ERR_SHAPE;
     AttnArgs a;
     a.c = kv_view(cache);
@@ -462,7 +770,7 @@ extern "C" hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, c
     a.scale = scale; a.causal = mask == HERO_MASK_CAUSAL; a.kv_len = kv_len; a.new_len = new_len;
     a.out = (uint16_t*)out; a.ldo = ldo; a.tiles = p.tiles; a.splits = p.splits;
     a.part = (float*)workspace; a.part_ml = a.part + (p.splits > 1 ? cache->B * Sq * Hq * p.splits * Dh : 0);
-#define HERO_KVA(DH, FMT) (dt == HERO_BF16 ? launch<DH, FMT, HERO_BF16>(a, p.rt, nb, st) : launch<DH, FMT, HERO_F16>(a, p.rt, nb, st))
+#define HERO_KVA(DH, FMT) (dt == HERO_BF16 ? launch<DH, FMT, HERO_BF16>(a, p, st) : launch<DH, FMT, HERO_F16>(a, p, st))
     if (cache->dt == HERO_I8) return Dh == 64 ? HERO_KVA(64, HERO_I8) : HERO_KVA(128, HERO_I8);
     return Dh == 64 ? HERO_KVA(64, HERO_F8E4M3) : HERO_KVA(128, HERO_F8E4M3);
 #undef HERO_KVA
