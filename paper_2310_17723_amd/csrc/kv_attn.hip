@@ -364,10 +364,32 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 // ------------------------------------------------------------------------------------------
 constexpr float SLACK = 7.0f;
 
-template <int DH, int FMT, int DT, int RTW, int GH>          // GH: groups of keys with scales of their own in 32 keys
-__global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(AttnArgs a) {
-    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, GE = 16 / GH;
-    constexpr int KU = DH / 64;                              // 16-byte units of K per thread and tile
+// The order of a step's instructions: vector instructions between the matrix instructions, which run beside them.
+template <int DS, int CT, int RTW, bool STAGE>
+__device__ __forceinline__ void interleave() {
+#define HERO_ORDER(what, count) __builtin_amdgcn_sched_group_barrier(what, count, 0)
+    constexpr int LDS_READ = 0x100, LDS_WRITE = 0x200, MATRIX = 0x008, EXP = 0x400;
+    HERO_ORDER(LDS_READ, 4);
+#pragma unroll
+    for (int i = 0; i < DS; ++i) {
+        HERO_ORDER(MATRIX, RTW);
+        HERO_ORDER(LDS_READ, 1);
+        HERO_ORDER(EXP, 2 * RTW);
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * CT; ++i) {
+        HERO_ORDER(MATRIX, RTW);
+        HERO_ORDER(LDS_READ, 1);
+        if constexpr (STAGE) HERO_ORDER(LDS_WRITE, 1);
+    }
+#undef HERO_ORDER
+}
+
+template <int DH, int FMT, int DT, int NW, int RTW, int GH>          // GH: groups of keys with scales of their own in 32 keys
+__global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
+    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, GE = 16 / GH, NT = 64 * NW, ROWS = 32 * RTW * NW;
+    constexpr int KU = 4 * DH / NT > 1 ? 4 * DH / NT : 1;    // 16-byte units of K per thread and tile (Dh = 64: half of the threads do the other half's again)
+    constexpr int VQ = 16 * DH / 4 / NT > 1 ? 16 * DH / 4 / NT : 1;    // units of V: 4 channels of 4 keys
     __shared__ __attribute__((aligned(1024))) uint8_t sK[NB][64 * KROW], sV[NB][DH * 128];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, ql = lane & 31;
     int u = blockIdx.x;
@@ -381,7 +403,7 @@ __global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(Att
     const int h = bh % a.c.H, b = bh / a.c.H;
     const int len = min(max(a.kv_len[b], 0), a.c.max_blocks << a.c.log2_block);
     const int n = a.new_len ? min(max(a.new_len[b], 0), a.Sq) : a.Sq;
-    const int row0 = tile * 128 * RTW, wrow = row0 + wave * 32 * RTW;
+    const int row0 = tile * ROWS, wrow = row0 + wave * 32 * RTW;
     auto range = [&](int r0, int count, int& all, int& last) {           // of rows [r0, r0 + count): keys that all / any of them see
         const int r1 = min(r0 + count, nrows) - 1;
         last = r0 >= n * a.group ? 0 : max(keys_seen(a, r0, len, n), keys_seen(a, min(r1, n * a.group - 1), len, n));
@@ -390,7 +412,7 @@ __global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(Att
         all = __builtin_amdgcn_readfirstlane(all);
     };
     int all, last, wall, wlast;
-    range(row0, 128 * RTW, all, last);
+    range(row0, ROWS, all, last);
     range(wrow, 32 * RTW, wall, wlast);
     int seen[RTW];
 #pragma unroll
@@ -420,52 +442,64 @@ __global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(Att
             for (int r = 0; r < 16; ++r) o[rt][c][r] = 0.0f;
     }
 
-    // ---- staging.  K: unit = 16 codes of a key; V: unit = 4 channels of the 8 keys that a lane half holds of 16 (0-3, 8-11 / 4-7, 12-15)
+    // ---- staging.  K: unit = 16 codes of a key; V: unit = 4 channels of 4 keys.  A lane half holds 8 keys of 16 (0-3, 8-11 / 4-7, 12-15)
     v4i kr[KU];
-    uint32_t vr[8];
-    const int kch = tid % (DH / 16), krow = tid / (DH / 16);             // of unit 0; unit 1: 32 rows on
-    const int vch = tid % (DH / 4), voct = (tid / (DH / 4)) & 7;         // Dh = 64: the first 128 threads
-    const bool vmine = DH == 128 || tid < 128;
+    uint32_t vr[VQ][4];
+    int vend[VQ];                                                        // how many keys there are from a unit's first on
+    const int kch = tid % (DH / 16), krow = tid / (DH / 16) % 64;        // of unit 0; the next: NT / (DH / 16) rows on
+    const int vch = tid % (DH / 4), vq = tid / (DH / 4) % 16;            // of unit 0; the next: NT / (DH / 4) quads on
     auto fetch = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
-            const int key = t * 64 + krow + i * 32;
+            const int key = t * 64 + krow + i * (NT / (DH / 16));
             const int blk = max(a.c.block_of(b, min(key >> a.c.log2_block, a.c.max_blocks - 1)), 0);
             kr[i] = *reinterpret_cast<const v4i*>(a.c.k.codes + (int64_t)blk * a.c.k.s_block + (int64_t)(key & ((1 << a.c.log2_block) - 1)) * a.c.k.s_row +
                                                   (int64_t)h * a.c.k.s_head + kch * 16);
         }
-        if (vmine) {
-            const int key = t * 64 + (voct >> 1) * 16 + (voct & 1) * 4;
+#pragma unroll
+        for (int i = 0; i < VQ; ++i) {
+            const int key = t * 64 + (vq + i * (NT / (DH / 4))) * 4;
             const int blk = a.c.block_of(b, min(key >> a.c.log2_block, a.c.max_blocks - 1));
             const uint8_t* const vp = a.c.v.codes + (int64_t)max(blk, 0) * a.c.v.s_block + (int64_t)(key & ((1 << a.c.log2_block) - 1)) * a.c.v.s_row +
                                       (int64_t)h * a.c.v.s_head + vch * 4;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) vr[j] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)((j >> 2) * 8 + (j & 3)) * a.c.v.s_row);
-            if (t * 64 + 64 > len || blk < 0)                            // what lies behind the last key is no code
-#pragma unroll
-                for (int j = 0; j < 8; ++j) vr[j] = key + (j >> 2) * 8 + (j & 3) < len && blk >= 0 ? vr[j] : 0u;
+            for (int j = 0; j < 4; ++j) vr[i][j] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)j * a.c.v.s_row);
+            vend[i] = blk < 0 ? 0 : len - key;
         }
+    };
+    // what lies behind the last key, or where no block is, is no code
+    auto blank = [&]() __attribute__((always_inline)) {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < VQ; ++i) any |= vend[i] < 4;
+        if (__builtin_amdgcn_ballot_w64(any) != 0)
+#pragma unroll
+            for (int i = 0; i < VQ; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) vr[i][j] = j < vend[i] ? vr[i][j] : 0u;
     };
     auto stage = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
-            const int row = krow + i * 32;
+            const int row = krow + i * (NT / (DH / 16));
             const int sw = DH == 128 ? row & 15 : (row >> 1) & 7;
             const v8h x0 = codes8<FMT>((uint32_t)kr[i][0], (uint32_t)kr[i][1]), x1 = codes8<FMT>((uint32_t)kr[i][2], (uint32_t)kr[i][3]);
             *reinterpret_cast<v8h*>(&sK[buf][row * KROW + ((2 * kch) ^ sw) * 16]) = x0;
             *reinterpret_cast<v8h*>(&sK[buf][row * KROW + ((2 * kch + 1) ^ sw) * 16]) = x1;
         }
-        if (vmine) {
-            uint32_t w[4][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                pair_of_keys<FMT, 0>(vr[2 * j], vr[2 * j + 1], w[0][j], w[1][j]);
-                pair_of_keys<FMT, 1>(vr[2 * j], vr[2 * j + 1], w[2][j], w[3][j]);
+        for (int u = 0; u < VQ; ++u) {
+            const int quad = vq + u * (NT / (DH / 4)), piece = (quad >> 2) * 2 + (quad & 1);
+            uint32_t w[4][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                pair_of_keys<FMT, 0>(vr[u][2 * j], vr[u][2 * j + 1], w[0][j], w[1][j]);
+                pair_of_keys<FMT, 1>(vr[u][2 * j], vr[u][2 * j + 1], w[2][j], w[3][j]);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int row = vch * 4 + i, rr = row >> 1;
-                *reinterpret_cast<v4i*>(&sV[buf][row * 128 + (voct ^ (rr & 7) ^ ((rr >> 3) & 1)) * 16]) = v4i{(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3]};
+                *reinterpret_cast<v2i*>(&sV[buf][row * 128 + (piece ^ (rr & 7) ^ ((rr >> 3) & 1)) * 16 + ((quad >> 1) & 1) * 8]) = v2i{(int)w[i][0], (int)w[i][1]};
             }
         }
     };
@@ -473,22 +507,20 @@ __global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(Att
     // scores of 32 keys (s of tile t in buf)
     typedef v16f Scores[RTW];
     auto scores = [&](int buf, int s, Scores& acc) __attribute__((always_inline)) {
-#pragma unroll
-        for (int rt = 0; rt < RTW; ++rt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[rt][r] = 0.0f;
+        const v16f zero = {};
         const int row = s * 32 + ql, sw = DH == 128 ? row & 15 : (row >> 1) & 7;
 #pragma unroll
         for (int d = 0; d < DS; ++d) {
             const v8h kf = *reinterpret_cast<const v8h*>(&sK[buf][row * KROW + ((2 * d + hh) ^ sw) * 16]);
 #pragma unroll
-            for (int rt = 0; rt < RTW; ++rt) acc[rt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[rt][d], acc[rt], 0, 0, 0);
+            for (int rt = 0; rt < RTW; ++rt) acc[rt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[rt][d], d ? acc[rt] : zero, 0, 0, 0);
         }
     };
     // their exponentials, and the second product
     struct Group { float ks, lv, iv; int lim; };
-    auto take = [&](int buf, int t, int s, Scores& acc, const Group (&gr)[GH], bool edge) __attribute__((always_inline)) {
-        float cand[RTW], ck[RTW][GH], lv[GH];
+    float ck[RTW][GH], lv[GH];
+    auto raise = [&](int t, int s, Scores& acc, const Group (&gr)[GH], bool edge) __attribute__((always_inline)) {
+        float cand[RTW];
 #pragma unroll
         for (int g = 0; g < GH; ++g) {
             lv[g] = gr[g].lv;
@@ -524,10 +556,10 @@ __global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(Att
             const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             cand[rt] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
         }
-        bool raise = cand[0] > m[0] + SLACK;
+        bool above = cand[0] > m[0] + SLACK;
 #pragma unroll
-        for (int rt = 1; rt < RTW; ++rt) raise |= cand[rt] > m[rt] + SLACK;
-        if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+        for (int rt = 1; rt < RTW; ++rt) above |= cand[rt] > m[rt] + SLACK;
+        if (__builtin_amdgcn_ballot_w64(above) != 0) {
 #pragma unroll
             for (int rt = 0; rt < RTW; ++rt) {
                 // (a row by its own scores alone: its result does not depend on the others of its wave)
@@ -540,6 +572,8 @@ __global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(Att
                     for (int r = 0; r < 16; ++r) o[rt][c][r] *= resc;
             }
         }
+    };
+    auto take = [&](int buf, int s, Scores& acc, const Group (&gr)[GH]) __attribute__((always_inline)) {
         uint32_t p[RTW][8];
 #pragma unroll
         for (int rt = 0; rt < RTW; ++rt) {
@@ -590,30 +624,39 @@ __global__ __launch_bounds__(256, RTW == 2 ? 1 : 2) void kv_attn_tile_kernel(Att
             }
     };
 
+    Scores acc, next;
     if (t0 < t1) {
         fetch(t0);
+        blank();
         stage(t0 % NB);
-        if (t0 + 1 < t1) fetch(t0 + 1);
+        fetch(min(t0 + 1, t1 - 1));
     }
     __syncthreads();
-    Scores acc, next;
     if (t0 < wt) scores(t0 % NB, 0, acc);
+    // (behind the last tile the last one is fetched and staged again, and scores are made that nobody takes: no branch in the middle)
     for (int t = t0; t < t1; ++t) {
         const int buf = t % NB, after = (t + 1) % NB;
-        Group gr[2][GH];
-        bool hole;
-        groups(t, gr, hole);
-        const bool edge = t * 64 + 64 > wall || hole;
+        blank();
         if (t < wt) {
+            Group gr[2][GH];
+            bool hole;
+            groups(t, gr, hole);
+            const bool edge = t * 64 + 64 > wall || hole;
+            raise(t, 0, acc, gr[0], edge);
             scores(buf, 1, next);
-            take(buf, t, 0, acc, gr[0], edge);
-        }
-        if (t + 1 < t1) stage(after);
-        __syncthreads();
-        if (t + 2 < t1) fetch(t + 2);
-        if (t < wt) {
-            if (t + 1 < wt) scores(after, 0, acc);
-            take(buf, t, 1, next, gr[1], edge);
+            take(buf, 0, acc, gr[0]);
+            stage(after);
+            interleave<DS, CT, RTW, true>();
+            __syncthreads();
+            fetch(min(t + 2, t1 - 1));
+            raise(t, 1, next, gr[1], edge);
+            scores(after, 0, acc);
+            take(buf, 1, next, gr[1]);
+            interleave<DS, CT, RTW, false>();
+        } else {
+            stage(after);
+            __syncthreads();
+            fetch(min(t + 2, t1 - 1));
         }
     }
 
@@ -687,8 +730,8 @@ Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq) {
     Plan p;
     const int64_t rows = Sq * (Hq / c->H), bh = c->B * c->H, steps = (c->max_blocks * c->block + 31) / 32;
     p.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.rtw = rows > 128 ? 2 : 0;
-    const int64_t tile = p.rtw ? 128 * p.rtw : 16 * p.rt;
+    p.rtw = rows > 128 ? 1 : 0;
+    const int64_t tile = p.rtw ? 256 : 16 * p.rt;
     p.tiles = (int)((rows + tile - 1) / tile);
     const int64_t units = bh * p.tiles;
     // pieces of 16 steps or more while there are fewer than four workgroups per CU (one, of many rows)
@@ -714,8 +757,8 @@ hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
     const dim3 block(256);
     if (p.rtw) {
         const dim3 grid((unsigned)(((int64_t)a.B * a.c.H + 7) / 8 * 8 * a.tiles * a.splits));
-        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 2, 2>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 2, 1>), grid, block, 0, st, a);
+        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 2>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 1>), grid, dim3(512), 0, st, a);
     } else {
         const dim3 grid((unsigned)((int64_t)a.B * a.c.H * a.tiles * a.splits));
         if (p.rt == 1) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 1, 4>), grid, block, 0, st, a);
