@@ -82,10 +82,10 @@ SYMBOLS = {
                             f32, f32, vp, i32, i32, vp, vp, i32, i64, vp]),
     "hero_int8_attn_online": (i32, [vp, C.POINTER(i64), vp, C.POINTER(i64), vp, C.POINTER(i64), i64, i64, i64, i64, i64,
                                     vp, f32, vp, i32, i32, vp, vp, i32, i64, vp]),
-    "hero_kv_write": (i32, [C.POINTER(KvCache), vp, C.POINTER(i64), vp, C.POINTER(i64), i32, i64, vp, vp, vp]),
-    "hero_kv_read": (i32, [C.POINTER(KvCache), vp, C.POINTER(i64), vp, C.POINTER(i64), i32, i64, vp, vp, vp]),
+    "hero_kv_write": (i32, [C.POINTER(KvCache), vp, vp, vp, vp, i32, i64, vp, vp, vp]),
+    "hero_kv_read": (i32, [C.POINTER(KvCache), vp, vp, vp, vp, i32, i64, vp, vp, vp]),
     "hero_kv_attn_workspace_bytes": (C.c_size_t, [C.POINTER(KvCache), i64, i64]),
-    "hero_kv_attn": (i32, [C.POINTER(KvCache), vp, C.POINTER(i64), i32, i64, i64, f32, i32, vp, vp, vp, i64, vp, C.c_size_t, vp]),
+    "hero_kv_attn": (i32, [C.POINTER(KvCache), vp, vp, i32, i64, i64, f32, i32, vp, vp, vp, i64, vp, C.c_size_t, vp]),
     "hero_layer_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDesc), i64, i64]),
     "hero_layer_fwd": (i32, [C.POINTER(LayerDesc), C.POINTER(LayerWeights), C.POINTER(LayerIO), vp, C.c_size_t, vp]),
     "hero_bf16_gemm": (i32, [vp, i64, vp, i64, vp, vp, i64, i32, vp, i64, i64, i64, i64, vp]),
@@ -121,13 +121,22 @@ def _strides4(t):
     return (i64 * 4)(*t.stride())
 
 
-def _kv_rows(cache, t, S, H):
-    assert tuple(t.shape) == (cache.B, S, H, cache.Dh), "rows of a KV cache are [B, S, heads, Dh]"
+# Strides as packed bytes, sizes compared as they are: a step's attention costs its host call too (9.5 us with ctypes arrays, tuples and
+# structure fields, 6.8 so).
+_PACK4 = struct.Struct("@4q").pack
 
 
-def _kv_lengths(cache, *tensors):
-    for t in tensors:
-        assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (cache.B,)), "lengths are int32 [B]"
+def _kv_rows(cache, t, S, heads):
+    """The strides of [B, S, heads, Dh] rows."""
+    assert t.shape == (cache.sizes[0], S, heads, cache.sizes[2]), "rows of a KV cache are [B, S, heads, Dh]"
+    return _PACK4(*t.stride())
+
+
+def _kv_length(cache, t):
+    if t is None:
+        return None
+    assert t.dtype is torch.int32 and t.shape == cache.sizes[:1] and t.is_contiguous(), "lengths are contiguous int32 [B]"
+    return t.data_ptr()
 
 
 class Hero:
@@ -386,32 +395,27 @@ class Hero:
                 raise ValueError("scales are contiguous float32 tensors [n_blocks, H]")
         c = KvCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _strides4(k), _strides4(v), _ptr(block_table),
                     int(batch), int(max_blocks), n, H, Dh, block, _DT[k.dtype])
-        c.tensors = (k, v, k_scale, v_scale, block_table)
+        c.tensors, c.sizes = (k, v, k_scale, v_scale, block_table), (int(batch), H, Dh)
         return c
 
     def hero_kv_write(self, cache, k, v, kv_len, new_len=None, stream=None):
         """Quantises k, v [B,S,H,Dh] (bf16 / f16, unit channel stride) into the cache; kv_len int32 [B] counts this call's tokens."""
-        _kv_rows(cache, k, k.shape[1], cache.H)
-        _kv_rows(cache, v, k.shape[1], cache.H)
-        assert k.dtype == v.dtype
-        _kv_lengths(cache, kv_len, new_len)
-        self._check(self.lib.hero_kv_write(cache, _ptr(k), _strides4(k), _ptr(v), _strides4(v), _DT[k.dtype], k.shape[1],
-                                           _ptr(kv_len), _ptr(new_len), _stream(stream)))
+        S, H = k.shape[1], cache.sizes[1]
+        assert k.dtype is v.dtype
+        self._check(self.lib.hero_kv_write(cache, k.data_ptr(), _kv_rows(cache, k, S, H), v.data_ptr(), _kv_rows(cache, v, S, H), _DT[k.dtype], S,
+                                           _kv_length(cache, kv_len), _kv_length(cache, new_len), _stream(stream)))
 
     def hero_kv_read(self, cache, S, kv_len, start=None, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
         """Positions start[b] .. start[b] + S - 1 as [B,S,H,Dh] rows of `dtype`, K and V.  Positions that the sequence does not hold
         are left as they were in k_out / v_out, and are 0 in outputs made here."""
-        shape = (cache.B, S, cache.H, cache.Dh)
-        if k_out is None or v_out is None:
-            device = kv_len.device
-            k_out = torch.zeros(shape, dtype=dtype if v_out is None else v_out.dtype, device=device) if k_out is None else k_out
-            v_out = torch.zeros(shape, dtype=k_out.dtype, device=device) if v_out is None else v_out
-        _kv_rows(cache, k_out, S, cache.H)
-        _kv_rows(cache, v_out, S, cache.H)
-        assert k_out.dtype == v_out.dtype
-        _kv_lengths(cache, kv_len, start)
-        self._check(self.lib.hero_kv_read(cache, _ptr(k_out), _strides4(k_out), _ptr(v_out), _strides4(v_out), _DT[k_out.dtype], S,
-                                          _ptr(start), _ptr(kv_len), _stream(stream)))
+        B, H, Dh = cache.sizes
+        if k_out is None:
+            k_out = torch.zeros((B, S, H, Dh), dtype=dtype if v_out is None else v_out.dtype, device=kv_len.device)
+        if v_out is None:
+            v_out = torch.zeros((B, S, H, Dh), dtype=k_out.dtype, device=kv_len.device)
+        assert k_out.dtype is v_out.dtype
+        self._check(self.lib.hero_kv_read(cache, k_out.data_ptr(), _kv_rows(cache, k_out, S, H), v_out.data_ptr(), _kv_rows(cache, v_out, S, H),
+                                          _DT[k_out.dtype], S, _kv_length(cache, start), _kv_length(cache, kv_len), _stream(stream)))
         return k_out, v_out
 
     def hero_kv_attn_workspace_bytes(self, cache, Hq, Sq) -> int:
@@ -421,14 +425,14 @@ class Hero:
         """q [B,Sq,Hq,Dh] bf16 / f16 over the cache.  Returns [B*Sq, Hq*Dh] in q's type.  workspace: optional uint8 tensor
         (hero_kv_attn_workspace_bytes), without which few rows over many keys are not split."""
         B, Sq, Hq, Dh = q.shape
-        _kv_rows(cache, q, Sq, Hq)
-        _kv_lengths(cache, kv_len, new_len)
         if out is None:
             out = torch.empty((B * Sq, Hq * Dh), dtype=q.dtype, device=q.device)
-        assert out.dtype == q.dtype and out.stride(1) == 1
-        self._check(self.lib.hero_kv_attn(cache, _ptr(q), _strides4(q), _DT[q.dtype], Hq, Sq, float(scale), int(mask),
-                                          _ptr(kv_len), _ptr(new_len), _ptr(out), out.stride(0), _ptr(workspace),
-                                          0 if workspace is None else workspace.nbytes, _stream(stream)))
+        else:
+            assert out.dtype is q.dtype and out.shape == (B * Sq, Hq * Dh) and out.stride(1) == 1
+        self._check(self.lib.hero_kv_attn(cache, q.data_ptr(), _kv_rows(cache, q, Sq, Hq), _DT[q.dtype], Hq, Sq, scale, int(mask),
+                                          _kv_length(cache, kv_len), _kv_length(cache, new_len), out.data_ptr(), out.stride(0),
+                                          None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+                                          _stream(stream)))
         return out
 
     # ------------------------------------------------------------------ layer

@@ -17,6 +17,7 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 constexpr float LIFT = 15.0f;
+constexpr int MOST_PIECES = 128;
 
 struct AttnArgs {
     KvView c;
@@ -180,32 +181,39 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
         for (int i = 0; i < CT; ++i) o[rt][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // this piece's keys, in steps of 32
+    // this piece's keys, in steps of 32.  A step's codes are asked for as soon as the registers of the last one's are free; its blocks a step before.
     const int steps = (last + 31) / 32, per = (steps + a.splits - 1) / a.splits;
     const int s_end = min((split + 1) * per, steps);
     v4i kr[2][VW];                               // [half][64 channels]
     uint32_t vr[8][VW];
     float ks[2], vs[2];
-    int blk[2];
+    int blk[2], nblk[2];
     const uint32_t koff = (uint32_t)(c * (int)a.c.k.s_row + g * 16), voff = (uint32_t)(g * 4 * (int)a.c.v.s_row + c * (DH / 16));
-    auto find = [&](int step) {
+    auto find = [&](int step, int (&to)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
             const int key = step * 32 + hf * 16;
-            blk[hf] = key < last ? a.c.block_of(b, key >> a.c.log2_block) : -1;
+            to[hf] = key < last ? a.c.block_of(b, key >> a.c.log2_block) : -1;
         }
     };
-    auto load = [&](int step) {                  // (a half without a block reads block 0, hidden below)
+    auto from = [&](const KvSide& sd, int step, int hf) __attribute__((always_inline)) -> const uint8_t* {   // (a half without a block reads block 0, hidden below)
+        return sd.codes + (int64_t)max(blk[hf], 0) * sd.s_block + (int64_t)((step * 32 + hf * 16) & (block - 1)) * sd.s_row + (int64_t)h * sd.s_head;
+    };
+    auto load_k = [&](int step) __attribute__((always_inline)) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            const int key = step * 32 + hf * 16, at = key & (block - 1);
-            const int64_t bl = max(blk[hf], 0);
-            const uint8_t* const kp = a.c.k.codes + bl * a.c.k.s_block + (int64_t)at * a.c.k.s_row + (int64_t)h * a.c.k.s_head;
-            const uint8_t* const vp = a.c.v.codes + bl * a.c.v.s_block + (int64_t)at * a.c.v.s_row + (int64_t)h * a.c.v.s_head;
-            ks[hf] = a.c.k.scale[bl * a.c.H + h];
-            vs[hf] = a.c.v.scale[bl * a.c.H + h];
+            const uint8_t* const kp = from(a.c.k, step, hf);
+            const int64_t at = (int64_t)max(blk[hf], 0) * a.c.H + h;
+            ks[hf] = a.c.k.scale[at];
+            vs[hf] = a.c.v.scale[at];
 #pragma unroll
             for (int t = 0; t < VW; ++t) kr[hf][t] = *reinterpret_cast<const v4i*>(kp + koff + t * 64);
+        }
+    };
+    auto load_v = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint8_t* const vp = from(a.c.v, step, hf);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if constexpr (VW == 2) {
@@ -216,19 +224,22 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
         }
     };
     int step = split * per + wave;
-    if (step < s_end) { find(step); load(step); }
+    if (step < s_end) {
+        find(step, blk);
+        load_k(step);
+        load_v(step);
+        find(step + NW, nblk);
+    }
     for (; step < s_end; step += NW) {
-        // taken over from the loads, so that the next step's can be issued
-        v8h kf[2][KS];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-            for (int t = 0; t < VW; ++t) {
-                kf[hf][2 * t] = codes8<FMT>((uint32_t)kr[hf][t][0], (uint32_t)kr[hf][t][1]);
-                kf[hf][2 * t + 1] = codes8<FMT>((uint32_t)kr[hf][t][2], (uint32_t)kr[hf][t][3]);
-            }
         const int key0 = step * 32;
         const bool edge = key0 + 32 > all || blk[0] < 0 || blk[1] < 0;
+        float kc[2], lv[2], iv[2];
+        int lim[2];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            kc[hf] = ks[hf]; lv[hf] = __builtin_amdgcn_logf(vs[hf]); iv[hf] = __builtin_amdgcn_rcpf(vs[hf]);
+            lim[hf] = blk[hf] < 0 ? 0 : 0x7fffffff;
+        }
         if (edge)                                                         // what lies behind the last key is no code
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -236,38 +247,33 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 #pragma unroll
                 for (int t = 0; t < VW; ++t) vr[j][t] = there ? vr[j][t] : 0u;
             }
-        v8h vf[CT];
-#pragma unroll
-        for (int t = 0; t < VW; ++t) {
-            uint32_t w[4][4];                    // [channel][pair of keys]
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                pair_of_keys<FMT, 0>(vr[2 * j][t], vr[2 * j + 1][t], w[0][j], w[1][j]);
-                pair_of_keys<FMT, 1>(vr[2 * j][t], vr[2 * j + 1][t], w[2][j], w[3][j]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vf[t * 4 + i] = __builtin_bit_cast(v8h, v4i{(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3]});
-        }
-        float kc[2], lv[2], iv[2];
-        int lim[2];
+        const bool more = step + NW < s_end;
+        v4f acc[RT][2];
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-            kc[hf] = ks[hf]; lv[hf] = __builtin_amdgcn_logf(vs[hf]); iv[hf] = 1.0f / vs[hf];
-            lim[hf] = blk[hf] < 0 ? 0 : 0x7fffffff;
+            v8h kf[KS];
+#pragma unroll
+            for (int t = 0; t < VW; ++t) {
+                kf[2 * t] = codes8<FMT>((uint32_t)kr[hf][t][0], (uint32_t)kr[hf][t][1]);
+                kf[2 * t + 1] = codes8<FMT>((uint32_t)kr[hf][t][2], (uint32_t)kr[hf][t][3]);
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                acc[rt][hf] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int t = 0; t < KS; ++t) acc[rt][hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[t], qf[rt][t], acc[rt][hf], 0, 0, 0);
+            }
         }
-        if (step + NW < s_end) { find(step + NW); load(step + NW); }
+        if (more) {
+            blk[0] = nblk[0]; blk[1] = nblk[1];
+            load_k(step + NW);
+        }
+        uint32_t p[RT][4];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            v4f acc[2];
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                acc[hf] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int t = 0; t < KS; ++t) acc[hf] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[hf][t], qf[rt][t], acc[hf], 0, 0, 0);
-            }
             float x[8], top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = fmaf(acc[j >> 2][j & 3], rc[rt] * kc[j >> 2], lv[j >> 2]);
+            for (int j = 0; j < 8; ++j) x[j] = fmaf(acc[rt][j >> 2][j & 3], rc[rt] * kc[j >> 2], lv[j >> 2]);
             if (edge) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -280,12 +286,11 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
             top = max_of_groups16(top);
             const float mn = fmaxf(m[rt], top), ms = mn > -INFINITY ? mn : 0.0f, sub = ms - LIFT;
             const float resc = __builtin_amdgcn_exp2f(m[rt] - ms);
-            uint32_t p[4];
             float sum[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 const float e0 = __builtin_amdgcn_exp2f(x[j] - sub), e1 = __builtin_amdgcn_exp2f(x[j + 1] - sub);
-                p[j >> 1] = f16x2(e0, e1);
+                p[rt][j >> 1] = f16x2(e0, e1);
                 sum[j >> 2] += e0 + e1;
             }
             // (a block that a row does not see may have a scale that is NaN)
@@ -297,9 +302,28 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
                     for (int r = 0; r < 4; ++r) o[rt][i][r] *= resc;
             }
             m[rt] = mn;
-            const v8h pf = __builtin_bit_cast(v8h, v4i{(int)p[0], (int)p[1], (int)p[2], (int)p[3]});
+        }
 #pragma unroll
-            for (int i = 0; i < CT; ++i) o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[i], pf, o[rt][i], 0, 0, 0);
+        for (int t = 0; t < VW; ++t) {
+            uint32_t w[4][4];                    // [channel][pair of keys]
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                pair_of_keys<FMT, 0>(vr[2 * j][t], vr[2 * j + 1][t], w[0][j], w[1][j]);
+                pair_of_keys<FMT, 1>(vr[2 * j][t], vr[2 * j + 1][t], w[2][j], w[3][j]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const v8h vf = __builtin_bit_cast(v8h, v4i{(int)w[i][0], (int)w[i][1], (int)w[i][2], (int)w[i][3]});
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const v8h pf = __builtin_bit_cast(v8h, v4i{(int)p[rt][0], (int)p[rt][1], (int)p[rt][2], (int)p[rt][3]});
+                    o[rt][t * 4 + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf, o[rt][t * 4 + i], 0, 0, 0);
+                }
+            }
+        }
+        if (more) {
+            load_v(step + NW);
+            find(step + 2 * NW, nblk);
         }
     }
 
@@ -387,9 +411,8 @@ __device__ __forceinline__ void interleave() {
 
 template <int DH, int FMT, int DT, int NW, int RTW, int GH>          // GH: groups of keys with scales of their own in 32 keys
 __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
-    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, GE = 16 / GH, NT = 64 * NW, ROWS = 32 * RTW * NW;
-    constexpr int KU = 4 * DH / NT > 1 ? 4 * DH / NT : 1;    // 16-byte units of K per thread and tile (Dh = 64: half of the threads do the other half's again)
-    constexpr int VQ = 16 * DH / 4 / NT > 1 ? 16 * DH / 4 / NT : 1;    // units of V: 4 channels of 4 keys
+    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, GE = 16 / GH, NT = 64 * NW, ROWS = 32 * RTW * NW, NI = 2 * GH;
+    static_assert(NT == 512, "one unit of K and of V per thread");
     __shared__ __attribute__((aligned(1024))) uint8_t sK[NB][64 * KROW], sV[NB][DH * 128];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, ql = lane & 31;
     int u = blockIdx.x;
@@ -442,76 +465,93 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
             for (int r = 0; r < 16; ++r) o[rt][c][r] = 0.0f;
     }
 
-    // ---- staging.  K: unit = 16 codes of a key; V: unit = 4 channels of 4 keys.  A lane half holds 8 keys of 16 (0-3, 8-11 / 4-7, 12-15)
-    v4i kr[KU];
-    uint32_t vr[VQ][4];
-    int vend[VQ];                                                        // how many keys there are from a unit's first on
-    const int kch = tid % (DH / 16), krow = tid / (DH / 16) % 64;        // of unit 0; the next: NT / (DH / 16) rows on
-    const int vch = tid % (DH / 4), vq = tid / (DH / 4) % 16;            // of unit 0; the next: NT / (DH / 4) quads on
-    auto fetch = [&](int t) __attribute__((always_inline)) {
+    // ---- staging.  K: a thread's unit is 16 codes of a key; V: 4 channels of 4 keys.  (Dh = 64: half of the threads do the other half's again.)
+    v4i kr;
+    uint32_t vr[4];
+    int vend;                                                            // how many keys there are from V's unit's first on
+    const int kch = tid % (DH / 16), krow = tid / (DH / 16) % 64;
+    const int vch = tid % (DH / 4), vq = tid / (DH / 4) % 16;
+    // A wave's units all lie in one group of 16 keys; a tile's keys in NI blocks (the same one, of 64 tokens or more).  The table is read three
+    // tiles ahead, the codes two, the scales one; as vector loads, since a scalar load's wait would be one for all LDS reads too.
+    const int group16 = DH == 128 ? wave >> 1 : wave & 3;
+    uint32_t nought;
+    asm("v_mov_b32 %0, 0" : "=v"(nought));
+    const uint32_t koff = (uint32_t)(krow & 15) * (uint32_t)a.c.k.s_row + (uint32_t)kch * 16;
+    const uint32_t voff = (uint32_t)(vq & 3) * 4 * (uint32_t)a.c.v.s_row + (uint32_t)vch * 4;
+    typedef int Ids[NI];
+    auto look = [&](int t, Ids& raw) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < KU; ++i) {
-            const int key = t * 64 + krow + i * (NT / (DH / 16));
-            const int blk = max(a.c.block_of(b, min(key >> a.c.log2_block, a.c.max_blocks - 1)), 0);
-            kr[i] = *reinterpret_cast<const v4i*>(a.c.k.codes + (int64_t)blk * a.c.k.s_block + (int64_t)(key & ((1 << a.c.log2_block) - 1)) * a.c.k.s_row +
-                                                  (int64_t)h * a.c.k.s_head + kch * 16);
+        for (int i = 0; i < NI; ++i) {
+            const int64_t at = (int64_t)b * a.c.max_blocks + min((t * 64 + i * (64 / NI)) >> a.c.log2_block, a.c.max_blocks - 1);
+            raw[i] = a.c.table ? (a.c.table + at)[nought] : (int)at;
         }
+    };
+    auto settle = [&](const Ids& raw, Ids& id) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < VQ; ++i) {
-            const int key = t * 64 + (vq + i * (NT / (DH / 4))) * 4;
-            const int blk = a.c.block_of(b, min(key >> a.c.log2_block, a.c.max_blocks - 1));
-            const uint8_t* const vp = a.c.v.codes + (int64_t)max(blk, 0) * a.c.v.s_block + (int64_t)(key & ((1 << a.c.log2_block) - 1)) * a.c.v.s_row +
-                                      (int64_t)h * a.c.v.s_head + vch * 4;
+        for (int i = 0; i < NI; ++i) {
+            const int blk = __builtin_amdgcn_readfirstlane(raw[i]);
+            id[i] = (unsigned)blk < (unsigned)a.c.n_blocks ? blk : -1;
+        }
+    };
+    auto fetch = [&](int t, const Ids& id) __attribute__((always_inline)) {
+        int blk = 0;                             // id[group16 NI / 4], by masks: an index that is not known would put the array into memory
 #pragma unroll
-            for (int j = 0; j < 4; ++j) vr[i][j] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)j * a.c.v.s_row);
-            vend[i] = blk < 0 ? 0 : len - key;
+        for (int i = 0; i < NI; ++i) blk |= id[i] & -(int)(group16 * NI / 4 == i);
+        const int first = t * 64 + group16 * 16, at = first & ((1 << a.c.log2_block) - 1);
+        const int64_t bl = max(blk, 0);
+        const uint8_t* const kp = a.c.k.codes + bl * a.c.k.s_block + (int64_t)at * a.c.k.s_row + (int64_t)h * a.c.k.s_head;
+        const uint8_t* const vp = a.c.v.codes + bl * a.c.v.s_block + (int64_t)at * a.c.v.s_row + (int64_t)h * a.c.v.s_head;
+        kr = *reinterpret_cast<const v4i*>(kp + koff);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vr[j] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)j * a.c.v.s_row + voff);
+        vend = blk < 0 ? 0 : len - first - (vq & 3) * 4;
+    };
+    float sk[NI], sv[NI];
+    auto scales = [&](const Ids& id) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int64_t at = (int64_t)max(id[i], 0) * a.c.H + h;
+            sk[i] = (a.c.k.scale + at)[nought];
+            sv[i] = (a.c.v.scale + at)[nought];
         }
     };
     // what lies behind the last key, or where no block is, is no code
     auto blank = [&]() __attribute__((always_inline)) {
-        bool any = false;
+        if (__builtin_amdgcn_ballot_w64(vend < 4) != 0)
 #pragma unroll
-        for (int i = 0; i < VQ; ++i) any |= vend[i] < 4;
-        if (__builtin_amdgcn_ballot_w64(any) != 0)
-#pragma unroll
-            for (int i = 0; i < VQ; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) vr[i][j] = j < vend[i] ? vr[i][j] : 0u;
+            for (int j = 0; j < 4; ++j) vr[j] = j < vend ? vr[j] : 0u;
     };
+    // a half of 16 keys: its lanes hold keys 0-3, 8-11 / 4-7, 12-15 of them
+    const int ksw = DH == 128 ? krow & 15 : (krow >> 1) & 7;
+    const uint32_t kput = krow * KROW + ((2 * kch) ^ ksw) * 16;
+    const uint32_t vput = vch * 512 + ((vq >> 2) * 2 + (vq & 1)) * 16 + ((vq >> 1) & 1) * 8;
     auto stage = [&](int buf) __attribute__((always_inline)) {
+        const v8h x0 = codes8<FMT>((uint32_t)kr[0], (uint32_t)kr[1]), x1 = codes8<FMT>((uint32_t)kr[2], (uint32_t)kr[3]);
+        *reinterpret_cast<v8h*>(&sK[buf][kput]) = x0;
+        *reinterpret_cast<v8h*>(&sK[buf][kput ^ 16]) = x1;
+        uint32_t w[4][2];
 #pragma unroll
-        for (int i = 0; i < KU; ++i) {
-            const int row = krow + i * (NT / (DH / 16));
-            const int sw = DH == 128 ? row & 15 : (row >> 1) & 7;
-            const v8h x0 = codes8<FMT>((uint32_t)kr[i][0], (uint32_t)kr[i][1]), x1 = codes8<FMT>((uint32_t)kr[i][2], (uint32_t)kr[i][3]);
-            *reinterpret_cast<v8h*>(&sK[buf][row * KROW + ((2 * kch) ^ sw) * 16]) = x0;
-            *reinterpret_cast<v8h*>(&sK[buf][row * KROW + ((2 * kch + 1) ^ sw) * 16]) = x1;
+        for (int j = 0; j < 2; ++j) {
+            pair_of_keys<FMT, 0>(vr[2 * j], vr[2 * j + 1], w[0][j], w[1][j]);
+            pair_of_keys<FMT, 1>(vr[2 * j], vr[2 * j + 1], w[2][j], w[3][j]);
         }
 #pragma unroll
-        for (int u = 0; u < VQ; ++u) {
-            const int quad = vq + u * (NT / (DH / 4)), piece = (quad >> 2) * 2 + (quad & 1);
-            uint32_t w[4][2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                pair_of_keys<FMT, 0>(vr[u][2 * j], vr[u][2 * j + 1], w[0][j], w[1][j]);
-                pair_of_keys<FMT, 1>(vr[u][2 * j], vr[u][2 * j + 1], w[2][j], w[3][j]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = vch * 4 + i, rr = row >> 1;
-                *reinterpret_cast<v2i*>(&sV[buf][row * 128 + (piece ^ (rr & 7) ^ ((rr >> 3) & 1)) * 16 + ((quad >> 1) & 1) * 8]) = v2i{(int)w[i][0], (int)w[i][1]};
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int rr = (vch * 4 + i) >> 1;
+            *reinterpret_cast<v2i*>(&sV[buf][(vput ^ (((rr & 7) ^ ((rr >> 3) & 1)) * 16)) + i * 128]) = v2i{(int)w[i][0], (int)w[i][1]};
         }
     };
 
     // scores of 32 keys (s of tile t in buf)
+    const uint32_t kget = ql * KROW + (hh ^ (DH == 128 ? ql & 15 : (ql >> 1) & 7)) * 16;
+    const uint32_t vget = ql * 128 + (hh ^ ((ql >> 1) & 7) ^ (ql >> 4)) * 16;
     typedef v16f Scores[RTW];
     auto scores = [&](int buf, int s, Scores& acc) __attribute__((always_inline)) {
         const v16f zero = {};
-        const int row = s * 32 + ql, sw = DH == 128 ? row & 15 : (row >> 1) & 7;
+        const uint8_t* const from = &sK[buf][s * 32 * KROW];
 #pragma unroll
         for (int d = 0; d < DS; ++d) {
-            const v8h kf = *reinterpret_cast<const v8h*>(&sK[buf][row * KROW + ((2 * d + hh) ^ sw) * 16]);
+            const v8h kf = *reinterpret_cast<const v8h*>(from + (kget ^ (d * 32)));
 #pragma unroll
             for (int rt = 0; rt < RTW; ++rt) acc[rt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[rt][d], d ? acc[rt] : zero, 0, 0, 0);
         }
@@ -596,8 +636,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
-                const int row = c * 32 + ql, rr = row >> 1;
-                const v8h vf = *reinterpret_cast<const v8h*>(&sV[buf][row * 128 + (((s * 2 + st) * 2 + hh) ^ (rr & 7) ^ ((rr >> 3) & 1)) * 16]);
+                const v8h vf = *reinterpret_cast<const v8h*>(&sV[buf][(vget ^ ((s * 2 + st) * 32)) + c * 4096]);
 #pragma unroll
                 for (int rt = 0; rt < RTW; ++rt) {
                     const v8h pf = __builtin_bit_cast(v8h, v4i{(int)p[rt][4 * st], (int)p[rt][4 * st + 1], (int)p[rt][4 * st + 2], (int)p[rt][4 * st + 3]});
@@ -605,59 +644,66 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
                 }
             }
     };
-    // the scales of a tile's keys; a group without a block has no keys
-    auto groups = [&](int t, Group (&gr)[2][GH], bool& hole) __attribute__((always_inline)) {
-        hole = false;
+    // of the scales that have come: what the exponents are made of; a group without a block has no keys
+    auto groups = [&](const Ids& id, Group (&gr)[2][GH]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int g = 0; g < GH; ++g) {
-                const int key = t * 64 + s * 32 + g * (32 / GH);
-                const int blk = key < last ? a.c.block_of(b, key >> a.c.log2_block) : -1;
-                const int64_t at = (int64_t)max(blk, 0) * a.c.H + h;
-                const float vs = a.c.v.scale[at];
-                gr[s][g].ks = a.c.k.scale[at];
-                gr[s][g].lv = __builtin_amdgcn_logf(vs);
-                gr[s][g].iv = 1.0f / vs;
-                gr[s][g].lim = blk < 0 ? 0 : 0x7fffffff;
-                hole |= blk < 0;
-            }
+        for (int i = 0; i < NI; ++i) gr[i / GH][i % GH] = Group{sk[i], __builtin_amdgcn_logf(sv[i]), __builtin_amdgcn_rcpf(sv[i]), id[i] < 0 ? 0 : 0x7fffffff};
     };
 
     Scores acc, next;
+    Ids raw, id, id1, id2;                                               // blocks of tile t + 3 as they come, of t, t + 1, t + 2
+    const int te = t1 - 1;
     if (t0 < t1) {
-        fetch(t0);
+        look(t0, raw);
+        settle(raw, id);
+        fetch(t0, id);
+        scales(id);
+        look(min(t0 + 1, te), raw);
+        settle(raw, id1);
         blank();
         stage(t0 % NB);
-        fetch(min(t0 + 1, t1 - 1));
+        fetch(min(t0 + 1, te), id1);
+        look(min(t0 + 2, te), raw);
+        settle(raw, id2);
     }
     __syncthreads();
     if (t0 < wt) scores(t0 % NB, 0, acc);
     // (behind the last tile the last one is fetched and staged again, and scores are made that nobody takes: no branch in the middle)
     for (int t = t0; t < t1; ++t) {
         const int buf = t % NB, after = (t + 1) % NB;
+        look(min(t + 3, te), raw);
         blank();
         if (t < wt) {
             Group gr[2][GH];
-            bool hole;
-            groups(t, gr, hole);
-            const bool edge = t * 64 + 64 > wall || hole;
+            groups(id, gr);
+            bool edge = t * 64 + 64 > wall;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) edge |= id[i] < 0;
             raise(t, 0, acc, gr[0], edge);
+            __builtin_amdgcn_s_setprio(1);
             scores(buf, 1, next);
             take(buf, 0, acc, gr[0]);
             stage(after);
             interleave<DS, CT, RTW, true>();
+            __builtin_amdgcn_s_setprio(0);
             __syncthreads();
-            fetch(min(t + 2, t1 - 1));
+            fetch(min(t + 2, te), id2);
+            scales(id1);
             raise(t, 1, next, gr[1], edge);
+            __builtin_amdgcn_s_setprio(1);
             scores(after, 0, acc);
             take(buf, 1, next, gr[1]);
             interleave<DS, CT, RTW, false>();
+            __builtin_amdgcn_s_setprio(0);
         } else {
             stage(after);
             __syncthreads();
-            fetch(min(t + 2, t1 - 1));
+            fetch(min(t + 2, te), id2);
+            scales(id1);
         }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) { id[i] = id1[i]; id1[i] = id2[i]; }
+        settle(raw, id2);
     }
 
 #pragma unroll
@@ -688,29 +734,52 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// The pieces of the keys joined: DH / 4 threads per row, added in the order of the pieces.
+// The pieces of the keys joined: a workgroup per row; groups of DH / 4 threads take every eighth (sixteenth) piece, four at a time in
+// flight, and meet in LDS, in a fixed order.  (A group per row that took its pieces one after the other: 31 us for 32 pieces of 128 rows.)
 // ------------------------------------------------------------------------------------------
 template <int DH, int DT>
 __global__ __launch_bounds__(256) void kv_attn_join_kernel(AttnArgs a) {
-    constexpr int TPR = DH / 4;
-    const int nrows = a.Sq * a.group;
-    const int64_t r = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    const int e = (threadIdx.x % TPR) * 4;
-    if (r >= (int64_t)a.B * a.c.H * nrows) return;
+    constexpr int TPR = DH / 4, NG = 256 / TPR;
+    __shared__ __attribute__((aligned(16))) float so[NG][DH];
+    __shared__ float sl[NG];
+    const int nrows = a.Sq * a.group, tid = threadIdx.x, grp = tid / TPR, e = (tid % TPR) * 4, lane = tid & 63;
+    const int64_t r = blockIdx.x;
     const float* const ml = a.part_ml + r * a.splits * 2;
     const float* const p = a.part + r * a.splits * DH + e;
-    float M = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) M = fmaxf(M, ml[2 * s]);
+    // at most MOST_PIECES: two to a lane
+    const float m0 = lane < a.splits ? ml[2 * lane] : -INFINITY, m1 = lane + 64 < a.splits ? ml[2 * lane + 128] : -INFINITY;
+    const float M = wave_max(fmaxf(m0, m1));
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
     float L = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float l = ml[2 * s + 1];
-        if (l == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - M);
-        const v4f x = *reinterpret_cast<const v4f*>(p + (int64_t)s * DH);
-        L = fmaf(l, f, L);
+    for (int s0 = grp; s0 < a.splits; s0 += 4 * NG) {
+        v4f x[4];
+        float m[4], l[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sum[t] = fmaf(x[t], f, sum[t]);
+        for (int i = 0; i < 4; ++i) {
+            const int s = min(s0 + i * NG, a.splits - 1);
+            x[i] = *reinterpret_cast<const v4f*>(p + (int64_t)s * DH);
+            m[i] = ml[2 * s];
+            l[i] = s0 + i * NG < a.splits ? ml[2 * s + 1] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (l[i] == 0.0f) continue;                                   // (no key in it; its maximum is -inf)
+            const float f = __builtin_amdgcn_exp2f(m[i] - M);
+            L = fmaf(l[i], f, L);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = fmaf(x[i][t], f, sum[t]);
+        }
+    }
+    *reinterpret_cast<v4f*>(&so[grp][e]) = sum;
+    if (e == 0) sl[grp] = L;
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int i = 1; i < NG; ++i) {
+        const v4f x = *reinterpret_cast<const v4f*>(&so[i][e]);
+        L += sl[i];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sum[t] += x[t];
     }
     const float inv = M == INFINITY ? __builtin_nanf("") : (L == 0.0f ? 0.0f : 1.0f / L);
     const int row = (int)(r % nrows), bh = (int)(r / nrows), h = bh % a.c.H, b = bh / a.c.H, s = row / a.group;
@@ -734,10 +803,11 @@ Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq) {
     const int64_t tile = p.rtw ? 256 : 16 * p.rt;
     p.tiles = (int)((rows + tile - 1) / tile);
     const int64_t units = bh * p.tiles;
-    // pieces of 16 steps or more while there are fewer than four workgroups per CU (one, of many rows)
-    int64_t s = ((p.rtw ? 256 : 1024) + units - 1) / units;
+    // Pieces of 16 steps or more while there are fewer than two workgroups per CU (one, of many rows).  us, towards 256 / 512 / 1024 workgroups:
+    // 4 x 8 heads x 4 rows over 131072 keys 192 / 179 / 184, 16 x 8 heads x 20 rows over 4096 keys (its write with it) 49 / 41 / 46.
+    int64_t s = ((p.rtw ? 256 : 512) + units - 1) / units;
     s = s < steps / 16 ? s : steps / 16;
-    p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    p.splits = (int)(s < 1 ? 1 : s > MOST_PIECES ? MOST_PIECES : s);
     return p;
 }
 
@@ -768,7 +838,7 @@ hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
     hero_status r = hero_launch_status();
     if (r != HERO_OK || a.splits == 1) return r;
     const int64_t rows = (int64_t)a.B * a.c.H * a.Sq * a.group;
-    hipLaunchKernelGGL((kv_attn_join_kernel<DH, DT>), dim3((unsigned)((rows * (DH / 4) + 255) / 256)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((kv_attn_join_kernel<DH, DT>), dim3((unsigned)rows), dim3(256), 0, st, a);
     return hero_launch_status();
 }
 
@@ -804,7 +874,7 @@ extern "C" hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, c
     Plan p = plan(cache, Hq, Sq);
     if (!workspace || workspace_bytes < part_bytes(cache, Hq, Sq, p.splits)) p.splits = 1;
     const int64_t nb = (cache->B * cache->H + 7) / 8 * 8 * p.tiles * p.splits;
-    if (nb > 0x7fffffffLL || cache->B * Sq * Hq * (Dh / 4) / 256 > 0x7ffffffeLL) return HERO_ERR_SHAPE;
+    if (nb > 0x7fffffffLL || cache->B * Sq * Hq > 0x7fffffffLL) return HERO_ERR_SHAPE;
     AttnArgs a;
     a.c = kv_view(cache);
     a.q = (const uint16_t*)q;
