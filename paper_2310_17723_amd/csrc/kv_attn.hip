@@ -409,9 +409,10 @@ __device__ __forceinline__ void interleave() {
 #undef HERO_ORDER
 }
 
-template <int DH, int FMT, int DT, int NW, int RTW, int GH>          // GH: groups of keys with scales of their own in 32 keys
+template <int DH, int FMT, int DT, int NW, int RTW, int NI>          // NI: blocks that a tile's 64 keys lie in
 __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
-    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, GE = 16 / GH, NT = 64 * NW, ROWS = 32 * RTW * NW, NI = 2 * GH;
+    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, NT = 64 * NW, ROWS = 32 * RTW * NW;
+    constexpr int GH = NI == 4 ? 2 : 1, GE = 16 / GH;        // groups of keys with scales of their own in 32 keys
     static_assert(NT == 512, "one unit of K and of V per thread");
     __shared__ __attribute__((aligned(1024))) uint8_t sK[NB][64 * KROW], sV[NB][DH * 128];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, ql = lane & 31;
@@ -477,13 +478,16 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     uint32_t nought;
     asm("v_mov_b32 %0, 0" : "=v"(nought));
     const uint32_t koff = (uint32_t)(krow & 15) * (uint32_t)a.c.k.s_row + (uint32_t)kch * 16;
-    const uint32_t voff = (uint32_t)(vq & 3) * 4 * (uint32_t)a.c.v.s_row + (uint32_t)vch * 4;
+    uint32_t voff[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) voff[j] = (uint32_t)((vq & 3) * 4 + j) * (uint32_t)a.c.v.s_row + (uint32_t)vch * 4;
     typedef int Ids[NI];
+    const int32_t* const table = a.c.table + (int64_t)b * a.c.max_blocks;
     auto look = [&](int t, Ids& raw) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int64_t at = (int64_t)b * a.c.max_blocks + min((t * 64 + i * (64 / NI)) >> a.c.log2_block, a.c.max_blocks - 1);
-            raw[i] = a.c.table ? (a.c.table + at)[nought] : (int)at;
+            const int at = min((t * 64 + i * (64 / NI)) >> a.c.log2_block, a.c.max_blocks - 1);
+            raw[i] = a.c.table ? (table + at)[nought] : b * a.c.max_blocks + at;
         }
     };
     auto settle = [&](const Ids& raw, Ids& id) __attribute__((always_inline)) {
@@ -493,26 +497,30 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
             id[i] = (unsigned)blk < (unsigned)a.c.n_blocks ? blk : -1;
         }
     };
+    const uint8_t* const khead = a.c.k.codes + (int64_t)h * a.c.k.s_head;
+    const uint8_t* const vhead = a.c.v.codes + (int64_t)h * a.c.v.s_head;
+    const int vrow = (int)a.c.v.s_row, krow_ = (int)a.c.k.s_row;         // (a block's rows span less than 2^31 elements)
     auto fetch = [&](int t, const Ids& id) __attribute__((always_inline)) {
         int blk = 0;                             // id[group16 NI / 4], by masks: an index that is not known would put the array into memory
 #pragma unroll
         for (int i = 0; i < NI; ++i) blk |= id[i] & -(int)(group16 * NI / 4 == i);
         const int first = t * 64 + group16 * 16, at = first & ((1 << a.c.log2_block) - 1);
-        const int64_t bl = max(blk, 0);
-        const uint8_t* const kp = a.c.k.codes + bl * a.c.k.s_block + (int64_t)at * a.c.k.s_row + (int64_t)h * a.c.k.s_head;
-        const uint8_t* const vp = a.c.v.codes + bl * a.c.v.s_block + (int64_t)at * a.c.v.s_row + (int64_t)h * a.c.v.s_head;
+        const uint8_t* const kp = khead + (int64_t)max(blk, 0) * a.c.k.s_block + (uint32_t)(at * krow_);
+        const uint8_t* const vp = vhead + (int64_t)max(blk, 0) * a.c.v.s_block + (uint32_t)(at * vrow);
         kr = *reinterpret_cast<const v4i*>(kp + koff);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) vr[j] = *reinterpret_cast<const uint32_t*>(vp + (int64_t)j * a.c.v.s_row + voff);
+        for (int j = 0; j < 4; ++j) vr[j] = *reinterpret_cast<const uint32_t*>(vp + voff[j]);
         vend = blk < 0 ? 0 : len - first - (vq & 3) * 4;
     };
     float sk[NI], sv[NI];
+    const float* const kscale = a.c.k.scale + h;
+    const float* const vscale = a.c.v.scale + h;
     auto scales = [&](const Ids& id) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int64_t at = (int64_t)max(id[i], 0) * a.c.H + h;
-            sk[i] = (a.c.k.scale + at)[nought];
-            sv[i] = (a.c.v.scale + at)[nought];
+            const int64_t at = (int64_t)max(id[i], 0) * a.c.H;
+            sk[i] = (kscale + at)[nought];
+            sv[i] = (vscale + at)[nought];
         }
     };
     // what lies behind the last key, or where no block is, is no code
@@ -647,7 +655,17 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     // of the scales that have come: what the exponents are made of; a group without a block has no keys
     auto groups = [&](const Ids& id, Group (&gr)[2][GH]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) gr[i / GH][i % GH] = Group{sk[i], __builtin_amdgcn_logf(sv[i]), __builtin_amdgcn_rcpf(sv[i]), id[i] < 0 ? 0 : 0x7fffffff};
+        for (int i = 0; i < NI; ++i) {
+            const Group x = {sk[i], __builtin_amdgcn_logf(sv[i]), __builtin_amdgcn_rcpf(sv[i]), id[i] < 0 ? 0 : 0x7fffffff};
+            if constexpr (NI == 1) gr[0][0] = gr[1][0] = x;
+            else gr[i / GH][i % GH] = x;
+        }
+    };
+    // what was written to LDS is there for the other waves, and global loads stay in flight
+    auto meet = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     };
 
     Scores acc, next;
@@ -655,55 +673,59 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     const int te = t1 - 1;
     if (t0 < t1) {
         look(t0, raw);
-        settle(raw, id);
-        fetch(t0, id);
-        scales(id);
-        look(min(t0 + 1, te), raw);
         settle(raw, id1);
+        fetch(t0, id1);
+        scales(id1);
+        look(min(t0 + 1, te), raw);
+        settle(raw, id2);
         blank();
         stage(t0 % NB);
-        fetch(min(t0 + 1, te), id1);
+        fetch(min(t0 + 1, te), id2);
         look(min(t0 + 2, te), raw);
-        settle(raw, id2);
     }
     __syncthreads();
     if (t0 < wt) scores(t0 % NB, 0, acc);
-    // (behind the last tile the last one is fetched and staged again, and scores are made that nobody takes: no branch in the middle)
-    for (int t = t0; t < t1; ++t) {
-        const int buf = t % NB, after = (t + 1) % NB;
-        look(min(t + 3, te), raw);
-        blank();
-        if (t < wt) {
-            Group gr[2][GH];
-            groups(id, gr);
-            bool edge = t * 64 + 64 > wall;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) edge |= id[i] < 0;
-            raise(t, 0, acc, gr[0], edge);
-            __builtin_amdgcn_s_setprio(1);
-            scores(buf, 1, next);
-            take(buf, 0, acc, gr[0]);
-            stage(after);
-            interleave<DS, CT, RTW, true>();
-            __builtin_amdgcn_s_setprio(0);
-            __syncthreads();
-            fetch(min(t + 2, te), id2);
-            scales(id1);
-            raise(t, 1, next, gr[1], edge);
-            __builtin_amdgcn_s_setprio(1);
-            scores(after, 0, acc);
-            take(buf, 1, next, gr[1]);
-            interleave<DS, CT, RTW, false>();
-            __builtin_amdgcn_s_setprio(0);
-        } else {
-            stage(after);
-            __syncthreads();
-            fetch(min(t + 2, te), id2);
-            scales(id1);
-        }
+    auto next_ids = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) { id[i] = id1[i]; id1[i] = id2[i]; }
         settle(raw, id2);
+        look(min(t + 3, te), raw);
+    };
+    // (behind the last tile the last one is fetched and staged again, and scores are made that nobody takes: no branch in the middle)
+    int t = t0;
+    for (; t < wt; ++t) {
+        const int buf = t % NB, after = (t + 1) % NB;
+        Group gr[2][GH];
+        next_ids(t);
+        groups(id, gr);
+        bool edge = t * 64 + 64 > wall;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) edge |= id[i] < 0;
+        blank();
+        raise(t, 0, acc, gr[0], edge);
+        __builtin_amdgcn_s_setprio(1);
+        scores(buf, 1, next);
+        take(buf, 0, acc, gr[0]);
+        stage(after);
+        fetch(min(t + 2, te), id2);
+        scales(id1);
+        interleave<DS, CT, RTW, true>();
+        __builtin_amdgcn_s_setprio(0);
+        meet();
+        raise(t, 1, next, gr[1], edge);
+        __builtin_amdgcn_s_setprio(1);
+        scores(after, 0, acc);
+        take(buf, 1, next, gr[1]);
+        interleave<DS, CT, RTW, false>();
+        __builtin_amdgcn_s_setprio(0);
+    }
+    for (; t < t1; ++t) {                                                // tiles that other waves' rows see
+        next_ids(t);
+        blank();
+        stage((t + 1) % NB);
+        fetch(min(t + 2, te), id2);
+        scales(id1);
+        meet();
     }
 
 #pragma unroll
@@ -792,20 +814,19 @@ __global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, i
     if (i < rows * cols) out[(i / cols) * ld + i % cols] = 0;
 }
 
-// How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 128 rtw of that of many; the keys into pieces.
-struct Plan { int rt, rtw, tiles, splits; };
+// How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 256 to one of that of many (rt = 0); the keys into pieces.
+struct Plan { int rt, tiles, splits; };
 
 Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq) {
     Plan p;
-    const int64_t rows = Sq * (Hq / c->H), bh = c->B * c->H, steps = (c->max_blocks * c->block + 31) / 32;
-    p.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.rtw = rows > 128 ? 1 : 0;
-    const int64_t tile = p.rtw ? 256 : 16 * p.rt;
+    const int64_t rows = Sq * (Hq / c->H), bh = c->B * c->H, keys = c->max_blocks * c->block, steps = (keys + 31) / 32;
+    p.rt = rows <= 16 ? 1 : rows > 64 && (double)rows * bh * keys * c->Dh >= 1.5e9 ? 0 : 2;
+    const int64_t tile = p.rt ? 16 * p.rt : 256;
     p.tiles = (int)((rows + tile - 1) / tile);
     const int64_t units = bh * p.tiles;
     // Pieces of 16 steps or more while there are fewer than two workgroups per CU (one, of many rows).  us, towards 256 / 512 / 1024 workgroups:
     // 4 x 8 heads x 4 rows over 131072 keys 192 / 179 / 184, 16 x 8 heads x 20 rows over 4096 keys (its write with it) 49 / 41 / 46.
-    int64_t s = ((p.rtw ? 256 : 512) + units - 1) / units;
+    int64_t s = ((p.rt ? 512 : 256) + units - 1) / units;
     s = s < steps / 16 ? s : steps / 16;
     p.splits = (int)(s < 1 ? 1 : s > MOST_PIECES ? MOST_PIECES : s);
     return p;
@@ -825,15 +846,15 @@ size_t part_bytes(const hero_kv_cache* c, int64_t Hq, int64_t Sq, int splits) {
 template <int DH, int FMT, int DT>
 hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
     const dim3 block(256);
-    if (p.rtw) {
+    if (p.rt == 0) {
         const dim3 grid((unsigned)(((int64_t)a.B * a.c.H + 7) / 8 * 8 * a.tiles * a.splits));
-        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 2>), grid, dim3(512), 0, st, a);
+        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 4>), grid, dim3(512), 0, st, a);
+        else if (a.c.log2_block == 5) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 2>), grid, dim3(512), 0, st, a);
         else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 1>), grid, dim3(512), 0, st, a);
     } else {
         const dim3 grid((unsigned)((int64_t)a.B * a.c.H * a.tiles * a.splits));
         if (p.rt == 1) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 1, 4>), grid, block, 0, st, a);
-        else if (p.rt == 2) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 2, 4>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 4, 4>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 2, 4>), grid, block, 0, st, a);
     }
     hero_status r = hero_launch_status();
     if (r != HERO_OK || a.splits == 1) return r;
