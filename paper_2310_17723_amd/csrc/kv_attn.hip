@@ -384,7 +384,8 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 // worked on.  Scores are computed transposed (S^T = K Q^T): a lane owns query lane % 32 of each of its RTW row tiles, and the exponentials are
 // the second product's operand as they stand.  The scores of 32 keys are made while the exponentials of the 32 before them are taken.
 // The maximum is raised, and the sums so far rescaled, only when a score exceeds it by SLACK (P stays within FP16's 2^15).
-// LDS holds 16-byte pieces XOR-swizzled by their row: fragment reads (turns of lanes 0-3, 12-15, 20-27 and so on) meet no bank conflict.
+// K's rows are 16 bytes longer than they need to be, V's 16-byte pieces XOR-swizzled by their row: fragment reads (turns of lanes 0-3, 12-15,
+// 20-27 and so on) meet no bank conflict.
 // ------------------------------------------------------------------------------------------
 constexpr float SLACK = 7.0f;
 
@@ -411,7 +412,7 @@ __device__ __forceinline__ void interleave() {
 
 template <int DH, int FMT, int DT, int NW, int RTW, int NI>          // NI: blocks that a tile's 64 keys lie in
 __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
-    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2, NB = 3, NT = 64 * NW, ROWS = 32 * RTW * NW;
+    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2 + 16, NB = 3, NT = 64 * NW, ROWS = 32 * RTW * NW;
     constexpr int GH = NI == 4 ? 2 : 1, GE = 16 / GH;        // groups of keys with scales of their own in 32 keys
     static_assert(NT == 512, "one unit of K and of V per thread");
     __shared__ __attribute__((aligned(1024))) uint8_t sK[NB][64 * KROW], sV[NB][DH * 128];
@@ -446,15 +447,6 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
 
     v8h qf[RTW][DS];
     float rc[RTW];
-#pragma unroll
-    for (int rt = 0; rt < RTW; ++rt) {
-        const int row = min(wrow + rt * 32 + ql, nrows - 1), s = row / a.group;
-        const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + row - s * a.group) * a.qs[2] + hh * 8;
-        v4i raw[DS];
-#pragma unroll
-        for (int t = 0; t < DS; ++t) raw[t] = *reinterpret_cast<const v4i*>(qp + t * 16);
-        rc[rt] = queries<DT, DS, 32>(raw, a.scale, qf[rt]);
-    }
     v16f o[RTW][CT];
     float m[RTW], l[RTW];
 #pragma unroll
@@ -530,13 +522,12 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
             for (int j = 0; j < 4; ++j) vr[j] = j < vend ? vr[j] : 0u;
     };
     // a half of 16 keys: its lanes hold keys 0-3, 8-11 / 4-7, 12-15 of them
-    const int ksw = DH == 128 ? krow & 15 : (krow >> 1) & 7;
-    const uint32_t kput = krow * KROW + ((2 * kch) ^ ksw) * 16;
+    const uint32_t kput = krow * KROW + kch * 32;
     const uint32_t vput = vch * 512 + ((vq >> 2) * 2 + (vq & 1)) * 16 + ((vq >> 1) & 1) * 8;
     auto stage = [&](int buf) __attribute__((always_inline)) {
         const v8h x0 = codes8<FMT>((uint32_t)kr[0], (uint32_t)kr[1]), x1 = codes8<FMT>((uint32_t)kr[2], (uint32_t)kr[3]);
         *reinterpret_cast<v8h*>(&sK[buf][kput]) = x0;
-        *reinterpret_cast<v8h*>(&sK[buf][kput ^ 16]) = x1;
+        *reinterpret_cast<v8h*>(&sK[buf][kput + 16]) = x1;
         uint32_t w[4][2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -551,7 +542,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     };
 
     // scores of 32 keys (s of tile t in buf)
-    const uint32_t kget = ql * KROW + (hh ^ (DH == 128 ? ql & 15 : (ql >> 1) & 7)) * 16;
+    const uint32_t kget = ql * KROW + hh * 16;
     const uint32_t vget = ql * 128 + (hh ^ ((ql >> 1) & 7) ^ (ql >> 4)) * 16;
     typedef v16f Scores[RTW];
     auto scores = [&](int buf, int s, Scores& acc) __attribute__((always_inline)) {
@@ -559,7 +550,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
         const uint8_t* const from = &sK[buf][s * 32 * KROW];
 #pragma unroll
         for (int d = 0; d < DS; ++d) {
-            const v8h kf = *reinterpret_cast<const v8h*>(from + (kget ^ (d * 32)));
+            const v8h kf = *reinterpret_cast<const v8h*>(from + kget + d * 32);
 #pragma unroll
             for (int rt = 0; rt < RTW; ++rt) acc[rt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[rt][d], d ? acc[rt] : zero, 0, 0, 0);
         }
@@ -669,6 +660,14 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     };
 
     Scores acc, next;
+    v4i qraw[RTW][DS];
+#pragma unroll
+    for (int rt = 0; rt < RTW; ++rt) {
+        const int row = min(wrow + rt * 32 + ql, nrows - 1), s = row / a.group;
+        const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + row - s * a.group) * a.qs[2] + hh * 8;
+#pragma unroll
+        for (int t = 0; t < DS; ++t) qraw[rt][t] = *reinterpret_cast<const v4i*>(qp + t * 16);
+    }
     Ids raw, id, id1, id2;                                               // blocks of tile t + 3 as they come, of t, t + 1, t + 2
     const int te = t1 - 1;
     if (t0 < t1) {
@@ -677,6 +676,10 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
         fetch(t0, id1);
         scales(id1);
         look(min(t0 + 1, te), raw);
+    }
+#pragma unroll
+    for (int rt = 0; rt < RTW; ++rt) rc[rt] = queries<DT, DS, 32>(qraw[rt], a.scale, qf[rt]);
+    if (t0 < t1) {
         settle(raw, id2);
         blank();
         stage(t0 % NB);
