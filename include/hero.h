@@ -462,7 +462,8 @@ hero_status hero_kv_write(const hero_kv_cache* cache, const void* k, const int64
  * HERO_F32).  Positions outside [0, min(kv_len[b], max_blocks block)) are left as they were in the output.
  *   k_out, v_out  [B, S, H, Dh], base pointers and 4 element strides (batch, token, head, channel); channel stride 1, the others
  *                 multiples of 8.  Either may be NULL (only the other is read).
- *   start  int32 [B] (device) or NULL (0 for every sequence); kv_len int32 [B] (device), required. */
+ *   start  int32 [B] (device) or NULL (0 for every sequence); kv_len int32 [B] (device), required.
+ * S * H <= 2^31 - 256. */
 hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, const int64_t k_strides[4],
                          void* v_out, const int64_t v_strides[4], hero_dtype out_dt, int64_t S,
                          const int32_t* start, const int32_t* kv_len, void* stream);
