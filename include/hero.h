@@ -489,6 +489,20 @@ hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, const int64_
                          int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,
                          void* out, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
 
+/* hero_layer_fwd with a block-scaled cache: a layer whose attention module is 16-bit (HERO_M_ATTN clear; else HERO_ERR_UNSUPPORTED)
+ * writes this call's K and V into `kv` and attends over it (hero_kv_write, hero_kv_attn with qk_scale and the layer's mask; HERO_MASK_PADDING
+ * asks for the same as HERO_MASK_NONE here), so that it prefills and decodes.  Everything else as for hero_layer_fwd.
+ *   kv       the layer's cache, for io->B sequences of desc->H heads of width desc->Dh (else HERO_ERR_SHAPE); io->k_cache and
+ *            io->v_cache are NULL.  io->kv_len [B], required, counts this call's tokens.
+ *   new_len  int32 [B] (device) or NULL: of the S rows of sequence b the first new_len[b] are tokens (a padded batch; the
+ *            other rows are computed without a key to attend to).
+ *   workspace: hero_layer_kv_workspace_bytes(desc, kv, S) bytes; what hero_layer_fwd accepts without is accepted without here,
+ *            and the attention of few rows is then not split. */
+size_t hero_layer_kv_workspace_bytes(const hero_layer_desc* desc, const hero_kv_cache* kv, int64_t S);
+hero_status hero_layer_fwd_kv(const hero_layer_desc* desc, const hero_layer_weights* w, const hero_layer_io* io,
+                              const hero_kv_cache* kv, const int32_t* new_len,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
 /* Model-load-time operators (not on the hot path): the pre-processing phase of the method on the GPU.
  *
  * hero_absmax_cols -- calibration statistic of the static scales (Sec. 2.1: FWQ / SQ scales are

@@ -88,6 +88,8 @@ SYMBOLS = {
     "hero_kv_attn": (i32, [C.POINTER(KvCache), vp, vp, i32, i64, i64, f32, i32, vp, vp, vp, i64, vp, C.c_size_t, vp]),
     "hero_layer_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDesc), i64, i64]),
     "hero_layer_fwd": (i32, [C.POINTER(LayerDesc), C.POINTER(LayerWeights), C.POINTER(LayerIO), vp, C.c_size_t, vp]),
+    "hero_layer_kv_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDesc), C.POINTER(KvCache), i64]),
+    "hero_layer_fwd_kv": (i32, [C.POINTER(LayerDesc), C.POINTER(LayerWeights), vp, C.POINTER(KvCache), vp, vp, C.c_size_t, vp]),
     "hero_bf16_gemm": (i32, [vp, i64, vp, i64, vp, vp, i64, i32, vp, i64, i64, i64, i64, vp]),
     "hero_bf16_attn": (i32, [vp, C.POINTER(i64), vp, C.POINTER(i64), vp, C.POINTER(i64), i64, i64, i64, i64, i64,
                              f32, i32, vp, vp, i64, vp]),
@@ -129,6 +131,7 @@ _PACK4 = struct.Struct("@4q").pack
 def _kv_rows(cache, t, S, heads):
     """The strides of [B, S, heads, Dh] rows."""
     assert t.shape == (cache.sizes[0], S, heads, cache.sizes[2]), "rows of a KV cache are [B, S, heads, Dh]"
+    assert t.get_device() == cache.device, "rows lie on the cache's device"
     return _PACK4(*t.stride())
 
 
@@ -136,7 +139,14 @@ def _kv_length(cache, t):
     if t is None:
         return None
     assert t.dtype is torch.int32 and t.shape == cache.sizes[:1] and t.is_contiguous(), "lengths are contiguous int32 [B]"
+    assert t.get_device() == cache.device, "lengths lie on the cache's device"
     return t.data_ptr()
+
+
+def _kv_stream(cache, stream):
+    if stream is None and cache.device != torch.cuda.current_device():
+        raise ValueError(f"the cache lies on device {cache.device}, which is not the current one")
+    return _stream(stream)
 
 
 class Hero:
@@ -390,12 +400,14 @@ class Hero:
             raise ValueError("a cache without a block table needs batch and max_blocks")
         if v.shape != k.shape or v.dtype != k.dtype or k.dtype not in (torch.int8, torch.float8_e4m3fn):
             raise ValueError("k and v are int8 or float8_e4m3fn tensors of one shape [n_blocks, block, H, Dh]")
+        if any(s.device != k.device for s in (v, k_scale, v_scale)) or (block_table is not None and block_table.device != k.device):
+            raise ValueError("the parts of a cache lie on one device")
         for s in (k_scale, v_scale):
             if s.dtype != torch.float32 or tuple(s.shape) != (n, H) or not s.is_contiguous():
                 raise ValueError("scales are contiguous float32 tensors [n_blocks, H]")
         c = KvCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _strides4(k), _strides4(v), _ptr(block_table),
                     int(batch), int(max_blocks), n, H, Dh, block, _DT[k.dtype])
-        c.tensors, c.sizes = (k, v, k_scale, v_scale, block_table), (int(batch), H, Dh)
+        c.tensors, c.sizes, c.device = (k, v, k_scale, v_scale, block_table), (int(batch), H, Dh), k.get_device()
         return c
 
     def hero_kv_write(self, cache, k, v, kv_len, new_len=None, stream=None):
@@ -403,7 +415,7 @@ class Hero:
         S, H = k.shape[1], cache.sizes[1]
         assert k.dtype is v.dtype
         self._check(self.lib.hero_kv_write(cache, k.data_ptr(), _kv_rows(cache, k, S, H), v.data_ptr(), _kv_rows(cache, v, S, H), _DT[k.dtype], S,
-                                           _kv_length(cache, kv_len), _kv_length(cache, new_len), _stream(stream)))
+                                           _kv_length(cache, kv_len), _kv_length(cache, new_len), _kv_stream(cache, stream)))
 
     def hero_kv_read(self, cache, S, kv_len, start=None, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
         """Positions start[b] .. start[b] + S - 1 as [B,S,H,Dh] rows of `dtype`, K and V.  Positions that the sequence does not hold
@@ -415,7 +427,7 @@ class Hero:
             v_out = torch.zeros((B, S, H, Dh), dtype=k_out.dtype, device=kv_len.device)
         assert k_out.dtype is v_out.dtype
         self._check(self.lib.hero_kv_read(cache, k_out.data_ptr(), _kv_rows(cache, k_out, S, H), v_out.data_ptr(), _kv_rows(cache, v_out, S, H),
-                                          _DT[k_out.dtype], S, _kv_length(cache, start), _kv_length(cache, kv_len), _stream(stream)))
+                                          _DT[k_out.dtype], S, _kv_length(cache, start), _kv_length(cache, kv_len), _kv_stream(cache, stream)))
         return k_out, v_out
 
     def hero_kv_attn_workspace_bytes(self, cache, Hq, Sq) -> int:
@@ -432,7 +444,7 @@ class Hero:
         self._check(self.lib.hero_kv_attn(cache, q.data_ptr(), _kv_rows(cache, q, Sq, Hq), _DT[q.dtype], Hq, Sq, scale, int(mask),
                                           _kv_length(cache, kv_len), _kv_length(cache, new_len), out.data_ptr(), out.stride(0),
                                           None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
-                                          _stream(stream)))
+                                          _kv_stream(cache, stream)))
         return out
 
     # ------------------------------------------------------------------ layer
@@ -462,3 +474,15 @@ class Hero:
                             ptr(next_read), 0 if next_read is None else next_read.nbytes)
         st = self._layer_fwd(C.byref(desc), C.byref(weights), io, workspace.data_ptr(), workspace.nbytes, _stream(stream))
         self._check(st)
+
+    def hero_layer_kv_workspace_bytes(self, desc: LayerDesc, cache: KvCache, S: int) -> int:
+        return int(self.lib.hero_layer_kv_workspace_bytes(C.byref(desc), cache, S))
+
+    def hero_layer_fwd_kv(self, desc, weights, cache, S, workspace, *, kv_len, new_len=None, x_q=None, x_scale=None, out_q=None, out_scale=None,
+                          h=None, x_hp=None, out_hp=None, next_read=None, stream=None):
+        """hero_layer_fwd of a layer with 16-bit attention over a block-scaled cache (kv_cache)."""
+        ptr = lambda t: 0 if t is None else t.data_ptr()
+        io = _LAYER_IO.pack(cache.sizes[0], S, ptr(x_q), ptr(x_scale), ptr(out_q), ptr(out_scale), ptr(h), _kv_length(cache, kv_len) or 0, 0, 0, 0,
+                            ptr(x_hp), ptr(out_hp), ptr(next_read), 0 if next_read is None else next_read.nbytes)
+        self._check(self.lib.hero_layer_fwd_kv(C.byref(desc), C.byref(weights), io, cache, _kv_length(cache, new_len), workspace.data_ptr(),
+                                               workspace.nbytes, _kv_stream(cache, stream)))

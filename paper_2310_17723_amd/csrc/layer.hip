@@ -7,10 +7,11 @@
 //                  -> FC1 + GELU^quant -> FC2 -> LN^quant(X_mid, X_2) -> X_out,int8 S_out
 // PRE_LN (GPT):    h (16-bit) -> LN^quant -> QKV -> attention -> W_o (+h) -> LN^quant
 //                  -> FC1 + GELU^quant -> FC2 (+h); h is updated in place.
+// hero_layer_fwd_kv: the same with a 16-bit attention over a block-scaled 8-bit KV cache (hero_kv_write, hero_kv_attn).
 // Every module is INT8 or 16-bit (bf16, or fp16 with HERO_M_F16) as its mode bit says; a tensor between two
 // modules is INT8 codes when its consumer is INT8 and 16-bit values otherwise (LN^quant writes its 16-bit copy
 // beside the codes when the next linear is 16-bit).
-#include "hero_common.h"
+#include "kv_cache.h"
 #include <algorithm>
 
 namespace {
@@ -118,12 +119,25 @@ extern "C" size_t hero_layer_workspace_bytes(const hero_layer_desc* desc, int64_
     return plan(desc, B * S).total;
 }
 
-extern "C" hero_status hero_layer_fwd(const hero_layer_desc* desc, const hero_layer_weights* w, const hero_layer_io* io,
-                                      void* workspace, size_t workspace_bytes, void* stream) {
+// the scratch of the attention over a block-scaled cache is that of the GEMMs' K split (stream order)
+extern "C" size_t hero_layer_kv_workspace_bytes(const hero_layer_desc* desc, const hero_kv_cache* kv, int64_t S) {
+    if (!desc || S < 0 || check(desc) != HERO_OK || kv_check(kv) != HERO_OK) return 0;
+    const Workspace ws = plan(desc, kv->B * S);
+    return std::max(ws.total, ws.gemm_ws + align256(hero_kv_attn_workspace_bytes(kv, desc->H, S)));
+}
+
+// kv (with new_len): the block-scaled cache of a 16-bit attention; NULL: hero_layer_fwd
+static hero_status layer_run(const hero_layer_desc* desc, const hero_layer_weights* w, const hero_layer_io* io,
+                             const hero_kv_cache* kv, const int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream) {
     if (!desc || !w || !io) return HERO_ERR_NULL;
     HERO_TRY(check(desc));
     const int64_t B = io->B, S = io->S, T = B * S;
     if (B < 0 || S < 0) return HERO_ERR_SHAPE;
+    if (kv) {
+        HERO_TRY(kv_check(kv));
+        if ((desc->mode_mask & HERO_M_ATTN) || io->k_cache || io->v_cache) return HERO_ERR_UNSUPPORTED;   // (an INT8 attention reads SQ codes)
+        if (kv->B != B || kv->H != desc->H || kv->Dh != desc->Dh || (!new_len && kv->max_blocks * kv->block < S)) return HERO_ERR_SHAPE;
+    }
     if (T == 0) return HERO_OK;
     const Workspace ws = plan(desc, T);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < ws.required) return HERO_ERR_WORKSPACE;
@@ -148,7 +162,8 @@ extern "C" hero_status hero_layer_fwd(const hero_layer_desc* desc, const hero_la
         if (!attn_i8) return HERO_ERR_UNSUPPORTED;            // the cache holds INT8 (SQ) codes
         if (io->Smax < S) return HERO_ERR_SHAPE;
     }
-    if (desc->mask == HERO_MASK_PADDING && !io->kv_len) return HERO_ERR_NULL;
+    if ((desc->mask == HERO_MASK_PADDING || kv) && !io->kv_len) return HERO_ERR_NULL;
+    if (kv && (((uintptr_t)io->kv_len & 3) || ((uintptr_t)new_len & 3))) return HERO_ERR_ALIGN;
     if (Dh != 64 && Dh != 128) return HERO_ERR_UNSUPPORTED;
     if (d % 64 || f % 64) return HERO_ERR_UNSUPPORTED;
     // what the chained entry points would refuse only after earlier stages had been enqueued (and, pre-LN, after
@@ -281,6 +296,11 @@ extern "C" hero_status hero_layer_fwd(const hero_layer_desc* desc, const hero_la
         HERO_TRY(attend8(false));
     } else {
         const uint16_t* qp = (const uint16_t*)qkv;
+        if (kv) {
+            HERO_TRY(hero_kv_write(kv, qp + d, qs, qp + 2 * d, qs, HP, S, io->kv_len, new_len, stream));
+            HERO_TRY(hero_kv_attn(kv, qp, qs, HP, H, S, w->qk_scale, desc->mask == HERO_MASK_CAUSAL ? HERO_MASK_CAUSAL : HERO_MASK_NONE,
+                                  io->kv_len, new_len, attn, d, gws, gws_bytes, stream));
+        } else
         HERO_TRY(hero_hp_attn(qp, qs, qp + d, qs, qp + 2 * d, qs, B, H, S, S, Dh, w->qk_scale,
                               (hero_mask)desc->mask, io->kv_len, attn, d, HP, stream));
     }
@@ -342,4 +362,16 @@ extern "C" hero_status hero_layer_fwd(const hero_layer_desc* desc, const hero_la
             HERO_TRY(hero_hp_gemm_ws(act, f, w->w_2_bf16, f, w->b_2, io->h, d, 0, io->h, d, T, d, f, HP, gws, gws_bytes, stream));
     }
     return HERO_OK;
+}
+
+extern "C" hero_status hero_layer_fwd(const hero_layer_desc* desc, const hero_layer_weights* w, const hero_layer_io* io,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+    return layer_run(desc, w, io, nullptr, nullptr, workspace, workspace_bytes, stream);
+}
+
+extern "C" hero_status hero_layer_fwd_kv(const hero_layer_desc* desc, const hero_layer_weights* w, const hero_layer_io* io,
+                                         const hero_kv_cache* kv, const int32_t* new_len,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+    if (!kv) return HERO_ERR_NULL;
+    return layer_run(desc, w, io, kv, new_len, workspace, workspace_bytes, stream);
 }

@@ -132,7 +132,43 @@ def test_descriptions_that_are_refused():
                 dict(k=k, v=k, k_scale=s, v_scale=s, block_table=table, batch=5), dict(k=k, v=k, k_scale=s, v_scale=s, block_table=table.t())):
         with pytest.raises(ValueError):
             hero.kv_cache(**bad)
+    with pytest.raises(ValueError):
+        hero.kv_cache(k, k, s, s.to("meta"), block_table=table)
     with pytest.raises(AssertionError):
         hero.hero_kv_write(c, torch.zeros((2, 1, 3, 64), dtype=torch.bfloat16), torch.zeros((2, 1, 3, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32))
     with pytest.raises(AssertionError):
         hero.hero_kv_attn(c, torch.zeros((2, 1, 2, 64), dtype=torch.bfloat16), 1.0, HB.MASK_CAUSAL, torch.zeros(2, dtype=torch.int64))
+
+
+def test_layers_that_are_refused(lib):
+    d = HB.LayerDesc(HB.ARCH_PRE_LN, 128, 2, 64, 256, 1e-5, HB.MASK_CAUSAL, HB.MODE_M1)
+    w, io = HB.LayerWeights(), HB._LAYER_IO.pack(3, 1, 0, 0, 0, 0, P, P, 0, 0, 0, 0, 0, 0, 0)
+    call = lambda d, io, c, new=None: lib.hero_layer_fwd_kv(d, w, io, c, new, C.c_void_p(P), 1 << 30, None)  # noqa: E731
+    assert call(d, io, None) == NULL
+    assert call(d, io, _cache(Dh=96)) == UNSUPPORTED and call(d, io, _cache(B=4)) == SHAPE and call(d, io, _cache(H=1)) == SHAPE
+    assert call(HB.LayerDesc(HB.ARCH_PRE_LN, 128, 2, 64, 256, 1e-5, HB.MASK_CAUSAL, HB.MODE_M2), io, _cache()) == UNSUPPORTED
+    assert call(d, HB._LAYER_IO.pack(3, 1, 0, 0, 0, 0, P, P, P, P, 64, 0, 0, 0, 0), _cache()) == UNSUPPORTED
+    assert call(d, HB._LAYER_IO.pack(3, 65, 0, 0, 0, 0, P, P, 0, 0, 0, 0, 0, 0, 0), _cache()) == SHAPE
+    assert call(d, HB._LAYER_IO.pack(3, 0, 0, 0, 0, 0, P, P, 0, 0, 0, 0, 0, 0, 0), _cache()) == OK
+    assert lib.hero_layer_kv_workspace_bytes(d, _cache(), 1) > 0 and lib.hero_layer_kv_workspace_bytes(d, _cache(Dh=96), 1) == 0
+    assert lib.hero_layer_kv_workspace_bytes(d, None, 1) == 0
+    assert lib.hero_layer_kv_workspace_bytes(d, _cache(max_blocks=8192, n_blocks=1), 1) >= lib.hero_kv_attn_workspace_bytes(_cache(max_blocks=8192, n_blocks=1), 2, 1) > 0
+
+
+def test_a_read_of_too_many_rows(lib):
+    assert _read(lib, _cache(), S=1 << 30) == SHAPE
+
+
+def test_a_cache_on_another_device_than_the_current_one(monkeypatch):
+    import paper_2310_17723_amd as pkg
+    hero = pkg.load()
+    k, s = torch.zeros((6, 16, 2, 64), dtype=torch.int8), torch.zeros((6, 2))
+    c = hero.kv_cache(k, k, s, s, max_blocks=3, batch=2)
+    q, lens = torch.zeros((2, 1, 2, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: hero.hero_kv_write(c, q, q, lens), lambda: hero.hero_kv_read(c, 1, lens), lambda: hero.hero_kv_attn(c, q, 1.0, HB.MASK_CAUSAL, lens)):
+        with pytest.raises(ValueError):
+            call()
+    c.device = 1                                                          # rows that do not lie where the cache does
+    with pytest.raises(AssertionError):
+        hero.hero_kv_attn(c, q, 1.0, HB.MASK_CAUSAL, lens)
