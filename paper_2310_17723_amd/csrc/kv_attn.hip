@@ -27,6 +27,7 @@ struct AttnArgs {
     const int32_t *kv_len, *new_len;
     uint16_t* out; int64_t ldo;
     int tiles, splits;                                        // tiles of rows; pieces of the keys
+    FastDiv by_group, by_splits, by_tiles, by_heads, by_bh8;  // (bh8: eighths of the heads of all sequences, rounded up)
     float* part; float* part_ml;                              // [B][H][rows][splits][Dh], [..][2]: a piece's sum of P c_v; its m, its denominator
 };
 
@@ -116,11 +117,23 @@ __device__ __forceinline__ float queries(const v4i (&raw)[N], float scale, v8h (
     }
 }
 
-// keys that row's query sees: [0, result)
+// Vector loads from a wave-uniform address: offsets of 32 bits per lane and per wave beside a descriptor in scalar registers.  (Of a pointer
+// plus an offset the compiler makes a 64-bit vector addition per load, and keeps the offsets in 64 bits.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_base(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, -1, 0x00020000);
+}
+__device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t base, uint32_t lane_offset, uint32_t wave_offset) {
+    return __builtin_amdgcn_raw_buffer_load_b32(base, (int)lane_offset, (int)wave_offset, 0);
+}
+__device__ __forceinline__ v4i load4(__amdgpu_buffer_rsrc_t base, uint32_t lane_offset, uint32_t wave_offset) {
+    return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(base, (int)lane_offset, (int)wave_offset, 0));
+}
+
+// keys that row's query sees: [0, result).  (s + 1 <= n: no sum passes len)
 __device__ __forceinline__ int keys_seen(const AttnArgs& a, int row, int len, int n) {
-    const int s = row / a.group;
+    const int s = a.by_group.div(row);
     if (row >= a.Sq * a.group || s >= n) return 0;
-    return a.causal ? (int)max((int64_t)0, min((int64_t)len, (int64_t)s + 1 + len - n)) : len;
+    return a.causal ? max(0, len + (s + 1 - n)) : len;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -137,10 +150,8 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) float so[NW][16][OLD];
     __shared__ float sm[NW][ROWS], sl[NW][ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-    int u = blockIdx.x;
-    const int split = u % a.splits; u /= a.splits;
-    const int tile = u % a.tiles; u /= a.tiles;
-    const int h = u % a.c.H, b = u / a.c.H;
+    int split = blockIdx.x, tile = a.by_splits.divmod(split), h = a.by_tiles.divmod(tile);
+    const int b = a.by_heads.divmod(h);
     const int block = 1 << a.c.log2_block;
     const int len = min(max(a.kv_len[b], 0), a.c.max_blocks << a.c.log2_block);
     const int n = a.new_len ? min(max(a.new_len[b], 0), a.Sq) : a.Sq;
@@ -164,7 +175,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
     float rc[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int row = min(row0 + rt * 16 + c, nrows - 1), s = row / a.group;
+        const int row = min(row0 + rt * 16 + c, nrows - 1), s = a.by_group.div(row);
         const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + row - s * a.group) * a.qs[2] + g * 16;
         v4i raw[KS];
 #pragma unroll
@@ -370,7 +381,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
             } else {
                 // (a score beyond fp32 has no exponent: NaN; no key: 0)
                 const float inv = top == INFINITY ? __builtin_nanf("") : (L == 0.0f ? 0.0f : 1.0f / L);
-                const int s = row / a.group;
+                const int s = a.by_group.div(row);
                 uint16_t* const op = a.out + ((int64_t)b * a.Sq + s) * a.ldo + (int64_t)(h * a.group + row - s * a.group) * DH + e;
                 *reinterpret_cast<v2i*>(op) = v2i{(int)pack2_hp<DT>(sum[0] * inv, sum[1] * inv), (int)pack2_hp<DT>(sum[2] * inv, sum[3] * inv)};
             }
@@ -379,56 +390,53 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Many rows: a workgroup of four waves owns 128 RTW rows, a wave 32 RTW of them; K and V of 64 keys at a time are made FP16 once, on their way
+// Many rows: a workgroup of eight waves owns 256 rows, a wave 32 of them; K and V of 64 keys at a time are made FP16 once, on their way
 // into LDS (K by rows, V by channels), three tiles deep, so that one barrier per tile is enough: a tile is written while the one before it is
-// worked on.  Scores are computed transposed (S^T = K Q^T): a lane owns query lane % 32 of each of its RTW row tiles, and the exponentials are
-// the second product's operand as they stand.  The scores of 32 keys are made while the exponentials of the 32 before them are taken.
-// The maximum is raised, and the sums so far rescaled, only when a score exceeds it by SLACK (P stays within FP16's 2^15).
+// worked on.  Scores are computed transposed (S^T = K Q^T): a lane owns query lane % 32, and the exponentials are the second product's operand
+// as they stand.  A step makes the scores of 32 keys, takes the exponentials of the 32 before them and multiplies V by those of the 32 before
+// those, in one block of instructions.
+// The maximum is not taken of every step's scores: exponentials are taken against the last one, and only a row whose 32 add up to more than
+// 2^15 (FP16 holds 65504; a score 2^7 times as likely as the last maximum) has its maximum raised, its sums rescaled and the step's
+// exponentials taken again.
 // K's rows are 16 bytes longer than they need to be, V's 16-byte pieces XOR-swizzled by their row: fragment reads (turns of lanes 0-3, 12-15,
 // 20-27 and so on) meet no bank conflict.
 // ------------------------------------------------------------------------------------------
-constexpr float SLACK = 7.0f;
+constexpr float HEADROOM = 8.0f;                             // what a maximum's own P is 2 to the power of
+constexpr float MOST_P = 32768.0f;
 
-// The order of a step's instructions: vector instructions between the matrix instructions, which run beside them.
-template <int DS, int CT, int RTW, bool STAGE>
-__device__ __forceinline__ void interleave() {
-#define HERO_ORDER(what, count) __builtin_amdgcn_sched_group_barrier(what, count, 0)
-    constexpr int LDS_READ = 0x100, LDS_WRITE = 0x200, MATRIX = 0x008, EXP = 0x400;
-    HERO_ORDER(LDS_READ, 4);
+// The order of a step's instructions: an exponential and an LDS read behind each matrix instruction.
+template <int COUNT>
+__device__ __forceinline__ void step_order() {
+    constexpr int LDS_READ = 0x100, MATRIX = 0x008, EXP = 0x400;
+    __builtin_amdgcn_sched_group_barrier(LDS_READ, 4, 0);
 #pragma unroll
-    for (int i = 0; i < DS; ++i) {
-        HERO_ORDER(MATRIX, RTW);
-        HERO_ORDER(LDS_READ, 1);
-        HERO_ORDER(EXP, 2 * RTW);
+    for (int i = 0; i < COUNT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(MATRIX, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(LDS_READ, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(EXP, 16 / COUNT, 0);
     }
-#pragma unroll
-    for (int i = 0; i < 2 * CT; ++i) {
-        HERO_ORDER(MATRIX, RTW);
-        HERO_ORDER(LDS_READ, 1);
-        if constexpr (STAGE) HERO_ORDER(LDS_WRITE, 1);
-    }
-#undef HERO_ORDER
 }
 
-template <int DH, int FMT, int DT, int NW, int RTW, int NI>          // NI: blocks that a tile's 64 keys lie in
-__global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
-    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2 + 16, NB = 3, NT = 64 * NW, ROWS = 32 * RTW * NW;
+template <int DH, int FMT, int DT, int NI>                   // NI: blocks that a tile's 64 keys lie in
+__global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
+    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2 + 16, NB = 3, ROWS = 256;
     constexpr int GH = NI == 4 ? 2 : 1, GE = 16 / GH;        // groups of keys with scales of their own in 32 keys
-    static_assert(NT == 512, "one unit of K and of V per thread");
-    __shared__ __attribute__((aligned(1024))) uint8_t sK[NB][64 * KROW], sV[NB][DH * 128];
+    constexpr int OROW = DH * 2 + 16;                        // a row of the result on its way out
+    __shared__ __attribute__((aligned(1024))) uint8_t pool[NB * (64 * KROW + DH * 128)];
+    static_assert(8 * 32 * OROW <= sizeof(pool), "every wave's rows of the result fit");
+    uint8_t (* const sK)[64 * KROW] = reinterpret_cast<uint8_t (*)[64 * KROW]>(pool);
+    uint8_t (* const sV)[DH * 128] = reinterpret_cast<uint8_t (*)[DH * 128]>(pool + NB * 64 * KROW);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, ql = lane & 31;
-    int u = blockIdx.x;
     const int nrows = a.Sq * a.group;
     // workgroups go round-robin to the XCDs: a head's row tiles to one of them; the last rows (which see the most keys) first
-    const int xcd = u & 7; u >>= 3;
-    const int per_xcd = (a.B * a.c.H + 7) / 8;
-    const int split = u % a.splits; u /= a.splits;
-    const int bh = (u % per_xcd) * 8 + xcd, tile = a.tiles - 1 - u / per_xcd;
+    int split = (int)(blockIdx.x >> 3), bh8 = a.by_splits.divmod(split);
+    const int tile = a.tiles - 1 - a.by_bh8.divmod(bh8), bh = bh8 * 8 + (int)(blockIdx.x & 7);
     if (bh >= a.B * a.c.H) return;
-    const int h = bh % a.c.H, b = bh / a.c.H;
+    int h = bh;
+    const int b = a.by_heads.divmod(h);
     const int len = min(max(a.kv_len[b], 0), a.c.max_blocks << a.c.log2_block);
     const int n = a.new_len ? min(max(a.new_len[b], 0), a.Sq) : a.Sq;
-    const int row0 = tile * ROWS, wrow = row0 + wave * 32 * RTW;
+    const int row0 = tile * ROWS, wrow = row0 + wave * 32, row = wrow + ql;
     auto range = [&](int r0, int count, int& all, int& last) {           // of rows [r0, r0 + count): keys that all / any of them see
         const int r1 = min(r0 + count, nrows) - 1;
         last = r0 >= n * a.group ? 0 : max(keys_seen(a, r0, len, n), keys_seen(a, min(r1, n * a.group - 1), len, n));
@@ -438,25 +446,10 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     };
     int all, last, wall, wlast;
     range(row0, ROWS, all, last);
-    range(wrow, 32 * RTW, wall, wlast);
-    int seen[RTW];
-#pragma unroll
-    for (int rt = 0; rt < RTW; ++rt) seen[rt] = keys_seen(a, wrow + rt * 32 + ql, len, n);
+    range(wrow, 32, wall, wlast);
+    const int seen = keys_seen(a, row, len, n);
     const int total = (last + 63) / 64, per = (total + a.splits - 1) / a.splits;
-    const int t0 = min(split * per, total), t1 = min(t0 + per, total), wt = min(t1, (wlast + 63) / 64);
-
-    v8h qf[RTW][DS];
-    float rc[RTW];
-    v16f o[RTW][CT];
-    float m[RTW], l[RTW];
-#pragma unroll
-    for (int rt = 0; rt < RTW; ++rt) {
-        m[rt] = -INFINITY; l[rt] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[rt][c][r] = 0.0f;
-    }
+    const int t0 = min(split * per, total), t1 = min(t0 + per, total), wt = min(t1, (wlast + 63) / 64), te = t1 - 1;
 
     // ---- staging.  K: a thread's unit is 16 codes of a key; V: 4 channels of 4 keys.  (Dh = 64: half of the threads do the other half's again.)
     v4i kr;
@@ -467,19 +460,16 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     // A wave's units all lie in one group of 16 keys; a tile's keys in NI blocks (the same one, of 64 tokens or more).  The table is read three
     // tiles ahead, the codes two, the scales one; as vector loads, since a scalar load's wait would be one for all LDS reads too.
     const int group16 = DH == 128 ? wave >> 1 : wave & 3;
-    uint32_t nought;
-    asm("v_mov_b32 %0, 0" : "=v"(nought));
-    const uint32_t koff = (uint32_t)(krow & 15) * (uint32_t)a.c.k.s_row + (uint32_t)kch * 16;
-    uint32_t voff[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) voff[j] = (uint32_t)((vq & 3) * 4 + j) * (uint32_t)a.c.v.s_row + (uint32_t)vch * 4;
+    const int kstride = (int)a.c.k.s_row, vstride = (int)a.c.v.s_row;    // (a block's rows span less than 2^31 elements)
+    const uint32_t koff = (uint32_t)((krow & 15) * kstride + kch * 16);
+    const uint32_t voff = (uint32_t)((vq & 3) * 4 * vstride + vch * 4);
     typedef int Ids[NI];
     const int32_t* const table = a.c.table + (int64_t)b * a.c.max_blocks;
     auto look = [&](int t, Ids& raw) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int at = min((t * 64 + i * (64 / NI)) >> a.c.log2_block, a.c.max_blocks - 1);
-            raw[i] = a.c.table ? (table + at)[nought] : b * a.c.max_blocks + at;
+            raw[i] = a.c.table ? (int)load1(uniform_base(table + at), 0, 0) : b * a.c.max_blocks + at;
         }
     };
     auto settle = [&](const Ids& raw, Ids& id) __attribute__((always_inline)) {
@@ -491,17 +481,16 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
     };
     const uint8_t* const khead = a.c.k.codes + (int64_t)h * a.c.k.s_head;
     const uint8_t* const vhead = a.c.v.codes + (int64_t)h * a.c.v.s_head;
-    const int vrow = (int)a.c.v.s_row, krow_ = (int)a.c.k.s_row;         // (a block's rows span less than 2^31 elements)
     auto fetch = [&](int t, const Ids& id) __attribute__((always_inline)) {
         int blk = 0;                             // id[group16 NI / 4], by masks: an index that is not known would put the array into memory
 #pragma unroll
         for (int i = 0; i < NI; ++i) blk |= id[i] & -(int)(group16 * NI / 4 == i);
         const int first = t * 64 + group16 * 16, at = first & ((1 << a.c.log2_block) - 1);
-        const uint8_t* const kp = khead + (int64_t)max(blk, 0) * a.c.k.s_block + (uint32_t)(at * krow_);
-        const uint8_t* const vp = vhead + (int64_t)max(blk, 0) * a.c.v.s_block + (uint32_t)(at * vrow);
-        kr = *reinterpret_cast<const v4i*>(kp + koff);
+        const uint8_t* const kp = khead + (int64_t)max(blk, 0) * a.c.k.s_block + (uint32_t)(at * kstride);
+        const uint8_t* const vp = vhead + (int64_t)max(blk, 0) * a.c.v.s_block + (uint32_t)(at * vstride);
+        kr = load4(uniform_base(kp), koff, 0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) vr[j] = *reinterpret_cast<const uint32_t*>(vp + voff[j]);
+        for (int j = 0; j < 4; ++j) vr[j] = load1(uniform_base(vp), voff, (uint32_t)(j * vstride));
         vend = blk < 0 ? 0 : len - first - (vq & 3) * 4;
     };
     float sk[NI], sv[NI];
@@ -511,8 +500,8 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int64_t at = (int64_t)max(id[i], 0) * a.c.H;
-            sk[i] = (kscale + at)[nought];
-            sv[i] = (vscale + at)[nought];
+            sk[i] = __uint_as_float(load1(uniform_base(kscale + at), 0, 0));
+            sv[i] = __uint_as_float(load1(uniform_base(vscale + at), 0, 0));
         }
     };
     // what lies behind the last key, or where no block is, is no code
@@ -540,110 +529,33 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
             *reinterpret_cast<v2i*>(&sV[buf][(vput ^ (((rr & 7) ^ ((rr >> 3) & 1)) * 16)) + i * 128]) = v2i{(int)w[i][0], (int)w[i][1]};
         }
     };
+    // what was written to LDS is there for the other waves, and global loads stay in flight
+    auto meet = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
 
-    // scores of 32 keys (s of tile t in buf)
+    // ---- the arithmetic
+    v8h qf[DS];
+    v16f o[CT];
+    float rc, m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c][r] = 0.0f;
+    // scores of 32 keys (s of the tile in buf)
     const uint32_t kget = ql * KROW + hh * 16;
     const uint32_t vget = ql * 128 + (hh ^ ((ql >> 1) & 7) ^ (ql >> 4)) * 16;
-    typedef v16f Scores[RTW];
-    auto scores = [&](int buf, int s, Scores& acc) __attribute__((always_inline)) {
-        const v16f zero = {};
+    auto scores = [&](int buf, int s) __attribute__((always_inline)) -> v16f {
+        v16f acc = {};
         const uint8_t* const from = &sK[buf][s * 32 * KROW];
 #pragma unroll
-        for (int d = 0; d < DS; ++d) {
-            const v8h kf = *reinterpret_cast<const v8h*>(from + kget + d * 32);
-#pragma unroll
-            for (int rt = 0; rt < RTW; ++rt) acc[rt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[rt][d], d ? acc[rt] : zero, 0, 0, 0);
-        }
+        for (int d = 0; d < DS; ++d) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h*>(from + kget + d * 32), qf[d], acc, 0, 0, 0);
+        return acc;
     };
-    // their exponentials, and the second product
+    // of the scales that have come: what the exponents are made of (score * ck + lv); a group without a block has no keys
     struct Group { float ks, lv, iv; int lim; };
-    float ck[RTW][GH], lv[GH];
-    auto raise = [&](int t, int s, Scores& acc, const Group (&gr)[GH], bool edge) __attribute__((always_inline)) {
-        float cand[RTW];
-#pragma unroll
-        for (int g = 0; g < GH; ++g) {
-            lv[g] = gr[g].lv;
-#pragma unroll
-            for (int rt = 0; rt < RTW; ++rt) ck[rt][g] = rc[rt] * gr[g].ks;
-        }
-        if (edge) {                              // the exponents themselves, those of hidden keys (of scales that may be NaN) replaced
-#pragma unroll
-            for (int rt = 0; rt < RTW; ++rt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = t * 64 + s * 32 + (r >> 2) * 8 + hh * 4 + (r & 3);
-                    const float x = fmaf(acc[rt][r], ck[rt][r / GE], lv[r / GE]);
-                    acc[rt][r] = key < min(seen[rt], gr[r / GE].lim) ? x : -INFINITY;
-                }
-#pragma unroll
-            for (int g = 0; g < GH; ++g) {
-                lv[g] = 0.0f;
-#pragma unroll
-                for (int rt = 0; rt < RTW; ++rt) ck[rt][g] = 1.0f;
-            }
-        }
-#pragma unroll
-        for (int rt = 0; rt < RTW; ++rt) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int g = 0; g < GH; ++g) {
-                float x = acc[rt][g * GE];
-#pragma unroll
-                for (int r = 1; r < GE; ++r) x = fmaxf(x, acc[rt][g * GE + r]);
-                top = fmaxf(top, fmaf(x, ck[rt][g], lv[g]));
-            }
-            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-            cand[rt] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-        }
-        bool above = cand[0] > m[0] + SLACK;
-#pragma unroll
-        for (int rt = 1; rt < RTW; ++rt) above |= cand[rt] > m[rt] + SLACK;
-        if (__builtin_amdgcn_ballot_w64(above) != 0) {
-#pragma unroll
-            for (int rt = 0; rt < RTW; ++rt) {
-                // (a row by its own scores alone: its result does not depend on the others of its wave)
-                const float mn = cand[rt] > m[rt] + SLACK ? cand[rt] : m[rt], resc = mn > m[rt] ? __builtin_amdgcn_exp2f(m[rt] - mn) : 1.0f;
-                m[rt] = mn;
-                l[rt] *= resc;
-#pragma unroll
-                for (int c = 0; c < CT; ++c)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[rt][c][r] *= resc;
-            }
-        }
-    };
-    auto take = [&](int buf, int s, Scores& acc, const Group (&gr)[GH]) __attribute__((always_inline)) {
-        uint32_t p[RTW][8];
-#pragma unroll
-        for (int rt = 0; rt < RTW; ++rt) {
-            const float sub = (m[rt] > -INFINITY ? m[rt] : 0.0f) - (LIFT - SLACK);
-#pragma unroll
-            for (int g = 0; g < GH; ++g) {
-                const float add = lv[g] - sub;
-                float sum = 0.0f;
-#pragma unroll
-                for (int r = g * GE; r < (g + 1) * GE; r += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(acc[rt][r], ck[rt][g], add));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(acc[rt][r + 1], ck[rt][g], add));
-                    sum += e0 + e1;
-                    p[rt][r >> 1] = f16x2(e0, e1);
-                }
-                l[rt] += sum == 0.0f ? 0.0f : sum * gr[g].iv;
-            }
-        }
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const v8h vf = *reinterpret_cast<const v8h*>(&sV[buf][(vget ^ ((s * 2 + st) * 32)) + c * 4096]);
-#pragma unroll
-                for (int rt = 0; rt < RTW; ++rt) {
-                    const v8h pf = __builtin_bit_cast(v8h, v4i{(int)p[rt][4 * st], (int)p[rt][4 * st + 1], (int)p[rt][4 * st + 2], (int)p[rt][4 * st + 3]});
-                    o[rt][c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf, o[rt][c], 0, 0, 0);
-                }
-            }
-    };
-    // of the scales that have come: what the exponents are made of; a group without a block has no keys
     auto groups = [&](const Ids& id, Group (&gr)[2][GH]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
@@ -652,24 +564,98 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
             else gr[i / GH][i % GH] = x;
         }
     };
-    // what was written to LDS is there for the other waves, and global loads stay in flight
-    auto meet = [&]() __attribute__((always_inline)) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    float ck[GH], lv[GH], sum[GH];
+    uint32_t p[8] = {0, 0, 0, 0, 0, 0, 0, 0}, q[8];                      // of the step before (nothing yet), of this one
+    auto exponents = [&](int t, int s, v16f& acc, const Group (&gr)[GH], bool edge) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < GH; ++g) { lv[g] = gr[g].lv; ck[g] = rc * gr[g].ks; }
+        if (edge) {                              // the exponents themselves, those of hidden keys (of scales that may be NaN) replaced
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int key = t * 64 + s * 32 + (r >> 2) * 8 + hh * 4 + (r & 3);
+                const float x = fmaf(acc[r], ck[r / GE], lv[r / GE]);
+                acc[r] = key < min(seen, gr[r / GE].lim) ? x : -INFINITY;
+            }
+#pragma unroll
+            for (int g = 0; g < GH; ++g) { lv[g] = 0.0f; ck[g] = 1.0f; }
+        }
+    };
+    auto weigh = [&](const v16f& acc) __attribute__((always_inline)) {
+        const float sub = (m > -INFINITY ? m : 0.0f) - HEADROOM;
+#pragma unroll
+        for (int g = 0; g < GH; ++g) {
+            const float add = lv[g] - sub;
+            sum[g] = 0.0f;
+#pragma unroll
+            for (int r = g * GE; r < (g + 1) * GE; r += 2) {
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(acc[r], ck[g], add)), e1 = __builtin_amdgcn_exp2f(fmaf(acc[r + 1], ck[g], add));
+                sum[g] += e0 + e1;
+                q[r >> 1] = f16x2(e0, e1);
+            }
+        }
+    };
+    bool fresh = true;                                                   // some row that sees a key of this piece has no maximum yet
+    auto raise = [&](const v16f& acc) __attribute__((always_inline)) {
+        float most = sum[0];
+#pragma unroll
+        for (int g = 1; g < GH; ++g) most += sum[g];
+        if (!fresh && __builtin_amdgcn_ballot_w64(most > MOST_P) == 0) return;
+        float top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < GH; ++g) {
+            float x = acc[g * GE];
+#pragma unroll
+            for (int r = 1; r < GE; ++r) x = fmaxf(x, acc[g * GE + r]);
+            top = fmaxf(top, fmaf(x, ck[g], lv[g]));
+        }
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+        top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+        most = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+        // (a row by its own scores alone: its result does not depend on the others of its wave)
+        const float mn = (most > MOST_P || m == -INFINITY) && top > m ? top : m, resc = mn > m ? __builtin_amdgcn_exp2f(m - mn) : 1.0f;
+        m = mn;
+        l *= resc;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[c][r] *= resc;
+        fresh = __builtin_amdgcn_ballot_w64(m == -INFINITY && seen > t0 * 64) != 0;
+        weigh(acc);
+    };
+    auto settled = [&](const Group (&gr)[GH]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < GH; ++g) l += sum[g] == 0.0f ? 0.0f : sum[g] * gr[g].iv;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) p[r] = q[r];
+    };
+    auto product = [&](int buf, int s, int i) __attribute__((always_inline)) {      // the i-th of its 2 CT matrix instructions
+        const int st = i / CT, c = i % CT;
+        const v8h pf = __builtin_bit_cast(v8h, v4i{(int)p[4 * st], (int)p[4 * st + 1], (int)p[4 * st + 2], (int)p[4 * st + 3]});
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h*>(&sV[buf][(vget ^ ((s * 2 + st) * 32)) + c * 4096]), pf, o[c], 0, 0, 0);
+    };
+    // the two products of a step, one matrix instruction of each after the other: the first's eight are a chain
+    static_assert(DS == 2 * CT, "as many of the one as of the other");
+    auto products = [&](int kbuf, int ks, int vbuf, int vs) __attribute__((always_inline)) -> v16f {
+        v16f acc = {};
+        const uint8_t* const from = &sK[kbuf][ks * 32 * KROW];
+#pragma unroll
+        for (int d = 0; d < DS; ++d) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const v8h*>(from + kget + d * 32), qf[d], acc, 0, 0, 0);
+            product(vbuf, vs, d);
+        }
+        return acc;
     };
 
-    Scores acc, next;
-    v4i qraw[RTW][DS];
-#pragma unroll
-    for (int rt = 0; rt < RTW; ++rt) {
-        const int row = min(wrow + rt * 32 + ql, nrows - 1), s = row / a.group;
-        const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + row - s * a.group) * a.qs[2] + hh * 8;
-#pragma unroll
-        for (int t = 0; t < DS; ++t) qraw[rt][t] = *reinterpret_cast<const v4i*>(qp + t * 16);
-    }
+    // ---- the first tile, whose codes are asked for before the queries
     Ids raw, id, id1, id2;                                               // blocks of tile t + 3 as they come, of t, t + 1, t + 2
-    const int te = t1 - 1;
+    v4i qraw[DS];
+    {
+        const int rr = min(row, nrows - 1), s = a.by_group.div(rr);
+        const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + rr - s * a.group) * a.qs[2] + hh * 8;
+#pragma unroll
+        for (int t = 0; t < DS; ++t) qraw[t] = *reinterpret_cast<const v4i*>(qp + t * 16);
+    }
     if (t0 < t1) {
         look(t0, raw);
         settle(raw, id1);
@@ -677,8 +663,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
         scales(id1);
         look(min(t0 + 1, te), raw);
     }
-#pragma unroll
-    for (int rt = 0; rt < RTW; ++rt) rc[rt] = queries<DT, DS, 32>(qraw[rt], a.scale, qf[rt]);
+    rc = queries<DT, DS, 32>(qraw, a.scale, qf);
     if (t0 < t1) {
         settle(raw, id2);
         blank();
@@ -687,7 +672,8 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
         look(min(t0 + 2, te), raw);
     }
     __syncthreads();
-    if (t0 < wt) scores(t0 % NB, 0, acc);
+    v16f acc = {}, next;
+    if (t0 < wt) acc = scores(t0 % NB, 0);
     auto next_ids = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) { id[i] = id1[i]; id1[i] = id2[i]; }
@@ -695,7 +681,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
         look(min(t + 3, te), raw);
     };
     // (behind the last tile the last one is fetched and staged again, and scores are made that nobody takes: no branch in the middle)
-    int t = t0;
+    int t = t0, before = t0 % NB;                                        // (a first product of nothing by a tile that is there)
     for (; t < wt; ++t) {
         const int buf = t % NB, after = (t + 1) % NB;
         Group gr[2][GH];
@@ -705,23 +691,27 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) edge |= id[i] < 0;
         blank();
-        raise(t, 0, acc, gr[0], edge);
-        __builtin_amdgcn_s_setprio(1);
-        scores(buf, 1, next);
-        take(buf, 0, acc, gr[0]);
+        exponents(t, 0, acc, gr[0], edge);
+        next = products(buf, 1, before, 1);
+        weigh(acc);
         stage(after);
         fetch(min(t + 2, te), id2);
         scales(id1);
-        interleave<DS, CT, RTW, true>();
-        __builtin_amdgcn_s_setprio(0);
+        step_order<DS + 2 * CT>();
+        raise(acc);
+        settled(gr[0]);
         meet();
-        raise(t, 1, next, gr[1], edge);
-        __builtin_amdgcn_s_setprio(1);
-        scores(after, 0, acc);
-        take(buf, 1, next, gr[1]);
-        interleave<DS, CT, RTW, false>();
-        __builtin_amdgcn_s_setprio(0);
+        exponents(t, 1, next, gr[1], edge);
+        acc = products(after, 0, buf, 0);
+        weigh(next);
+        step_order<DS + 2 * CT>();
+        raise(next);
+        settled(gr[1]);
+        before = buf;
     }
+    if (t0 < wt)
+#pragma unroll
+        for (int i = 0; i < DS; ++i) product(before, 1, i);
     for (; t < t1; ++t) {                                                // tiles that other waves' rows see
         next_ids(t);
         blank();
@@ -731,30 +721,38 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_tile_kernel(AttnArgs a) {
         meet();
     }
 
+    l += __shfl_xor(l, 32);
+    if (a.splits > 1) {
+        if (row >= nrows) return;
+        const int64_t pr = ((int64_t)bh * nrows + row) * a.splits + split;
 #pragma unroll
-    for (int rt = 0; rt < RTW; ++rt) {
-        l[rt] += __shfl_xor(l[rt], 32);
-        const int row = wrow + rt * 32 + ql;
-        if (row >= nrows) continue;
-        if (a.splits > 1) {
-            const int64_t pr = ((int64_t)bh * nrows + row) * a.splits + split;
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<v4f*>(a.part + pr * DH + c * 32 + g * 8 + hh * 4) = v4f{o[c][4 * g], o[c][4 * g + 1], o[c][4 * g + 2], o[c][4 * g + 3]};
+        if (hh == 0) { a.part_ml[pr * 2] = m; a.part_ml[pr * 2 + 1] = l; }
+        return;
+    }
+    // by way of LDS (each wave its own part, once all have read their last tile), so that a store covers whole rows
+    __syncthreads();
+    uint8_t* const mine = pool + wave * (32 * OROW);
+    const float inv = m == INFINITY ? __builtin_nanf("") : (l == 0.0f ? 0.0f : 1.0f / l);
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<v4f*>(a.part + pr * DH + c * 32 + g * 8 + hh * 4) = v4f{o[rt][c][4 * g], o[rt][c][4 * g + 1], o[rt][c][4 * g + 2], o[rt][c][4 * g + 3]};
-            if (hh == 0) { a.part_ml[pr * 2] = m[rt]; a.part_ml[pr * 2 + 1] = l[rt]; }
-        } else {
-            const float inv = m[rt] == INFINITY ? __builtin_nanf("") : (l[rt] == 0.0f ? 0.0f : 1.0f / l[rt]);
-            const int s = row / a.group;
-            uint16_t* const op = a.out + ((int64_t)b * a.Sq + s) * a.ldo + (int64_t)(h * a.group + row - s * a.group) * DH;
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<v2i*>(mine + ql * OROW + (c * 32 + g * 8 + hh * 4) * 2) =
+                v2i{(int)pack2_hp<DT>(o[c][4 * g] * inv, o[c][4 * g + 1] * inv), (int)pack2_hp<DT>(o[c][4 * g + 2] * inv, o[c][4 * g + 3] * inv)};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    constexpr int LPR = DH / 4, RPS = 64 / LPR;              // lanes to a row, rows to a store
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<v2i*>(op + c * 32 + g * 8 + hh * 4) =
-                        v2i{(int)pack2_hp<DT>(o[rt][c][4 * g] * inv, o[rt][c][4 * g + 1] * inv), (int)pack2_hp<DT>(o[rt][c][4 * g + 2] * inv, o[rt][c][4 * g + 3] * inv)};
-        }
+    for (int i = 0; i < 32 / RPS; ++i) {
+        const int rr = i * RPS + lane / LPR, r = wrow + rr, e = lane % LPR * 4;
+        const v2i w = *reinterpret_cast<const v2i*>(mine + rr * OROW + e * 2);
+        if (r >= nrows) continue;
+        const int s = a.by_group.div(r);
+        *reinterpret_cast<v2i*>(a.out + ((int64_t)b * a.Sq + s) * a.ldo + (int64_t)(h * a.group + r - s * a.group) * DH + e) = w;
     }
 }
 
@@ -807,7 +805,9 @@ __global__ __launch_bounds__(256) void kv_attn_join_kernel(AttnArgs a) {
         for (int t = 0; t < 4; ++t) sum[t] += x[t];
     }
     const float inv = M == INFINITY ? __builtin_nanf("") : (L == 0.0f ? 0.0f : 1.0f / L);
-    const int row = (int)(r % nrows), bh = (int)(r / nrows), h = bh % a.c.H, b = bh / a.c.H, s = row / a.group;
+    const int bh = (int)(r / nrows), row = (int)(r - (int64_t)bh * nrows), s = a.by_group.div(row);
+    int h = bh;
+    const int b = a.by_heads.divmod(h);
     uint16_t* const op = a.out + ((int64_t)b * a.Sq + s) * a.ldo + (int64_t)(h * a.group + row - s * a.group) * DH + e;
     *reinterpret_cast<v2i*>(op) = v2i{(int)pack2_hp<DT>(sum[0] * inv, sum[1] * inv), (int)pack2_hp<DT>(sum[2] * inv, sum[3] * inv)};
 }
@@ -851,9 +851,9 @@ hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
     const dim3 block(256);
     if (p.rt == 0) {
         const dim3 grid((unsigned)(((int64_t)a.B * a.c.H + 7) / 8 * 8 * a.tiles * a.splits));
-        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 4>), grid, dim3(512), 0, st, a);
-        else if (a.c.log2_block == 5) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 2>), grid, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 8, 1, 1>), grid, dim3(512), 0, st, a);
+        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 4>), grid, dim3(512), 0, st, a);
+        else if (a.c.log2_block == 5) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 2>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 1>), grid, dim3(512), 0, st, a);
     } else {
         const dim3 grid((unsigned)((int64_t)a.B * a.c.H * a.tiles * a.splits));
         if (p.rt == 1) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 1, 4>), grid, block, 0, st, a);
@@ -906,6 +906,8 @@ extern "C" hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, c
     a.B = (int)cache->B; a.Hq = (int)Hq; a.Sq = (int)Sq; a.group = (int)(Hq / cache->H);
     a.scale = scale; a.causal = mask == HERO_MASK_CAUSAL; a.kv_len = kv_len; a.new_len = new_len;
     a.out = (uint16_t*)out; a.ldo = ldo; a.tiles = p.tiles; a.splits = p.splits;
+    a.by_group = fast_div(a.group); a.by_splits = fast_div(p.splits); a.by_tiles = fast_div(p.tiles);
+    a.by_heads = fast_div(a.c.H); a.by_bh8 = fast_div((cache->B * cache->H + 7) / 8);
     a.part = (float*)workspace; a.part_ml = a.part + (p.splits > 1 ? cache->B * Sq * Hq * p.splits * Dh : 0);
 #define HERO_KVA(DH, FMT) (dt == HERO_BF16 ? launch<DH, FMT, HERO_BF16>(a, p, st) : launch<DH, FMT, HERO_F16>(a, p, st))
     if (cache->dt == HERO_I8) return Dh == 64 ? HERO_KVA(64, HERO_I8) : HERO_KVA(128, HERO_I8);

@@ -2,6 +2,24 @@
 #pragma once
 #include "hero_common.h"
 
+// n / d for 0 <= n < 2^31 without a division: (floor(m n / 2^32) + n) >> s with 2^s >= d, m = floor(2^32 (2^s - d) / d) + 1 (Granlund and
+// Montgomery's division by an invariant integer)
+struct FastDiv {
+    uint32_t m, s, d;
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+    __device__ __forceinline__ int divmod(int& n) const {                  // the remainder stays in n
+        const int q = div(n);
+        n -= q * (int)d;
+        return q;
+    }
+};
+static inline FastDiv fast_div(int64_t d) {
+    FastDiv f{0, 0, (uint32_t)d};
+    while ((1ULL << f.s) < (uint64_t)d) ++f.s;
+    f.m = (uint32_t)((((1ULL << f.s) - (uint64_t)d) << 32) / (uint64_t)d) + 1;
+    return f;
+}
+
 struct KvSide { uint8_t* codes; float* scale; int64_t s_block, s_row, s_head; };       // element strides
 
 struct KvView {
