@@ -7,6 +7,7 @@ constexpr float SMALLEST = 0x1p-64f;       // no scale is smaller: the logarithm
 
 struct WriteArgs {
     KvView c;
+    FastDiv by_heads;
     const uint16_t* x[2];                  // K, V
     int64_t xs[2][3];                      // batch, token, head
     int B, S, touched;
@@ -17,12 +18,31 @@ template <int FMT> struct Fmt;
 template <> struct Fmt<HERO_I8> { static constexpr float most = 127.0f; };
 template <> struct Fmt<HERO_F8E4M3> { static constexpr float most = 448.0f; };
 
-// four codes of values in fp32 at a scale, by the definition's IEEE division; 0 at a scale that is not finite
+// The definition's IEEE quotient x / s without a division: of r = 1 / s, rounded to nearest, x r is two units off at most, one correction with the
+// exact remainder makes it one of the quotient's neighbours and the next the quotient rounded to nearest (Markstein's theorem; for every 11-bit
+// mantissa of x and every mantissa of s it is, by trial).  The
+// remainder is exact where a code can depend on it: |x / s| >= 2^-10 with s >= 2^-64 leaves it above 2^-100.  At a scale that is not finite: 0 for
+// every finite x.
+struct Divisor {
+    float s, r;
+    __device__ __forceinline__ explicit Divisor(float scale) {
+        const bool ok = scale == scale && scale < INFINITY;
+        s = ok ? scale : 1.0f;
+        r = ok ? __fdiv_rn(1.0f, s) : 0.0f;
+    }
+    __device__ __forceinline__ float quotient(float x) const {
+        float q = x * r;
+        q = fmaf(fmaf(-q, s, x), r, q);
+        return fmaf(fmaf(-q, s, x), r, q);
+    }
+};
+
+// four codes of finite values in fp32 at a scale
 template <int FMT>
-__device__ __forceinline__ uint32_t codes4(const float* x, float s) {
+__device__ __forceinline__ uint32_t codes4(const float* x, const Divisor& by) {
     float y[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) y[t] = __fdiv_rn(x[t], s);
+    for (int t = 0; t < 4; ++t) y[t] = by.quotient(x[t]);
     if constexpr (FMT == HERO_I8) return quant4_sat(y[0], y[1], y[2], y[3]);
     else return fp8x4_sat(y[0], y[1], y[2], y[3]);
 }
@@ -43,17 +63,14 @@ __device__ __forceinline__ void values4(uint32_t w, float (&x)[4]) {
 // each), so that they are read once for the maximum and the codes.  The maximum is one of bit patterns: NaN > infinity > numbers.
 // A unit whose block holds older tokens and whose maximum grows codes those anew from the cache.
 // ------------------------------------------------------------------------------------------
-template <int FMT, int DT, int TPU, int CH>
-__global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a, int Dh) {
+template <int FMT, int DT, int DH, int TPU, int CH>
+__global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
     constexpr int UPB = 256 / TPU;
     __shared__ uint32_t part[4];
-    const int tid = threadIdx.x % TPU, cpr = Dh / 8;
-    int64_t u = (int64_t)blockIdx.x * UPB + threadIdx.x / TPU;
-    if constexpr (TPU >= 64) u = (int64_t)blockIdx.x * UPB + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / TPU));
-    const int h = (int)(u % a.c.H); u /= a.c.H;
-    const int t = (int)(u % a.touched); u /= a.touched;
-    const int side = (int)(u & 1), b = (int)(u >> 1);
-    if (b >= a.B) return;
+    constexpr int cpr = DH / 8;
+    const int tid = threadIdx.x % TPU;
+    int h = (int)blockIdx.x * UPB + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / TPU));
+    const int t = a.by_heads.divmod(h), b = blockIdx.y, side = blockIdx.z;
     const int block = 1 << a.c.log2_block, cap = a.c.max_blocks << a.c.log2_block;
     const int len = a.kv_len[b], n = a.new_len ? min(max(a.new_len[b], 0), a.S) : a.S;
     const int64_t origin = (int64_t)len - n;                             // the position of row 0
@@ -62,13 +79,6 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a, int Dh) {
     const int64_t first = ((int64_t)(begin >> a.c.log2_block) + t) << a.c.log2_block;
     const int lo = (int)max((int64_t)begin, first), hi = (int)min((int64_t)end, first + block);
     if (lo >= hi) return;
-    const int blk = a.c.block_of(b, (int)(first >> a.c.log2_block));
-    if (blk < 0) return;
-    const KvSide sd = side ? a.c.v : a.c.k;
-    float* const scale = sd.scale + (int64_t)blk * a.c.H + h;
-    const bool older = lo > first;
-    const float s_old = older ? *scale : 0.0f;
-
     const uint16_t* const x = a.x[side] + (int64_t)b * a.xs[side][0] + (lo - origin) * a.xs[side][1] + (int64_t)h * a.xs[side][2];
     const int chunks = (hi - lo) * cpr;
     v4i raw[CH];
@@ -79,6 +89,13 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a, int Dh) {
         raw[i] = v4i{0, 0, 0, 0};
         if (at < chunks) raw[i] = *reinterpret_cast<const v4i*>(x + (int64_t)(at / cpr) * a.xs[side][1] + (at % cpr) * 8);
     }
+    // (the rows are on their way while the block is looked up)
+    const int blk = a.c.block_of(b, (int)(first >> a.c.log2_block));
+    if (blk < 0) return;
+    const KvSide sd = side ? a.c.v : a.c.k;
+    float* const scale = sd.scale + (int64_t)blk * a.c.H + h;
+    const bool older = lo > first;
+    const float s_old = older ? *scale : 0.0f;
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
@@ -97,7 +114,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a, int Dh) {
     const float wanted = fmaxf(__fdiv_rn(hp_to_f32<DT>(top), Fmt<FMT>::most), SMALLEST);
     const float s = !finite || s_old != s_old ? __builtin_nanf("") : fmaxf(s_old, wanted);
     if (tid == 0) *scale = s;
-    const float by = s == s ? s : INFINITY;                              // (codes at a scale that is NaN: 0, whatever the values)
+    const Divisor by(s);                                                 // (codes at a scale that is NaN: 0, whatever the values)
     uint8_t* const out = sd.codes + (int64_t)blk * sd.s_block + (int64_t)h * sd.s_head;
     const int r0 = (int)(lo - first);
 #pragma unroll
@@ -113,7 +130,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a, int Dh) {
         *reinterpret_cast<v2i*>(out + (int64_t)(r0 + at / cpr) * sd.s_row + (at % cpr) * 8) =
             v2i{(int)codes4<FMT>(f, by), (int)codes4<FMT>(f + 4, by)};
     }
-    if (older && !(s == s_old))
+    if (older && !(s == s_old)) {
         for (int at = tid; at < r0 * cpr; at += TPU) {
             v2i* const p = reinterpret_cast<v2i*>(out + (int64_t)(at / cpr) * sd.s_row + (at % cpr) * 8);
             v2i w = *p;
@@ -122,11 +139,12 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a, int Dh) {
                 float f[4];
                 values4<FMT>((uint32_t)w[j], f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = s == s ? f[e] * s_old : 0.0f;
+                for (int e = 0; e < 4; ++e) f[e] = s == s ? f[e] * s_old : 0.0f;   // (of a scale that was NaN, too)
                 w[j] = (int)codes4<FMT>(f, by);
             }
             *p = w;
         }
+    }
 }
 
 struct ReadArgs {
@@ -179,15 +197,15 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
     }
 }
 
-template <int FMT, int DT>
-hero_status launch_write(const WriteArgs& a, int Dh, int rows, hipStream_t st) {
-    const int64_t units = (int64_t)a.B * 2 * a.touched * a.c.H;
-    const int chunks = rows * (Dh / 8);                                  // of the fullest unit
+template <int FMT, int DT, int DH>
+hero_status launch_write(const WriteArgs& a, int rows, hipStream_t st) {
+    const int64_t units = (int64_t)a.touched * a.c.H;                    // of a sequence's K (or V)
+    const int chunks = rows * (DH / 8);                                  // of the fullest unit
     const int upb = chunks <= 256 ? 4 : 1;
     const int64_t nb = (units + upb - 1) / upb;
-    if (nb > 0x7fffffffLL) return HERO_ERR_SHAPE;
-    const dim3 grid((unsigned)nb), block(256);
-#define HERO_KVW(TPU, CH) hipLaunchKernelGGL((kv_write_kernel<FMT, DT, TPU, CH>), grid, block, 0, st, a, Dh)
+    if (units > 0x7ffffff0LL) return HERO_ERR_SHAPE;
+    const dim3 grid((unsigned)nb, (unsigned)a.B, 2), block(256);
+#define HERO_KVW(TPU, CH) hipLaunchKernelGGL((kv_write_kernel<FMT, DT, DH, TPU, CH>), grid, block, 0, st, a)
     if (chunks <= 64) HERO_KVW(64, 1);
     else if (chunks <= 256) HERO_KVW(64, 4);
     else if (chunks <= 1024) HERO_KVW(256, 4);
@@ -220,10 +238,13 @@ extern "C" hero_status hero_kv_write(const hero_kv_cache* cache, const void* k, 
     a.B = (int)cache->B; a.S = (int)S; a.kv_len = kv_len; a.new_len = new_len;
     a.touched = (int)((S + cache->block - 2) / cache->block + 1);        // S tokens lie in at most so many blocks
     if (a.touched > a.c.max_blocks) a.touched = a.c.max_blocks;
-    const int rows = S < cache->block ? (int)S : cache->block, Dh = cache->Dh;
+    const int rows = S < cache->block ? (int)S : cache->block;
+    a.by_heads = fast_div(a.c.H);
     hipStream_t st = (hipStream_t)stream;
-    if (cache->dt == HERO_I8) return dt == HERO_BF16 ? launch_write<HERO_I8, HERO_BF16>(a, Dh, rows, st) : launch_write<HERO_I8, HERO_F16>(a, Dh, rows, st);
-    return dt == HERO_BF16 ? launch_write<HERO_F8E4M3, HERO_BF16>(a, Dh, rows, st) : launch_write<HERO_F8E4M3, HERO_F16>(a, Dh, rows, st);
+#define HERO_KVW(FMT, DT) (cache->Dh == 64 ? launch_write<FMT, DT, 64>(a, rows, st) : launch_write<FMT, DT, 128>(a, rows, st))
+    if (cache->dt == HERO_I8) return dt == HERO_BF16 ? HERO_KVW(HERO_I8, HERO_BF16) : HERO_KVW(HERO_I8, HERO_F16);
+    return dt == HERO_BF16 ? HERO_KVW(HERO_F8E4M3, HERO_BF16) : HERO_KVW(HERO_F8E4M3, HERO_F16);
+#undef HERO_KVW
 }
 
 extern "C" hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, const int64_t k_strides[4],
