@@ -757,52 +757,68 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// The pieces of the keys joined: a workgroup per row; groups of DH / 4 threads take every eighth (sixteenth) piece, four at a time in
-// flight, and meet in LDS, in a fixed order.  (A group per row that took its pieces one after the other: 31 us for 32 pieces of 128 rows.)
+// The pieces of the keys joined: a row is the business of GPR groups of DH / 4 threads, each of which takes every GPR-th piece, four at a time
+// in flight; the groups meet in LDS.  All in a fixed order.  (One group whose loads waited for each other: 31 us for 32 pieces of 128 rows, eight
+// groups 4; eight groups for the 4 pieces of 2560 rows 4.8, one 3.)
 // ------------------------------------------------------------------------------------------
-template <int DH, int DT>
+template <int DH, int DT, int GPR>
 __global__ __launch_bounds__(256) void kv_attn_join_kernel(AttnArgs a) {
-    constexpr int TPR = DH / 4, NG = 256 / TPR;
-    __shared__ __attribute__((aligned(16))) float so[NG][DH];
-    __shared__ float sl[NG];
-    const int nrows = a.Sq * a.group, tid = threadIdx.x, grp = tid / TPR, e = (tid % TPR) * 4, lane = tid & 63;
-    const int64_t r = blockIdx.x;
+    constexpr int TPR = DH / 4, RPB = 256 / TPR / GPR;
+    __shared__ __attribute__((aligned(16))) float so[GPR > 1 ? GPR : 1][DH];
+    __shared__ float sm[GPR], sl[GPR];
+    static_assert(GPR == 1 || RPB == 1, "one row where groups meet");
+    const int nrows = a.Sq * a.group, tid = threadIdx.x, grp = GPR > 1 ? tid / TPR : 0, e = (tid % TPR) * 4;
+    const int64_t r = (int64_t)blockIdx.x * RPB + (GPR > 1 ? 0 : tid / TPR);
+    if (r >= (int64_t)a.B * a.c.H * nrows) return;
     const float* const ml = a.part_ml + r * a.splits * 2;
     const float* const p = a.part + r * a.splits * DH + e;
-    // at most MOST_PIECES: two to a lane
-    const float m0 = lane < a.splits ? ml[2 * lane] : -INFINITY, m1 = lane + 64 < a.splits ? ml[2 * lane + 128] : -INFINITY;
-    const float M = wave_max(fmaxf(m0, m1));
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    float L = 0.0f;
-    for (int s0 = grp; s0 < a.splits; s0 += 4 * NG) {
+    float M = -INFINITY, L = 0.0f;
+    for (int s0 = grp; s0 < a.splits; s0 += 4 * GPR) {
         v4f x[4];
-        float m[4], l[4];
+        float m[4], l[4], top = M;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int s = min(s0 + i * NG, a.splits - 1);
+            const int s = min(s0 + i * GPR, a.splits - 1);
             x[i] = *reinterpret_cast<const v4f*>(p + (int64_t)s * DH);
             m[i] = ml[2 * s];
-            l[i] = s0 + i * NG < a.splits ? ml[2 * s + 1] : 0.0f;
+            l[i] = s0 + i * GPR < a.splits ? ml[2 * s + 1] : 0.0f;        // (0: no key in it; its maximum is -inf)
         }
 #pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, m[i]);
+        const float base = top > -INFINITY ? top : 0.0f, f0 = __builtin_amdgcn_exp2f(M - base);
+        L *= f0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sum[t] *= f0;
+#pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (l[i] == 0.0f) continue;                                   // (no key in it; its maximum is -inf)
-            const float f = __builtin_amdgcn_exp2f(m[i] - M);
+            if (l[i] == 0.0f) continue;
+            const float f = __builtin_amdgcn_exp2f(m[i] - base);
             L = fmaf(l[i], f, L);
 #pragma unroll
             for (int t = 0; t < 4; ++t) sum[t] = fmaf(x[i][t], f, sum[t]);
         }
+        M = top;
     }
-    *reinterpret_cast<v4f*>(&so[grp][e]) = sum;
-    if (e == 0) sl[grp] = L;
-    __syncthreads();
-    if (grp) return;
+    if constexpr (GPR > 1) {
+        *reinterpret_cast<v4f*>(&so[grp][e]) = sum;
+        if (e == 0) { sm[grp] = M; sl[grp] = L; }
+        __syncthreads();
+        if (grp) return;
 #pragma unroll
-    for (int i = 1; i < NG; ++i) {
-        const v4f x = *reinterpret_cast<const v4f*>(&so[i][e]);
-        L += sl[i];
+        for (int i = 1; i < GPR; ++i) M = fmaxf(M, sm[i]);
+        sum = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        L = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sum[t] += x[t];
+        for (int i = 0; i < GPR; ++i) {
+            const v4f x = *reinterpret_cast<const v4f*>(&so[i][e]);
+            const float l = sl[i];
+            if (l == 0.0f) continue;
+            const float f = __builtin_amdgcn_exp2f(sm[i] - (M > -INFINITY ? M : 0.0f));
+            L = fmaf(l, f, L);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = fmaf(x[t], f, sum[t]);
+        }
     }
     const float inv = M == INFINITY ? __builtin_nanf("") : (L == 0.0f ? 0.0f : 1.0f / L);
     const int bh = (int)(r / nrows), row = (int)(r - (int64_t)bh * nrows), s = a.by_group.div(row);
@@ -862,7 +878,9 @@ hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
     hero_status r = hero_launch_status();
     if (r != HERO_OK || a.splits == 1) return r;
     const int64_t rows = (int64_t)a.B * a.c.H * a.Sq * a.group;
-    hipLaunchKernelGGL((kv_attn_join_kernel<DH, DT>), dim3((unsigned)rows), dim3(256), 0, st, a);
+    constexpr int NG = 256 / (DH / 4);
+    if (a.splits <= 8) hipLaunchKernelGGL((kv_attn_join_kernel<DH, DT, 1>), dim3((unsigned)((rows + NG - 1) / NG)), block, 0, st, a);
+    else hipLaunchKernelGGL((kv_attn_join_kernel<DH, DT, NG>), dim3((unsigned)rows), block, 0, st, a);
     return hero_launch_status();
 }
 
