@@ -465,19 +465,20 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
     const uint32_t voff = (uint32_t)((vq & 3) * 4 * vstride + vch * 4);
     typedef int Ids[NI];
     const int32_t* const table = a.c.table + (int64_t)b * a.c.max_blocks;
-    auto look = [&](int t, Ids& raw) __attribute__((always_inline)) {
+    auto place = [&](int t, int i) __attribute__((always_inline)) { return min((t * 64 + i * (64 / NI)) >> a.c.log2_block, a.c.max_blocks - 1); };
+    auto look = [&](int t, Ids& raw) __attribute__((always_inline)) {    // (without a table nothing, not even a register, is touched: it could be waited for)
+        if (a.c.table)
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int at = min((t * 64 + i * (64 / NI)) >> a.c.log2_block, a.c.max_blocks - 1);
-            raw[i] = a.c.table ? (int)load1(uniform_base(table + at), 0, 0) : b * a.c.max_blocks + at;
-        }
+            for (int i = 0; i < NI; ++i) raw[i] = (int)load1(uniform_base(table + place(t, i)), 0, 0);
     };
-    auto settle = [&](const Ids& raw, Ids& id) __attribute__((always_inline)) {
+    auto settle = [&](int t, const Ids& raw, Ids& id) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int blk = __builtin_amdgcn_readfirstlane(raw[i]);
-            id[i] = (unsigned)blk < (unsigned)a.c.n_blocks ? blk : -1;
-        }
+        for (int i = 0; i < NI; ++i) id[i] = b * a.c.max_blocks + place(t, i);
+        if (a.c.table)
+#pragma unroll
+            for (int i = 0; i < NI; ++i) id[i] = __builtin_amdgcn_readfirstlane(raw[i]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) id[i] = (unsigned)id[i] < (unsigned)a.c.n_blocks ? id[i] : -1;
     };
     const uint8_t* const khead = a.c.k.codes + (int64_t)h * a.c.k.s_head;
     const uint8_t* const vhead = a.c.v.codes + (int64_t)h * a.c.v.s_head;
@@ -647,9 +648,20 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
         return acc;
     };
 
-    // ---- the first tile, whose codes are asked for before the queries
-    Ids raw, id, id1, id2;                                               // blocks of tile t + 3 as they come, of t, t + 1, t + 2
+    // ---- the first tile.  (The blocks are looked up and the scales asked for in front of the codes here as in the loop: what waits for them there
+    // is not to wait for codes.)
+    Ids raw = {}, id, id1, id2;                                               // blocks of tile t + 3 as they come, of t, t + 1, t + 2
     v4i qraw[DS];
+    if (t0 < t1) {
+        Ids raw1 = {}, raw2 = {};
+        look(t0, raw1);
+        look(min(t0 + 1, te), raw2);
+        look(min(t0 + 2, te), raw);
+        settle(t0, raw1, id1);
+        settle(min(t0 + 1, te), raw2, id2);
+        scales(id1);
+        fetch(t0, id1);
+    }
     {
         const int rr = min(row, nrows - 1), s = a.by_group.div(rr);
         const uint16_t* const qp = a.q + (int64_t)b * a.qs[0] + (int64_t)s * a.qs[1] + (int64_t)(h * a.group + rr - s * a.group) * a.qs[2] + hh * 8;
@@ -657,27 +669,18 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
         for (int t = 0; t < DS; ++t) qraw[t] = *reinterpret_cast<const v4i*>(qp + t * 16);
     }
     if (t0 < t1) {
-        look(t0, raw);
-        settle(raw, id1);
-        fetch(t0, id1);
-        scales(id1);
-        look(min(t0 + 1, te), raw);
-    }
-    rc = queries<DT, DS, 32>(qraw, a.scale, qf);
-    if (t0 < t1) {
-        settle(raw, id2);
         blank();
         stage(t0 % NB);
         fetch(min(t0 + 1, te), id2);
-        look(min(t0 + 2, te), raw);
     }
+    rc = queries<DT, DS, 32>(qraw, a.scale, qf);
     __syncthreads();
     v16f acc = {}, next;
     if (t0 < wt) acc = scores(t0 % NB, 0);
     auto next_ids = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) { id[i] = id1[i]; id1[i] = id2[i]; }
-        settle(raw, id2);
+        settle(min(t + 2, te), raw, id2);
         look(min(t + 3, te), raw);
     };
     // (behind the last tile the last one is fetched and staged again, and scores are made that nobody takes: no branch in the middle)
@@ -687,6 +690,7 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
         Group gr[2][GH];
         next_ids(t);
         groups(id, gr);
+        scales(id1);                             // (in front of the codes of this iteration, whose arrival the next one's start does not wait for)
         bool edge = t * 64 + 64 > wall;
 #pragma unroll
         for (int i = 0; i < NI; ++i) edge |= id[i] < 0;
@@ -696,7 +700,6 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
         weigh(acc);
         stage(after);
         fetch(min(t + 2, te), id2);
-        scales(id1);
         step_order<DS + 2 * CT>();
         raise(acc);
         settled(gr[0]);
@@ -717,7 +720,6 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
         blank();
         stage((t + 1) % NB);
         fetch(min(t + 2, te), id2);
-        scales(id1);
         meet();
     }
 
