@@ -479,7 +479,8 @@ hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, const int64_t 
  *        (HERO_MASK_PADDING -> HERO_ERR_UNSUPPORTED: new_len says it.)  A query that sees no key, i >= n among them, outputs 0.
  * The scores, the softmax and all sums are fp32; the probabilities (times the V scale of their block) are rounded to FP16 for
  * the second product whatever dt is, behind a shift that keeps them normal numbers down to 2^-29 of the row's largest; BF16
- * queries go through FP16 as well, each row times a power of two (exact down to 2^-29 of the row's largest).
+ * queries go through FP16 as well, each row times a power of two (exact down to 2^-29 of the row's largest).  (A block whose
+ * V scale is more than 2^100 times smaller than another's that the row sees may be taken for one that it does not see.)
  * Few rows (Sq * Hq / H) over many keys are split along the keys when `workspace` has room: hero_kv_attn_workspace_bytes(cache,
  * Hq, Sq) bytes (0: this size is not split), device memory, 256-byte aligned (else HERO_ERR_WORKSPACE).  NULL or smaller: one piece (slower, and
  * fp32 sums are ordered otherwise).  Pure scratch, nothing is kept between calls: calls that may overlap on the GPU need

@@ -86,6 +86,7 @@ SYMBOLS = {
     "hero_kv_read": (i32, [C.POINTER(KvCache), vp, vp, vp, vp, i32, i64, vp, vp, vp]),
     "hero_kv_attn_workspace_bytes": (C.c_size_t, [C.POINTER(KvCache), i64, i64]),
     "hero_kv_attn": (i32, [C.POINTER(KvCache), vp, vp, i32, i64, i64, f32, i32, vp, vp, vp, i64, vp, C.c_size_t, vp]),
+    "hero_kv_attn_tile": (i32, [C.POINTER(KvCache), vp, vp, i32, i64, i64, f32, i32, vp, vp, vp, i64, vp, C.c_size_t, vp, i32]),
     "hero_layer_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDesc), i64, i64]),
     "hero_layer_fwd": (i32, [C.POINTER(LayerDesc), C.POINTER(LayerWeights), C.POINTER(LayerIO), vp, C.c_size_t, vp]),
     "hero_layer_kv_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDesc), C.POINTER(KvCache), i64]),
@@ -433,18 +434,19 @@ class Hero:
     def hero_kv_attn_workspace_bytes(self, cache, Hq, Sq) -> int:
         return int(self.lib.hero_kv_attn_workspace_bytes(cache, Hq, Sq))
 
-    def hero_kv_attn(self, cache, q, scale, mask, kv_len, new_len=None, out=None, workspace=None, stream=None):
+    def hero_kv_attn(self, cache, q, scale, mask, kv_len, new_len=None, out=None, workspace=None, stream=None, tile=None):
         """q [B,Sq,Hq,Dh] bf16 / f16 over the cache.  Returns [B*Sq, Hq*Dh] in q's type.  workspace: optional uint8 tensor
-        (hero_kv_attn_workspace_bytes), without which few rows over many keys are not split."""
+        (hero_kv_attn_workspace_bytes), without which few rows over many keys are not split; tile=<rows> -> the test hook
+        hero_kv_attn_tile (include/hero_debug.h: the kernel forced)."""
         B, Sq, Hq, Dh = q.shape
         if out is None:
             out = torch.empty((B * Sq, Hq * Dh), dtype=q.dtype, device=q.device)
         else:
             assert out.dtype is q.dtype and out.shape == (B * Sq, Hq * Dh) and out.stride(1) == 1
-        self._check(self.lib.hero_kv_attn(cache, q.data_ptr(), _kv_rows(cache, q, Sq, Hq), _DT[q.dtype], Hq, Sq, scale, int(mask),
-                                          _kv_length(cache, kv_len), _kv_length(cache, new_len), out.data_ptr(), out.stride(0),
-                                          None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
-                                          _kv_stream(cache, stream)))
+        args = (cache, q.data_ptr(), _kv_rows(cache, q, Sq, Hq), _DT[q.dtype], Hq, Sq, float(scale), int(mask),
+                _kv_length(cache, kv_len), _kv_length(cache, new_len), out.data_ptr(), out.stride(0),
+                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _kv_stream(cache, stream))
+        self._check(self.lib.hero_kv_attn(*args) if tile is None else self.lib.hero_kv_attn_tile(*args, int(tile)))
         return out
 
     # ------------------------------------------------------------------ layer

@@ -838,10 +838,12 @@ __global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, i
 // How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 256 to one of that of many (rt = 0); the keys into pieces.
 struct Plan { int rt, tiles, splits; };
 
-Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq) {
+// forced: 0, or the rows of a tile (16, 32, 256)
+Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq, int forced) {
     Plan p;
     const int64_t rows = Sq * (Hq / c->H), bh = c->B * c->H, keys = c->max_blocks * c->block, steps = (keys + 31) / 32;
     p.rt = rows <= 16 ? 1 : rows > 64 && (double)rows * bh * keys * c->Dh >= 1.5e9 ? 0 : 2;
+    if (forced) p.rt = forced == 256 ? 0 : forced / 16;
     const int64_t tile = p.rt ? 16 * p.rt : 256;
     p.tiles = (int)((rows + tile - 1) / tile);
     const int64_t units = bh * p.tiles;
@@ -890,14 +892,21 @@ hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
 
 extern "C" size_t hero_kv_attn_workspace_bytes(const hero_kv_cache* cache, int64_t Hq, int64_t Sq) {
     if (kv_check(cache) != HERO_OK || check_sizes(cache, Hq, Sq) != HERO_OK || cache->B == 0 || Hq == 0 || Sq == 0) return 0;
-    return part_bytes(cache, Hq, Sq, plan(cache, Hq, Sq).splits);
+    return part_bytes(cache, Hq, Sq, plan(cache, Hq, Sq, 0).splits);
 }
 
 extern "C" hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, const int64_t q_strides[4], hero_dtype dt,
                                     int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,
                                     void* out, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream) {
+    return hero_kv_attn_tile(cache, q, q_strides, dt, Hq, Sq, scale, mask, kv_len, new_len, out, ldo, workspace, workspace_bytes, stream, 0);
+}
+
+extern "C" hero_status hero_kv_attn_tile(const hero_kv_cache* cache, const void* q, const int64_t q_strides[4], hero_dtype dt,
+                                         int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,
+                                         void* out, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream, int forced) {
     hero_status r = kv_check(cache);
     if (r != HERO_OK) return r;
+    if (forced != 0 && forced != 16 && forced != 32 && forced != 256) return HERO_ERR_UNSUPPORTED;
     if (dt != HERO_BF16 && dt != HERO_F16) return HERO_ERR_UNSUPPORTED;
     if (mask != HERO_MASK_NONE && mask != HERO_MASK_CAUSAL) return HERO_ERR_UNSUPPORTED;
     if ((r = check_sizes(cache, Hq, Sq)) != HERO_OK) return r;
@@ -915,7 +924,7 @@ extern "C" hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, c
         hipLaunchKernelGGL(kv_attn_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (uint16_t*)out, cache->B * Sq, Hq * Dh, ldo);
         return hero_launch_status();
     }
-    Plan p = plan(cache, Hq, Sq);
+    Plan p = plan(cache, Hq, Sq, forced);
     if (!workspace || workspace_bytes < part_bytes(cache, Hq, Sq, p.splits)) p.splits = 1;
     const int64_t nb = (cache->B * cache->H + 7) / 8 * 8 * p.tiles * p.splits;
     if (nb > 0x7fffffffLL || cache->B * Sq * Hq > 0x7fffffffLL) return HERO_ERR_SHAPE;

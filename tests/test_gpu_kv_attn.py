@@ -14,10 +14,14 @@ def _dev(a):
     return None if a is None else torch.tensor(a, dtype=torch.int32, device="cuda")
 
 
+TILES = [None, 16, 32, 256]                                               # the library's choice of a kernel, and each kernel
+
+
 def _attend(p, q, scale, mask, lens, new=None, workspace=True, **kw):
     ws = None
     if workspace:
-        ws = torch.empty(p.hero.hero_kv_attn_workspace_bytes(p.cache, q.shape[2], q.shape[1]), dtype=torch.uint8, device="cuda")
+        n = p.hero.hero_kv_attn_workspace_bytes(p.cache, q.shape[2], q.shape[1]) if kw.get("tile") is None else 64 << 20
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     return p.hero.hero_kv_attn(p.cache, q, scale, mask, _dev(lens), new_len=_dev(new), workspace=ws, **kw)
 
 
@@ -81,6 +85,22 @@ def test_several_tokens(hero, S, H, group, Dh, mask, fmt, hp):
     q = _rows(13, len(lens), S, H * group, Dh, HP[hp], spread=False)
     _check(p, q, Dh ** -0.5, mask, lens, new)
     _check(p, q, Dh ** -0.5, mask, lens)
+    for tile in TILES[1:]:
+        _check(p, q, Dh ** -0.5, mask, lens, new, tile=tile)
+
+
+@pytest.mark.parametrize("hp", ["bf16", "f16"])
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("Dh,block,layout", [(64, 16, "tokens"), (128, 64, "heads"), (128, 16, "fused"), (64, 128, "heads"), (64, 64, "fused"), (128, 32, "tokens"), (128, 128, "heads")])
+@pytest.mark.parametrize("S,group", [(1, 1), (20, 4), (300, 1)])
+def test_every_kernel_on_every_layout(hero, S, group, Dh, block, layout, fmt, hp):
+    H, lens = 2, [S, S + 1, S + 63, S + 129]
+    p = _filled(hero, fmt, len(lens), H, Dh, block, -(-(S + 129) // block), paged=True, layout=layout)
+    _fill(p, lens, S + Dh, HP[hp])
+    q = _rows(14, len(lens), S, H * group, Dh, HP[hp], spread=False)
+    for tile in TILES[1:]:
+        for mask in (HB.MASK_NONE, HB.MASK_CAUSAL):
+            _check(p, q, Dh ** -0.5, mask, lens, tile=tile)
 
 
 @pytest.mark.parametrize("fmt", ["i8", "e4m3"])
@@ -97,6 +117,9 @@ def test_keys_in_pieces(hero, S, group, B, fmt):
     assert torch.equal(one, two)                                          # the order of the sums is fixed
     _check(p, q, Dh ** -0.5, HB.MASK_CAUSAL, lens, got=one)
     _check(p, q, Dh ** -0.5, HB.MASK_CAUSAL, lens, workspace=False)
+    for tile in TILES[1:]:
+        _check(p, q, Dh ** -0.5, HB.MASK_CAUSAL, lens, tile=tile)
+        _check(p, q, Dh ** -0.5, HB.MASK_CAUSAL, lens, tile=tile, workspace=False)
 
 
 @pytest.mark.parametrize("S", [1, 40, 140])
@@ -112,7 +135,8 @@ def test_scales_and_sizes_of_queries(hero, hp, scale, S):
     size = [1e-38, 1e-20, 0.0, 1.0, 300.0, 1e-4, 1.0, 7.0] if hp == "bf16" else [6e-8, 1e-5, 0.0, 1.0, 300.0, 1e-4, 1.0, 7.0]
     q = q * torch.tensor(size, device="cuda")[:, None]
     q[:, :, 6, 3] = 3e4
-    _check(p, q.to(HP[hp]), scale if scale != 0.7 else 0.7 / 300, HB.MASK_CAUSAL, lens)
+    for tile in TILES:
+        _check(p, q.to(HP[hp]), scale if scale != 0.7 else 0.7 / 300, HB.MASK_CAUSAL, lens, tile=tile)
 
 
 @pytest.mark.parametrize("S", [1, 20, 140])
@@ -132,7 +156,8 @@ def test_blocks_of_very_different_size(hero, fmt, S):
     k[2, 77, :, 0], q[2, :, :, 0] = 16, 8                                 # e^16 times as likely as each of the others
     v[2, 77] = 0
     p.write(k, v, [L] * 3)
-    _check(p, q, Dh ** -0.5, HB.MASK_NONE, [L] * 3)
+    for tile in TILES:
+        _check(p, q, Dh ** -0.5, HB.MASK_NONE, [L] * 3, tile=tile)
 
 
 @pytest.mark.parametrize("S,group", [(1, 1), (4, 4), (64, 3)])
@@ -144,7 +169,8 @@ def test_an_index_that_is_no_block(hero, S, group):
     _fill(p, lens, 51, torch.float16)
     p.table[0, 1], p.table[1, 0], p.table[1, 6], p.table[2, 4], p.table[3] = -1, 10 ** 9, -7, p.codes["k"].shape[0], -1
     p.dev_table.copy_(torch.from_numpy(p.table))
-    _check(p, _rows(52, 4, S, H * group, Dh, torch.float16, spread=False), 0.1, HB.MASK_CAUSAL, lens)
+    for tile in TILES:
+        _check(p, _rows(52, 4, S, H * group, Dh, torch.float16, spread=False), 0.1, HB.MASK_CAUSAL, lens, tile=tile)
 
 
 @pytest.mark.parametrize("S,group", [(1, 1), (20, 1), (40, 4), (140, 2)])
@@ -158,17 +184,56 @@ def test_a_scale_that_is_no_number_reaches_who_sees_it(hero, S, group):
     k[0, at, 1, 5], v[1, at, 2, 7] = float("nan"), float("inf")
     p.write(k, v, lens)
     q = _rows(63, 2, S, H * group, Dh, torch.bfloat16, spread=False)
-    y = _attend(p, q, 0.1, HB.MASK_CAUSAL, lens).view(2, S, H, group, Dh)
+    ys = [_attend(p, q, 0.1, HB.MASK_CAUSAL, lens, tile=tile).view(2, S, H, group, Dh) for tile in TILES]
     first = at // block * block - 60                                      # the first row that sees the block
     want = torch.zeros((2, S, H, group, Dh), dtype=torch.bool, device="cuda")
     want[0, max(first, 0):, 1], want[1, max(first, 0):, 2] = True, True
-    assert torch.equal(torch.isnan(y), want)
-    clean = torch.where(want, torch.zeros((), device="cuda", dtype=y.dtype), y)
     for x in "kv":                                                        # the same without the blocks that are NaN
         p.scale[x] = np.nan_to_num(p.scale[x], nan=1.0)
         p.dev_scale[x].copy_(torch.from_numpy(p.scale[x]))
-    z = torch.where(want, torch.zeros((), device="cuda", dtype=y.dtype), _attend(p, q, 0.1, HB.MASK_CAUSAL, lens).view_as(y))
-    assert torch.equal(clean, z)
+    for tile, y in zip(TILES, ys):
+        assert torch.equal(torch.isnan(y), want)
+        z = _attend(p, q, 0.1, HB.MASK_CAUSAL, lens, tile=tile).view_as(y)
+        assert torch.equal(y[~want], z[~want])
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("hp", ["bf16", "f16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_no_number_stays_in_its_row(hero, bad, hp, tile):
+    H, group, Dh, S = 2, 2, 64, 50
+    p = _filled(hero, "e4m3", 2, H, Dh, 16, 8)
+    _fill(p, [120, 77], 91, HP[hp])
+    q = _rows(92, 2, S, H * group, Dh, HP[hp], spread=False)
+    y = _attend(p, q, 0.1, HB.MASK_CAUSAL, [120, 77], tile=tile).view(2, S, H * group, Dh)
+    q[1, 17, 3, 5] = bad
+    z = _attend(p, q, 0.1, HB.MASK_CAUSAL, [120, 77], tile=tile).view_as(y)
+    rest = torch.ones((2, S, H * group), dtype=torch.bool, device="cuda")
+    rest[1, 17, 3] = False
+    assert bool(torch.isnan(z[1, 17, 3]).all()) and torch.equal(z[rest], y[rest])
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_scores_that_rise_and_a_score_beyond_fp32(hero, tile):
+    """The maximum rises in every step of keys, by little, by more than FP16 holds, from far below; and a row whose score fp32 does not
+    hold is NaN, not zeros."""
+    H, Dh, S, L = 1, 64, 40, 320
+    p = _filled(hero, "i8", 4, H, Dh, 16, L // 16)
+    k, v, q = (torch.zeros((4, n, H, Dh), device="cuda") for n in (L, L, S))
+    v[:] = _rows(95, 4, L, H, Dh, torch.float32, spread=False)
+    at = torch.arange(L, device="cuda").float()
+    k[0, :, 0, 0], k[1, :, 0, 0], k[2, :, 0, 0] = at / 10, at * 2, at / 4 - 400
+    k[3, :, 0, 0] = 1e30
+    q[:, :, 0, 0] = 1.0
+    q[3, 17, 0, 0] = 1e10
+    for x in (k, v):
+        x.copy_(x.to(torch.bfloat16))
+    p.write(k.to(torch.bfloat16), v.to(torch.bfloat16), [L] * 4)
+    y = _attend(p, q.to(torch.bfloat16), 1.0, HB.MASK_NONE, [L] * 4, tile=tile).view(4, S, Dh)
+    assert bool(torch.isnan(y[3, 17]).all()) and not bool(torch.isnan(y[:3]).any())
+    three = Pool(hero, "i8", 3, H, Dh, 16, L // 16, fill=0x7f)
+    three.write(k[:3].to(torch.bfloat16), v[:3].to(torch.bfloat16), [L] * 3)
+    _check(three, q[:3].to(torch.bfloat16), 1.0, HB.MASK_NONE, [L] * 3, tile=tile)
 
 
 @pytest.mark.parametrize("S", [1, 40, 140])
@@ -179,10 +244,11 @@ def test_strides_and_rows_of_the_output(hero, S):
     _fill(p, lens, 71, torch.bfloat16)
     buf = _rows(72, 2, S, H * group * 3 + 1, Dh, torch.bfloat16, spread=False)
     q = buf[:, :, 1:1 + H * group]
-    out = torch.full((2 * S, H * group * Dh + 12), 7.0, dtype=torch.bfloat16, device="cuda")
-    _attend(p, q, 0.125, HB.MASK_CAUSAL, lens, out=out[:, :H * group * Dh])
-    assert bool((out[:, H * group * Dh:] == 7.0).all())
-    _check(p, q, 0.125, HB.MASK_CAUSAL, lens, got=out[:, :H * group * Dh].contiguous())
+    for tile in TILES:
+        out = torch.full((2 * S, H * group * Dh + 12), 7.0, dtype=torch.bfloat16, device="cuda")
+        _attend(p, q, 0.125, HB.MASK_CAUSAL, lens, out=out[:, :H * group * Dh], tile=tile)
+        assert bool((out[:, H * group * Dh:] == 7.0).all())
+        _check(p, q, 0.125, HB.MASK_CAUSAL, lens, got=out[:, :H * group * Dh].contiguous())
 
 
 def test_a_cache_without_blocks(hero):

@@ -88,6 +88,10 @@ def test_attention_that_is_refused(lib, kw, status):
     assert _attn(lib, _cache(), **kw) == status
 
 
+def test_a_kernel_that_is_not_there(lib):
+    assert lib.hero_kv_attn_tile(_cache(), P, ST, HB.BF16, 2, 4, 0.125, HB.MASK_CAUSAL, P, None, P, 128, None, 0, None, 64) == UNSUPPORTED
+
+
 def test_nothing_to_do(lib):
     for kw in (dict(B=0), dict(H=0)):
         c = _cache(k=None, v=None, k_scale=None, v_scale=None, **kw)
