@@ -140,6 +140,10 @@ __device__ __forceinline__ int keys_seen(const AttnArgs& a, int row, int len, in
 // Few rows: a wave owns 16 RT rows and 32 keys at a time, its K and V fragments straight from memory into registers (K: a lane's 16
 // channels of its key; V: a lane's 8 (4) channels of 8 keys, paired up by byte permutes), and an online softmax of its own; the NW waves of
 // a workgroup split the keys of its piece and meet in LDS.
+// Bound by HBM: each code is read once for all rows that share its head (the matrix instructions work on 16 rows whether there are 1 or 16, 8 %
+// of the time at that).  K's next codes are asked for behind the first product and V's behind the second, which leaves registers for
+// four waves per SIMD.  4 x 8 heads x 4 rows over 131072 E4M3 keys: 1.03 GB in 174-179 us, 5.8-5.9 TB/s (a read-only stream 6.15); 64 x 32 heads x 1 row
+// over 1100 .. 2048 INT8 keys, 0.82 GB: 150 us, 5.5 TB/s; 16 x 8 heads x 20 rows over 3000 .. 4096: 26.6 us, 4.4 TB/s.
 // ------------------------------------------------------------------------------------------
 template <int DH, int FMT, int DT, int RT, int NW>
 __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
@@ -400,6 +404,12 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 // exponentials taken again.
 // K's rows are 16 bytes longer than they need to be, V's 16-byte pieces XOR-swizzled by their row: fragment reads (turns of lanes 0-3, 12-15,
 // 20-27 and so on) meet no bank conflict.
+// 8 x 32 heads x 256 rows behind 2304 E4M3 keys 90-92 us (800-817 TFLOP/s; a library product of 8192^3 runs at 1250), 4 x 32 x 2048 causal INT8 182 us
+// (755).  In clocks per tile and CU, of 3793 (2048 of matrix instructions): without fragment reads 2783, without staging and loads 2877, without
+// exponentials 3528, without any of them 2335; but the clock the power limit allows falls with what is left (1.94 GHz -> 1.73), so that orders of
+// instructions, priorities, 32 vector instructions fewer and loads that nothing waits for changed a launch by 2 % or not at all.  64 rows to a wave halve the
+// reads, but leave one wave per SIMD and too few registers: 150 us.  Beside the loop a workgroup takes 7 us (arguments, lengths, first tile, result); two
+// row tiles to a workgroup cost the loop more (8 %) than they saved.
 // ------------------------------------------------------------------------------------------
 constexpr float HEADROOM = 8.0f;                             // what a maximum's own P is 2 to the power of
 constexpr float MOST_P = 32768.0f;
@@ -836,6 +846,10 @@ __global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, i
 }
 
 // How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 256 to one of that of many (rt = 0); the keys into pieces.
+// The kernel of many rows reads K and V once per 256 rows instead of 32, and takes longer to begin and end.  us, few / many: 36 rows of 512 heads over 2048 keys of
+// 128 values 90 / 120, 64 of 8 over 65536 50 / 63, 80 of 512 over 1000 75 / 67, 128 of 8 over 2048 (0.3 G multiply-adds) 18 / 20, 256 of 8 over 2048 (0.5) 19 / 27, 160 of 8 over
+// 4000 (0.7) 25 / 26, 200 of 128 heads of 64 over 600 (1.0) 21 / 24, 512 of 96 heads of 64 over 512 (1.6) 26 / 22, 128 of 32 over 4096 (2.1) 34 / 31,
+// 1024 of 32 over 1024 causal (4.3) 49 / 59, 512 of 8 over 8192 (4.3) 45 / 40, 160 of 128 over 4000 (10) 126 / 93, 2048 of 32 over 2048 causal (17) 137 / 76.
 struct Plan { int rt, tiles, splits; };
 
 // forced: 0, or the rows of a tile (16, 32, 256)
