@@ -483,7 +483,7 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
     };
     auto settle = [&](int t, const Ids& raw, Ids& id) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) id[i] = b * a.c.max_blocks + place(t, i);
+        for (int i = 0; i < NI; ++i) id[i] = (int)((uint32_t)b * (uint32_t)a.c.max_blocks + (uint32_t)place(t, i));
         if (a.c.table)
 #pragma unroll
             for (int i = 0; i < NI; ++i) id[i] = __builtin_amdgcn_readfirstlane(raw[i]);
