@@ -48,7 +48,7 @@ hero_status hero_hp_gemm_tile(const void* A, int64_t lda, const void* Wt, int64_
 int hero_gemm_kernel(hero_dtype dt, hero_epilogue epi, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldb);
 
 /* hero_kv_attn with the kernel forced: `tile` rows (queries of the heads that share a head of the cache) to a tile, 16 or 32 the kernel of
- * few rows, 256 that of many, 0 the library's own choice; else HERO_ERR_UNSUPPORTED.  The keys are split as the library would with such
+ * few rows, 256 that of many (heads of 64: 128 rows), 0 the library's own choice; else HERO_ERR_UNSUPPORTED.  The keys are split as the library would with such
  * tiles, where `workspace` has room for it. */
 hero_status hero_kv_attn_tile(const hero_kv_cache* cache, const void* q, const int64_t q_strides[4], hero_dtype dt,
                               int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,

@@ -394,7 +394,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Many rows: a workgroup of eight waves owns 256 rows, a wave 32 of them; K and V of 64 keys at a time are made FP16 once, on their way
+// Many rows: a workgroup of eight waves owns 256 rows (heads of 64: of four, 128), a wave 32 of them; K and V of 64 keys at a time are made FP16 once, on their way
 // into LDS (K by rows, V by channels), three tiles deep, so that one barrier per tile is enough: a tile is written while the one before it is
 // worked on.  Scores are computed transposed (S^T = K Q^T): a lane owns query lane % 32, and the exponentials are the second product's operand
 // as they stand.  A step makes the scores of 32 keys, takes the exponentials of the 32 before them and multiplies V by those of the 32 before
@@ -427,13 +427,18 @@ __device__ __forceinline__ void step_order() {
     }
 }
 
+// A thread stages one unit of K and one of V per tile of 64 keys, which for heads of 64 gives work to 256 threads; three such workgroups fit a CU.  us against eight
+// waves whose halves stage the same: 4 x 32 heads of 64 x 2048 rows causal INT8 136 -> 105, 8 x 12 x 512 causal 20.1 -> 16.9, 16 x 12 x 128 over 1024 34.0 -> 26.9.
+constexpr int tile_waves(int Dh) { return Dh == 64 ? 4 : 8; }
+
 template <int DH, int FMT, int DT, int NI>                   // NI: blocks that a tile's 64 keys lie in
-__global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
-    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2 + 16, NB = 3, ROWS = 256;
+__global__ __launch_bounds__(64 * tile_waves(DH), DH == 64 ? 3 : 2) void kv_attn_tile_kernel(AttnArgs a) {
+    constexpr int NW = tile_waves(DH), ROWS = 32 * NW;
+    constexpr int DS = DH / 16, CT = DH / 32, KROW = DH * 2 + 16, NB = 3;
     constexpr int GH = NI == 4 ? 2 : 1, GE = 16 / GH;        // groups of keys with scales of their own in 32 keys
     constexpr int OROW = DH * 2 + 16;                        // a row of the result on its way out
     __shared__ __attribute__((aligned(1024))) uint8_t pool[NB * (64 * KROW + DH * 128)];
-    static_assert(8 * 32 * OROW <= sizeof(pool), "every wave's rows of the result fit");
+    static_assert(NW * 32 * OROW <= sizeof(pool), "every wave's rows of the result fit");
     uint8_t (* const sK)[64 * KROW] = reinterpret_cast<uint8_t (*)[64 * KROW]>(pool);
     uint8_t (* const sV)[DH * 128] = reinterpret_cast<uint8_t (*)[DH * 128]>(pool + NB * 64 * KROW);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, ql = lane & 31;
@@ -461,15 +466,15 @@ __global__ __launch_bounds__(512) void kv_attn_tile_kernel(AttnArgs a) {
     const int total = (last + 63) / 64, per = (total + a.splits - 1) / a.splits;
     const int t0 = min(split * per, total), t1 = min(t0 + per, total), wt = min(t1, (wlast + 63) / 64), te = t1 - 1;
 
-    // ---- staging.  K: a thread's unit is 16 codes of a key; V: 4 channels of 4 keys.  (Dh = 64: half of the threads do the other half's again.)
+    // ---- staging.  K: a thread's unit is 16 codes of a key; V: 4 channels of 4 keys.
     v4i kr;
     uint32_t vr[4];
     int vend;                                                            // how many keys there are from V's unit's first on
-    const int kch = tid % (DH / 16), krow = tid / (DH / 16) % 64;
-    const int vch = tid % (DH / 4), vq = tid / (DH / 4) % 16;
+    const int kch = tid % (DH / 16), krow = tid / (DH / 16);
+    const int vch = tid % (DH / 4), vq = tid / (DH / 4);
     // A wave's units all lie in one group of 16 keys; a tile's keys in NI blocks (the same one, of 64 tokens or more).  The table is read three
     // tiles ahead, the codes two, the scales one; as vector loads, since a scalar load's wait would be one for all LDS reads too.
-    const int group16 = DH == 128 ? wave >> 1 : wave & 3;
+    const int group16 = wave * 4 / NW;
     const int kstride = (int)a.c.k.s_row, vstride = (int)a.c.v.s_row;    // (a block's rows span less than 2^31 elements)
     const uint32_t koff = (uint32_t)((krow & 15) * kstride + kch * 16);
     const uint32_t voff = (uint32_t)((vq & 3) * 4 * vstride + vch * 4);
@@ -845,25 +850,27 @@ __global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, i
     if (i < rows * cols) out[(i / cols) * ld + i % cols] = 0;
 }
 
-// How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 256 to one of that of many (rt = 0); the keys into pieces.
-// The kernel of many rows reads K and V once per 256 rows instead of 32, and takes longer to begin and end.  us, few / many: 36 rows of 512 heads over 2048 keys of
+// How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 256 (heads of 64: 128) to one of that of many (rt = 0); the keys into pieces.
+// The kernel of many rows reads K and V once per such tile, and takes longer to begin and end.  us, few / many: 36 rows of 512 heads over 2048 keys of
 // 128 values 90 / 120, 64 of 8 over 65536 50 / 63, 80 of 512 over 1000 75 / 67, 128 of 8 over 2048 (0.3 G multiply-adds) 18 / 20, 256 of 8 over 2048 (0.5) 19 / 27, 160 of 8 over
-// 4000 (0.7) 25 / 26, 200 of 128 heads of 64 over 600 (1.0) 21 / 24, 512 of 96 heads of 64 over 512 (1.6) 26 / 22, 128 of 32 over 4096 (2.1) 34 / 31,
+// 4000 (0.7) 25 / 26, 200 of 128 heads of 64 over 600 (1.0) 20 / 20, 128 of 128 heads of 64 over 1000 (1.0) 18 / 22,
+// 100 of 48 heads of 64 over 4096 (1.3) 32 / 26, 512 of 96 heads of 64 over 512 (1.6) 24 / 17, 300 of 24 heads of 64 over 4096 (1.9) 30 / 32, 128 of 32 over 4096 (2.1) 34 / 31,
 // 1024 of 32 over 1024 causal (4.3) 49 / 59, 512 of 8 over 8192 (4.3) 45 / 40, 160 of 128 over 4000 (10) 126 / 93, 2048 of 32 over 2048 causal (17) 137 / 76.
 struct Plan { int rt, tiles, splits; };
 
-// forced: 0, or the rows of a tile (16, 32, 256)
+// forced: 0, or the rows of a tile (16, 32, 256 for the kernel of many rows)
 Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq, int forced) {
     Plan p;
     const int64_t rows = Sq * (Hq / c->H), bh = c->B * c->H, keys = c->max_blocks * c->block, steps = (keys + 31) / 32;
     p.rt = rows <= 16 ? 1 : rows > 64 && (double)rows * bh * keys * c->Dh >= 1.5e9 ? 0 : 2;
     if (forced) p.rt = forced == 256 ? 0 : forced / 16;
-    const int64_t tile = p.rt ? 16 * p.rt : 256;
+    const int64_t tile = p.rt ? 16 * p.rt : 32 * tile_waves(c->Dh);
     p.tiles = (int)((rows + tile - 1) / tile);
     const int64_t units = bh * p.tiles;
-    // Pieces of 16 steps or more while there are fewer than two workgroups per CU (one, of many rows).  us, towards 256 / 512 / 1024 workgroups:
-    // 4 x 8 heads x 4 rows over 131072 keys 192 / 179 / 184, 16 x 8 heads x 20 rows over 4096 keys (its write with it) 49 / 41 / 46.
-    int64_t s = ((p.rt ? 512 : 256) + units - 1) / units;
+    // Pieces of 16 steps or more while there are fewer than two workgroups per CU (one, of many rows of heads of 128).  us, towards 256 / 512 / 1024 workgroups:
+    // 4 x 8 heads x 4 rows over 131072 keys 192 / 179 / 184, 16 x 8 heads x 20 rows over 4096 keys (its write with it) 49 / 41 / 46.  Many rows of heads of 64,
+    // towards 256 / 512 / 768: 4 x 8 x 512 rows over 8192 keys 79 / 61 / 61.
+    int64_t s = ((p.rt == 0 && c->Dh == 128 ? 256 : 512) + units - 1) / units;
     s = s < steps / 16 ? s : steps / 16;
     p.splits = (int)(s < 1 ? 1 : s > MOST_PIECES ? MOST_PIECES : s);
     return p;
@@ -885,9 +892,9 @@ hero_status launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
     const dim3 block(256);
     if (p.rt == 0) {
         const dim3 grid((unsigned)(((int64_t)a.B * a.c.H + 7) / 8 * 8 * a.tiles * a.splits));
-        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 4>), grid, dim3(512), 0, st, a);
-        else if (a.c.log2_block == 5) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 2>), grid, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 1>), grid, dim3(512), 0, st, a);
+        if (a.c.log2_block == 4) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 4>), grid, dim3(64 * tile_waves(DH)), 0, st, a);
+        else if (a.c.log2_block == 5) hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 2>), grid, dim3(64 * tile_waves(DH)), 0, st, a);
+        else hipLaunchKernelGGL((kv_attn_tile_kernel<DH, FMT, DT, 1>), grid, dim3(64 * tile_waves(DH)), 0, st, a);
     } else {
         const dim3 grid((unsigned)((int64_t)a.B * a.c.H * a.tiles * a.splits));
         if (p.rt == 1) hipLaunchKernelGGL((kv_attn_rows_kernel<DH, FMT, DT, 1, 4>), grid, block, 0, st, a);
