@@ -463,7 +463,7 @@ hero_status hero_kv_write(const hero_kv_cache* cache, const void* k, const int64
  *   k_out, v_out  [B, S, H, Dh], base pointers and 4 element strides (batch, token, head, channel); channel stride 1, the others
  *                 multiples of 8.  Either may be NULL (only the other is read).
  *   start  int32 [B] (device) or NULL (0 for every sequence); kv_len int32 [B] (device), required.
- * S * H <= 2^31 - 256. */
+ * S * H <= 2^31 - 256 and S * H * Dh < 2^36 (else HERO_ERR_SHAPE). */
 hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, const int64_t k_strides[4],
                          void* v_out, const int64_t v_strides[4], hero_dtype out_dt, int64_t S,
                          const int32_t* start, const int32_t* kv_len, void* stream);
@@ -484,7 +484,8 @@ hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, const int64_t 
  * Few rows (Sq * Hq / H) over many keys are split along the keys when `workspace` has room: hero_kv_attn_workspace_bytes(cache,
  * Hq, Sq) bytes (0: this size is not split), device memory, 256-byte aligned (else HERO_ERR_WORKSPACE).  NULL or smaller: one piece (slower, and
  * fp32 sums are ordered otherwise).  Pure scratch, nothing is kept between calls: calls that may overlap on the GPU need
- * their own.  The order of the sums depends on the sizes alone, so results are reproducible. */
+ * their own.  The order of the sums depends on the sizes alone, so results are reproducible.
+ * B * Sq * Hq < 2^31, and workgroups (B * H for every 16 rows, where rows are that few) for less than 2^32 threads: else HERO_ERR_SHAPE. */
 size_t hero_kv_attn_workspace_bytes(const hero_kv_cache* cache, int64_t Hq, int64_t Sq);
 hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, const int64_t q_strides[4], hero_dtype dt,
                          int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,

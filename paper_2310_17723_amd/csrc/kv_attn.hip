@@ -10,6 +10,7 @@
 // multiplied by a power of two that takes their largest value to [2^14, 2^15), which keeps every bit of values down to 2^-29 of it.
 // Rows: the queries of all heads that share a head of the cache, row = token * group + head of the group.
 #include "kv_cache.h"
+#include <algorithm>
 
 namespace {
 
@@ -846,8 +847,9 @@ __global__ __launch_bounds__(256) void kv_attn_join_kernel(AttnArgs a) {
 }
 
 __global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < rows * cols) out[(i / cols) * ld + i % cols] = 0;
+    const int64_t step = (int64_t)gridDim.x * 1024;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < rows * cols; i += step)
+        *reinterpret_cast<v2i*>(out + (i / cols) * ld + i % cols) = v2i{0, 0};
 }
 
 // How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 256 (heads of 64: 128) to one of that of many (rt = 0); the keys into pieces.
@@ -940,15 +942,15 @@ extern "C" hero_status hero_kv_attn_tile(const hero_kv_cache* cache, const void*
     if (workspace && ((uintptr_t)workspace & 255)) return HERO_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     if (cache->n_blocks == 0 || cache->max_blocks == 0) {                // no key anywhere
-        const int64_t n = cache->B * Sq * Hq * Dh;
-        if ((n + 255) / 256 > 0x7fffffffLL) return HERO_ERR_SHAPE;
-        hipLaunchKernelGGL(kv_attn_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (uint16_t*)out, cache->B * Sq, Hq * Dh, ldo);
+        if (cache->B * Sq * Hq > 0x7fffffffLL) return HERO_ERR_SHAPE;
+        const int64_t groups = (cache->B * Sq * Hq * Dh + 1023) / 1024;
+        hipLaunchKernelGGL(kv_attn_zero_kernel, dim3((unsigned)std::min<int64_t>(groups, 8192)), dim3(256), 0, st, (uint16_t*)out, cache->B * Sq, Hq * Dh, ldo);
         return hero_launch_status();
     }
     Plan p = plan(cache, Hq, Sq, forced);
     if (!workspace || workspace_bytes < part_bytes(cache, Hq, Sq, p.splits)) p.splits = 1;
     const int64_t nb = (cache->B * cache->H + 7) / 8 * 8 * p.tiles * p.splits;
-    if (nb > 0x7fffffffLL || cache->B * Sq * Hq > 0x7fffffffLL) return HERO_ERR_SHAPE;
+    if (!kv_launchable(nb, p.rt ? 256 : 64 * tile_waves(Dh)) || cache->B * Sq * Hq > 0x7fffffffLL) return HERO_ERR_SHAPE;
     AttnArgs a;
     a.c = kv_view(cache);
     a.q = (const uint16_t*)q;

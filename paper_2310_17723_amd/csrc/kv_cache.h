@@ -65,6 +65,9 @@ static inline KvView kv_view(const hero_kv_cache* c) {
     return v;
 }
 
+// whether `groups` workgroups can be launched: HIP counts a dimension's threads in 32 bits
+static inline bool kv_launchable(int64_t groups, int threads) { return groups <= 0xffffffffLL / threads; }
+
 // strides of [B, S, heads, Dh] rows: unit channels, the others multiples of 8 elements
 static inline hero_status kv_check_rows(const void* p, const int64_t* s) {
     if (!p || !s) return HERO_ERR_NULL;

@@ -206,7 +206,7 @@ hero_status launch_write(const WriteArgs& a, int rows, hipStream_t st) {
     const int chunks = rows * (DH / 8);                                  // of the fullest unit
     const int upb = chunks <= 256 ? 4 : 1;
     const int64_t nb = (units + upb - 1) / upb;
-    if (units > 0x7ffffff0LL) return HERO_ERR_SHAPE;
+    if (!kv_launchable(nb, 256) || units > 0x7ffffff0LL) return HERO_ERR_SHAPE;
     const dim3 grid((unsigned)nb, (unsigned)a.B, 2), block(256);
 #define HERO_KVW(TPU, CH) hipLaunchKernelGGL((kv_write_kernel<FMT, DT, DH, TPU, CH>), grid, block, 0, st, a)
     if (chunks <= 64) HERO_KVW(64, 1);
@@ -273,7 +273,7 @@ extern "C" hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, con
     a.S = (int)S; a.start = start; a.kv_len = kv_len;
     a.sides = k_out && v_out ? 2 : (v_out ? 1 : 0);
     const int64_t per = 256 / (cache->Dh / 16), nb = (S * cache->H + per - 1) / per;
-    if (S * cache->H > 0x7fffff00LL) return HERO_ERR_SHAPE;
+    if (!kv_launchable(nb, 256) || S * cache->H > 0x7fffff00LL) return HERO_ERR_SHAPE;
     hipStream_t st = (hipStream_t)stream;
     const dim3 block(256), grid((unsigned)nb, (unsigned)cache->B, a.sides == 2 ? 2 : 1);
 #define HERO_KVR(FMT, DT) do { if (cache->Dh == 64) hipLaunchKernelGGL((kv_read_kernel<FMT, DT, 64>), grid, block, 0, st, a); \

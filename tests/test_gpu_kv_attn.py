@@ -262,6 +262,18 @@ def test_a_cache_without_blocks(hero):
     assert not bool(hero.hero_kv_read(c, 9, lens)[0].any())
 
 
+def test_many_rows_without_a_block(hero):
+    """More than 2^23 values to clear, rows apart from each other."""
+    B, S, H = 2, 9001, 8
+    codes = torch.empty((0, 16, H, 64), dtype=torch.int8, device="cuda")
+    scales = torch.empty((0, H), device="cuda")
+    cache = hero.kv_cache(codes, codes, scales, scales, max_blocks=0, batch=B)
+    q = torch.ones((B, S, H, 64), dtype=torch.bfloat16, device="cuda")
+    buf = torch.full((B * S, H * 64 + 12), 7.0, dtype=torch.bfloat16, device="cuda")
+    hero.hero_kv_attn(cache, q, 0.1, HB.MASK_NONE, _dev([0, 5]), out=buf[:, :H * 64])
+    assert int(buf[:, :H * 64].count_nonzero()) == 0 and bool((buf[:, H * 64:] == 7.0).all())
+
+
 @pytest.mark.parametrize("hp", ["bf16", "f16"])
 @pytest.mark.parametrize("fmt", ["i8", "e4m3"])
 def test_a_prompt_then_tokens(hero, fmt, hp):

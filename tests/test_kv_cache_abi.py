@@ -163,6 +163,19 @@ def test_a_read_of_too_many_rows(lib):
     assert _read(lib, _cache(), S=1 << 30) == SHAPE
 
 
+def test_more_threads_than_a_launch_has(lib):
+    # 2^32 threads and more: 65535 x 300 rows of one workgroup each; 512 blocks of 65535 heads, one each; 2^29 rows of 8 threads
+    assert _attn(lib, _cache(B=65535, H=300, n_blocks=1), Hq=300, Sq=1, ldo=300 * 64) == SHAPE
+    assert _write(lib, _cache(H=65535, block=128, max_blocks=512, n_blocks=1), S=1 << 16) == SHAPE
+    assert _read(lib, _cache(H=1 << 14, Dh=128), S=1 << 15) == SHAPE
+
+
+@pytest.mark.parametrize("blocks", (dict(n_blocks=0), dict(max_blocks=0)))
+def test_more_rows_than_fit_without_a_key(lib, blocks):
+    c = _cache(B=65535, H=65535, **blocks)
+    assert _attn(lib, c, Hq=65535, Sq=1 << 30, ldo=65535 * 64) == SHAPE     # (their elements pass 64 bits)
+
+
 def test_a_cache_on_another_device_than_the_current_one(monkeypatch):
     import paper_2310_17723_amd as pkg
     hero = pkg.load()
