@@ -424,13 +424,14 @@ hero_status hero_bf16_attn(const void* q, const int64_t q_strides[4],
  *                     stride must be 1, the others multiples of 16 that are not negative.  [n_blocks, H, block, Dh] keeps a head's block
  *                     in one piece.  The blocks of K and of V lie apart from each other (two views of one buffer will do).
  *   k_scale, v_scale  f32 [n_blocks, H]: token t of a block stands for codes[t] * scale.  Nothing needs clearing: a write that
- *                     begins a block (its first position is the block's first) sets its scales, whatever was there.
+ *                     begins a block (its first position is the block's first) sets its scales, whatever was there.  V's scales are positive
+ *                     where tokens lie (every write's are).
  *   block_table       int32 [B, max_blocks] (device): positions [j block, (j + 1) block) of sequence b lie in block block_table[b][j].
  *                     NULL: in block b max_blocks + j (n_blocks >= B max_blocks then).  An index outside [0, n_blocks) is no block:
  *                     nothing is written there, its keys are left out of the attention, its positions read as 0.  Sequences may
  *                     share blocks that are only read; a block that is written belongs to one sequence, once.
- * Constraints: Dh in {64, 128}; block in {16, 32, 64, 128}; max_blocks * block <= 2^30; H <= 65535; a block's 16 rows
- * span less than 2^31 elements.  The pointers are device pointers as everywhere; the structure itself is read during the call only. */
+ * Constraints: Dh in {64, 128}; block in {16, 32, 64, 128}; max_blocks * block <= 2^30; B, H <= 65535; n_blocks < 2^31;
+ * block times the position stride < 2^31.  The pointers are device pointers as everywhere; the structure itself is read during the call only. */
 typedef struct {
     void* k; void* v;
     float* k_scale; float* v_scale;

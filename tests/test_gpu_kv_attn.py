@@ -274,6 +274,61 @@ def test_many_rows_without_a_block(hero):
     assert int(buf[:, :H * 64].count_nonzero()) == 0 and bool((buf[:, H * 64:] == 7.0).all())
 
 
+FAR = {"blocks": (2 ** 30, 256, 128, 2 ** 29), "rows": (4096, 2 ** 24 - 16, 128, 2 ** 23), "heads": (2 ** 20, 128, 2 ** 32, 2 ** 31)}    # block, token (as far as it may), head, V behind K
+
+
+@pytest.mark.parametrize("far", sorted(FAR))
+def test_offsets_that_pass_32_bits(hero, far):
+    """Blocks, tokens of a block or heads that lie so far apart that their offsets pass 31 or 32 bits: the bits of the same cache in one piece."""
+    B, H, Dh, block, mb = 2, 2, 128, 128, 2
+    near = _filled(hero, "i8", B, H, Dh, block, mb, paged=True)
+    lens = [135, 256]
+    _fill(near, lens, 5, torch.bfloat16)
+    n = near.raw["k"].shape[0]
+    sb, sr, sh, sv = FAR[far]
+    buf = torch.empty((n - 1) * sb + (block - 1) * sr + (H - 1) * sh + sv + Dh, dtype=torch.int8, device="cuda")
+    k, v = (buf[off:].as_strided((n, block, H, Dh), (sb, sr, sh, 1), off) for off in (0, sv))
+    k.copy_(near.raw["k"].view(torch.int8))
+    v.copy_(near.raw["v"].view(torch.int8))
+    scales = [near.dev_scale[x].clone() for x in "kv"]
+    cache = hero.kv_cache(k, v, *scales, block_table=near.dev_table)
+    lens = [136, 256]
+    kn, vn = _rows(7, B, 1, H, Dh, torch.bfloat16), _rows(8, B, 1, H, Dh, torch.bfloat16)
+    near.write(kn, vn, lens)
+    hero.hero_kv_write(cache, kn, vn, _dev(lens))
+    near.check()
+    assert all(torch.equal(s, near.dev_scale[x]) for s, x in zip(scales, "kv"))
+    for x, y in zip(hero.hero_kv_read(cache, 256, _dev(lens)), hero.hero_kv_read(near.cache, 256, _dev(lens))):
+        assert torch.equal(x, y)
+    for S, tile in ((1, 16), (9, 32), (70, 256)):
+        q = _rows(9, B, S, 2 * H, Dh, torch.bfloat16, spread=False)
+        got = hero.hero_kv_attn(cache, q, 0.088, HB.MASK_CAUSAL, _dev(lens), tile=tile)
+        assert torch.equal(got, hero.hero_kv_attn(near.cache, q, 0.088, HB.MASK_CAUSAL, _dev(lens), tile=tile))
+        _check(near, q, 0.088, HB.MASK_CAUSAL, lens, got=got)
+
+
+@pytest.mark.parametrize("S,tile", [(20, 16), (20, 32), (33, 256)])
+def test_rows_that_lie_far_apart(hero, S, tile):
+    """Queries, rows to write, rows read and results whose offsets pass 32 bits: tokens 2^27 values apart."""
+    B, H, Dh, block, step = 2, 2, 64, 32, 2 ** 27
+    p, lens = _filled(hero, "i8", B, H, Dh, block, 3), [S, 96]
+    buf = torch.empty(B * S * step, dtype=torch.bfloat16, device="cuda")
+    place = lambda i, heads: buf.as_strided((B, S, heads, Dh), (S * step, step, Dh, 1), i * 1024)  # noqa: E731
+    k, v, q, ko, vo = (place(i, h) for i, h in enumerate((H, H, 2 * H, H, H)))
+    for x, seed in ((k, 1), (v, 2), (q, 3)):
+        x.copy_(_rows(seed, B, S, x.shape[2], Dh, torch.bfloat16, spread=False))
+    _fill(p, [96, 96], 5, torch.bfloat16)
+    p.write(k, v, lens)
+    p.check()
+    start = _dev([x - S for x in lens])
+    hero.hero_kv_read(p.cache, S, _dev(lens), start=start, k_out=ko, v_out=vo)
+    for x, y in zip(hero.hero_kv_read(p.cache, S, _dev(lens), start=start), (ko, vo)):
+        assert torch.equal(x, y)
+    out = buf.as_strided((B * S, 2 * H * Dh), (step, 1), 8192)
+    hero.hero_kv_attn(p.cache, q, 0.125, HB.MASK_CAUSAL, _dev(lens), out=out, tile=tile)
+    _check(p, q, 0.125, HB.MASK_CAUSAL, lens, got=out.contiguous())
+
+
 @pytest.mark.parametrize("hp", ["bf16", "f16"])
 @pytest.mark.parametrize("fmt", ["i8", "e4m3"])
 def test_a_prompt_then_tokens(hero, fmt, hp):

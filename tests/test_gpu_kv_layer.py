@@ -125,6 +125,35 @@ def test_tokens_one_by_one_are_the_whole_sequence(hero, fmt, arch):
     assert float((got - whole).norm() / whole.norm()) <= 3e-2
 
 
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+def test_a_captured_step(hero, fmt):
+    """A decode step captured once and replayed for other tokens and lengths in the same buffers, each replay against the step as it is called."""
+    shape, desc, W, t = _layer(hero, synth.PRE_LN, "M1", "bf16")
+    B, d = shape.B, shape.d
+    one, two = (Pool(hero, fmt, B, shape.H, shape.Dh, 16, 4, paged=True) for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(6)
+    h, lens = torch.zeros((B, d), dtype=torch.bfloat16, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    ws, ws2 = (torch.empty(hero.hero_layer_kv_workspace_bytes(desc, one.cache, 1), dtype=torch.uint8, device="cuda") for _ in range(2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        hero.hero_layer_fwd_kv(desc, W, one.cache, 1, ws, kv_len=lens, h=h)      # (lengths of 0: nothing is written)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hero.hero_layer_fwd_kv(desc, W, one.cache, 1, ws, kv_len=lens, h=h)
+    for step in range(20):
+        x = torch.randn((B, d), device="cuda", generator=g).to(torch.bfloat16)
+        h.copy_(x)
+        lens.copy_(torch.tensor([step + 1, max(step - 3, 0), step + 1]))
+        graph.replay()
+        hero.hero_layer_fwd_kv(desc, W, two.cache, 1, ws2, kv_len=lens, h=x)
+        assert torch.equal(h, x)
+        torch.cuda.synchronize()
+        for a, b in zip(hero.hero_kv_read(one.cache, 64, lens), hero.hero_kv_read(two.cache, 64, lens)):
+            assert torch.equal(a, b)
+
+
 def test_what_the_layer_refuses(hero):
     shape, desc, W, t = _layer(hero, synth.PRE_LN, "M1", "bf16")
     pool = Pool(hero, "i8", shape.B, shape.H, shape.Dh, 16, 4)

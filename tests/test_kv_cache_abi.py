@@ -51,7 +51,7 @@ BAD_CACHES = [(dict(Dh=96), UNSUPPORTED), (dict(Dh=256), UNSUPPORTED), (dict(blo
               (dict(k=None), NULL), (dict(v=None), NULL), (dict(k_scale=None), NULL), (dict(v_scale=None), NULL),
               (dict(ks=(2048, 64, 1024, 2)), UNSUPPORTED), (dict(vs=(2048, 72, 1024, 1)), ALIGN), (dict(ks=(2048, 64, 1000, 1)), ALIGN),
               (dict(ks=(2040, 64, 1024, 1)), ALIGN), (dict(vs=(-2048, 64, 1024, 1)), SHAPE), (dict(ks=(2048, -64, 1024, 1)), SHAPE),
-              (dict(ks=(2048, 2 ** 28, 1024, 1)), SHAPE), (dict(k=P + 8), ALIGN), (dict(v=P + 4), ALIGN), (dict(k_scale=P + 2), ALIGN),
+              (dict(ks=(2048, 2 ** 28, 1024, 1)), SHAPE), (dict(block=128, vs=(4096, 2 ** 24, 1024, 1)), SHAPE), (dict(k=P + 8), ALIGN), (dict(v=P + 4), ALIGN), (dict(k_scale=P + 2), ALIGN),
               (dict(table=P + 1), ALIGN)]
 
 
