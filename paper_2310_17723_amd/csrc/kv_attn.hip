@@ -872,6 +872,7 @@ Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq, int forced) {
     // Pieces of 16 steps or more while there are fewer than two workgroups per CU (one, of many rows of heads of 128).  us, towards 256 / 512 / 1024 workgroups:
     // 4 x 8 heads x 4 rows over 131072 keys 192 / 179 / 184, 16 x 8 heads x 20 rows over 4096 keys (its write with it) 49 / 41 / 46.  Many rows of heads of 64,
     // towards 256 / 512 / 768: 4 x 8 x 512 rows over 8192 keys 79 / 61 / 61.
+    // Pieces of 8 / 16 / 24 steps or more: 12 heads of 64 x 1 row over 512 keys 12.2 / 10.0 / 9.8, 4 x 8 x 4 rows over 2048 12.3 / 12.0 / 15.3, 3 x 2 x 539 over 1111 14.2 / 14.5 / 15.9.
     int64_t s = ((p.rt == 0 && c->Dh == 128 ? 256 : 512) + units - 1) / units;
     s = s < steps / 16 ? s : steps / 16;
     p.splits = (int)(s < 1 ? 1 : s > MOST_PIECES ? MOST_PIECES : s);
