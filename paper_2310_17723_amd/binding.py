@@ -443,6 +443,8 @@ class Hero:
             out = torch.empty((B * Sq, Hq * Dh), dtype=q.dtype, device=q.device)
         else:
             assert out.dtype is q.dtype and out.shape == (B * Sq, Hq * Dh) and out.stride(1) == 1
+            assert out.get_device() == cache.device, "the result lies on the cache's device"
+        assert workspace is None or workspace.get_device() == cache.device, "the workspace lies on the cache's device"
         args = (cache, q.data_ptr(), _kv_rows(cache, q, Sq, Hq), _DT[q.dtype], Hq, Sq, float(scale), int(mask),
                 _kv_length(cache, kv_len), _kv_length(cache, new_len), out.data_ptr(), out.stride(0),
                 None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _kv_stream(cache, stream))
@@ -484,6 +486,7 @@ class Hero:
                           h=None, x_hp=None, out_hp=None, next_read=None, stream=None):
         """hero_layer_fwd of a layer with 16-bit attention over a block-scaled cache (kv_cache)."""
         ptr = lambda t: 0 if t is None else t.data_ptr()
+        assert workspace.get_device() == cache.device, "the workspace lies on the cache's device"
         io = _LAYER_IO.pack(cache.sizes[0], S, ptr(x_q), ptr(x_scale), ptr(out_q), ptr(out_scale), ptr(h), _kv_length(cache, kv_len) or 0, 0, 0, 0,
                             ptr(x_hp), ptr(out_hp), ptr(next_read), 0 if next_read is None else next_read.nbytes)
         self._check(self.lib.hero_layer_fwd_kv(C.byref(desc), C.byref(weights), io, cache, _kv_length(cache, new_len), workspace.data_ptr(),

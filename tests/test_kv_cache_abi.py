@@ -189,3 +189,19 @@ def test_a_cache_on_another_device_than_the_current_one(monkeypatch):
     c.device = 1                                                          # rows that do not lie where the cache does
     with pytest.raises(AssertionError):
         hero.hero_kv_attn(c, q, 1.0, HB.MASK_CAUSAL, lens)
+
+
+class _Elsewhere(torch.Tensor):
+    def get_device(self):
+        return 1
+
+
+@pytest.mark.parametrize("part", ["out", "workspace"])
+def test_a_result_or_a_workspace_on_another_device(part):
+    import paper_2310_17723_amd as pkg
+    hero, z = pkg.load(), lambda *s: torch.zeros(s, dtype=torch.int8)  # noqa: E731
+    c = hero.kv_cache(z(4, 16, 2, 64), z(4, 16, 2, 64), torch.zeros(4, 2), torch.zeros(4, 2), max_blocks=2, batch=2)
+    q, lens = torch.zeros((2, 1, 2, 64), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    far = {"out": torch.zeros((2, 128), dtype=torch.bfloat16), "workspace": torch.zeros(256, dtype=torch.uint8)}[part].as_subclass(_Elsewhere)
+    with pytest.raises(AssertionError, match=part if part == "workspace" else "result"):
+        hero.hero_kv_attn(c, q, 1.0, HB.MASK_CAUSAL, lens, **{part: far})
