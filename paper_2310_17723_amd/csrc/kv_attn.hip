@@ -619,12 +619,7 @@ __global__ __launch_bounds__(64 * tile_waves(DH), DH == 64 ? 3 : 2) void kv_attn
         if (!fresh && __builtin_amdgcn_ballot_w64(most > MOST_P) == 0) return;
         float top = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < GH; ++g) {
-            float x = acc[g * GE];
-#pragma unroll
-            for (int r = 1; r < GE; ++r) x = fmaxf(x, acc[g * GE + r]);
-            top = fmaxf(top, fmaf(x, ck[g], lv[g]));
-        }
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaf(acc[r], ck[r / GE], lv[r / GE]));      // (a K scale may be negative: not of the largest score alone)
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
         top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
