@@ -4,7 +4,7 @@
 // The mathematics.  With K = ks c_k, V = vs c_v (scales of the key's block and head) and, base 2, a = scale log2(e) ks (q . c_k):
 //   out = sum_k 2^a vs c_v / sum_k 2^a = sum_k 2^b c_v / sum_k 2^b / vs,     b = a + log2 vs
 // so V's scale costs nothing per value: it is the addend of the fma that makes a score an exponent, and its reciprocal weighs a block's
-// share of the denominator.  The running maximum m is that of b; P = 2^(b - m + 15) is what FP16 holds: at most 2^15, and a normal number
+// share of the denominator.  The running maximum m is that of b; P = 2^(b - m + 15) is what FP16 holds: at most 2^15 (many rows: 2^15.94), and a normal number
 // down to 2^-29 of the row's largest (a long flat tail of small probabilities is not lost).  The denominator is summed before that rounding: a
 // block whose V is small beside the others' has a small P and may still hold most of the weight.  q is made FP16 too: rows of BF16 are
 // multiplied by a power of two that takes their largest value to [2^14, 2^15), which keeps every bit of values down to 2^-29 of it.
@@ -400,9 +400,11 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 // worked on.  Scores are computed transposed (S^T = K Q^T): a lane owns query lane % 32, and the exponentials are the second product's operand
 // as they stand.  A step makes the scores of 32 keys, takes the exponentials of the 32 before them and multiplies V by those of the 32 before
 // those, in one block of instructions.
-// The maximum is not taken of every step's scores: exponentials are taken against the last one, and only a row whose 32 add up to more than
-// 2^15 (FP16 holds 65504; a score 2^7 times as likely as the last maximum) has its maximum raised, its sums rescaled and the step's
-// exponentials taken again.
+// The maximum is taken of every step's exponents before P is made of them, and the sums so far are rescaled only where a row's has risen by more than SLACK: the
+// largest P of a row lies in [2^15, 2^15.94], its normal numbers reach down to 2^-29 of it as in the kernel of few rows.  (Exponentials against the last maximum, raised
+// behind a step whose P came near FP16's end, need 7 bits of room there: P was normal down to 2^-22 of the largest only, and a flat tail at 2^-28.5 behind a key with V = 0
+// off by 3 %.  us for the two cases below, so / as it is, with queries of a quarter, the listed and 2.5 times the size: 82 / 96, 88 / 96, 98 / 96 and 170 / 192,
+// 182 / 198, 207 / 199.)
 // K's rows are 16 bytes longer than they need to be, V's 16-byte pieces XOR-swizzled by their row: fragment reads (turns of lanes 0-3, 12-15,
 // 20-27 and so on) meet no bank conflict.
 // 8 x 32 heads x 256 rows behind 2304 E4M3 keys 90-92 us (800-817 TFLOP/s; a library product of 8192^3 runs at 1250), 4 x 32 x 2048 causal INT8 182 us
@@ -412,8 +414,7 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 // reads, but leave one wave per SIMD and too few registers: 150 us.  Beside the loop a workgroup takes 7 us (arguments, lengths, first tile, result); two
 // row tiles to a workgroup cost the loop more (8 %) than they saved.
 // ------------------------------------------------------------------------------------------
-constexpr float HEADROOM = 8.0f;                             // what a maximum's own P is 2 to the power of
-constexpr float MOST_P = 32768.0f;
+constexpr float SLACK = 0.9375f;                            // P stays below 2^15.95, FP16's end is 65504
 
 // The order of a step's instructions: an exponential and an LDS read behind each matrix instruction.
 template <int COUNT>
@@ -581,61 +582,54 @@ __global__ __launch_bounds__(64 * tile_waves(DH), DH == 64 ? 3 : 2) void kv_attn
             else gr[i / GH][i % GH] = x;
         }
     };
-    float ck[GH], lv[GH], sum[GH];
+    float sum[GH], resc;
     uint32_t p[8] = {0, 0, 0, 0, 0, 0, 0, 0}, q[8];                      // of the step before (nothing yet), of this one
+    // scores -> exponents, and what the largest makes of the row's maximum.  (A row by its own scores alone: its result does not depend on the others of its wave.)
     auto exponents = [&](int t, int s, v16f& acc, const Group (&gr)[GH], bool edge) __attribute__((always_inline)) {
 #pragma unroll
-        for (int g = 0; g < GH; ++g) { lv[g] = gr[g].lv; ck[g] = rc * gr[g].ks; }
-        if (edge) {                              // the exponents themselves, those of hidden keys (of scales that may be NaN) replaced
+        for (int g = 0; g < GH; ++g) {
+            const float ck = rc * gr[g].ks;
+#pragma unroll
+            for (int r = g * GE; r < (g + 1) * GE; ++r) acc[r] = fmaf(acc[r], ck, gr[g].lv);
+        }
+        if (edge) {                              // hidden keys (of scales that may be NaN)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int key = t * 64 + s * 32 + (r >> 2) * 8 + hh * 4 + (r & 3);
-                const float x = fmaf(acc[r], ck[r / GE], lv[r / GE]);
-                acc[r] = key < min(seen, gr[r / GE].lim) ? x : -INFINITY;
+                acc[r] = key < min(seen, gr[r / GE].lim) ? acc[r] : -INFINITY;
             }
-#pragma unroll
-            for (int g = 0; g < GH; ++g) { lv[g] = 0.0f; ck[g] = 1.0f; }
         }
+        float top = acc[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+        const float mn = top > m + SLACK ? top : m;
+        resc = mn > m ? __builtin_amdgcn_exp2f(m - mn) : 1.0f;
+        m = mn;
     };
     auto weigh = [&](const v16f& acc) __attribute__((always_inline)) {
-        const float sub = (m > -INFINITY ? m : 0.0f) - HEADROOM;
+        const float sub = (m > -INFINITY ? m : 0.0f) - LIFT;
 #pragma unroll
         for (int g = 0; g < GH; ++g) {
-            const float add = lv[g] - sub;
             sum[g] = 0.0f;
 #pragma unroll
             for (int r = g * GE; r < (g + 1) * GE; r += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(fmaf(acc[r], ck[g], add)), e1 = __builtin_amdgcn_exp2f(fmaf(acc[r + 1], ck[g], add));
+                const float e0 = __builtin_amdgcn_exp2f(acc[r] - sub), e1 = __builtin_amdgcn_exp2f(acc[r + 1] - sub);
                 sum[g] += e0 + e1;
                 q[r >> 1] = f16x2(e0, e1);
             }
         }
     };
-    bool fresh = true;                                                   // some row that sees a key of this piece has no maximum yet
-    auto raise = [&](const v16f& acc) __attribute__((always_inline)) {
-        float most = sum[0];
-#pragma unroll
-        for (int g = 1; g < GH; ++g) most += sum[g];
-        if (!fresh && __builtin_amdgcn_ballot_w64(most > MOST_P) == 0) return;
-        float top = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaf(acc[r], ck[r / GE], lv[r / GE]));      // (a K scale may be negative: not of the largest score alone)
-        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
-        top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-        most = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
-        // (a row by its own scores alone: its result does not depend on the others of its wave)
-        const float mn = (most > MOST_P || m == -INFINITY) && top > m ? top : m, resc = mn > m ? __builtin_amdgcn_exp2f(m - mn) : 1.0f;
-        m = mn;
-        l *= resc;
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[c][r] *= resc;
-        fresh = __builtin_amdgcn_ballot_w64(m == -INFINITY && seen > t0 * 64) != 0;
-        weigh(acc);
-    };
+    // behind the products, which were of the P before: all sums at the maximum of this step
     auto settled = [&](const Group (&gr)[GH]) __attribute__((always_inline)) {
+        if (__builtin_amdgcn_ballot_w64(resc != 1.0f) != 0) {
+            l *= resc;
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[c][r] *= resc;
+        }
 #pragma unroll
         for (int g = 0; g < GH; ++g) l += sum[g] == 0.0f ? 0.0f : sum[g] * gr[g].iv;
 #pragma unroll
@@ -712,14 +706,12 @@ __global__ __launch_bounds__(64 * tile_waves(DH), DH == 64 ? 3 : 2) void kv_attn
         stage(after);
         fetch(min(t + 2, te), id2);
         step_order<DS + 2 * CT>();
-        raise(acc);
         settled(gr[0]);
         meet();
         exponents(t, 1, next, gr[1], edge);
         acc = products(after, 0, buf, 0);
         weigh(next);
         step_order<DS + 2 * CT>();
-        raise(next);
         settled(gr[1]);
         before = buf;
     }

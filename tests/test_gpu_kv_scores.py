@@ -1,4 +1,4 @@
-"""hero_kv_attn where the scores make it hard: K scales of either sign, against 64 bits on the same codes and scales."""
+"""hero_kv_attn where the scores make it hard (K scales of either sign, probabilities far below the largest), against 64 bits on the same codes and scales."""
 import numpy as np
 import pytest
 import torch
@@ -28,3 +28,26 @@ def test_k_scales_of_either_sign(hero, fmt, block, S):
     for tile in TILES:
         for mask in (HB.MASK_NONE, HB.MASK_CAUSAL):
             _check(p, q, Dh ** -0.5, mask, [L, L - 7], tile=tile)
+
+
+@pytest.mark.parametrize("S", [1, 40, 140])
+@pytest.mark.parametrize("nats", [18.5, 19.75, 20.0])                     # 2^-26.7, 2^-28.5, 2^-28.9 of the largest
+@pytest.mark.parametrize("hp", ["bf16", "f16"])
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+def test_a_flat_tail_far_below_the_largest(hero, fmt, hp, nats, S):
+    """One key holds nearly all of a row's weight and its V is zero: the result is a long tail of equal probabilities down to 2^-29 of the largest, which are
+    normal numbers of FP16 there, off by 2^-11.  The large key is seen first (each later step is taken against its maximum), in the middle, last, and in steps
+    that double it."""
+    H, Dh, block, L = 1, 64, 16, 480
+    p = _filled(hero, fmt, 4, H, Dh, block, L // block)
+    q, k = (torch.zeros((4, n, H, Dh), device="cuda") for n in (S, L))
+    v = _rows(111, 4, L, H, Dh, torch.float32, spread=False).abs() * 2.0 ** 10
+    q[..., 0] = 8
+    for b, at in ((0, 3), (1, 250), (2, L - 1), (3, L - 1)):
+        k[b, at, :, 0] = nats                                             # the score: 8 nats / sqrt(64)
+        v[b, at] = 0
+    k[3, 7::40, :, 0] = torch.arange(1, 13, device="cuda")[:, None].float() * 1.25
+    v[3, 7::40] = 0
+    p.write(k.to(HP[hp]), v.to(HP[hp]), [L] * 4)
+    for tile in TILES:
+        _check(p, q.to(HP[hp]), Dh ** -0.5, HB.MASK_NONE, [L] * 4, tile=tile)
