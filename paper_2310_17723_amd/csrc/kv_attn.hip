@@ -36,6 +36,13 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {       // v_cvt_p
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{lo, hi}), v2h));
 }
 
+// What the exponents of a row whose largest is `top` are taken against: LIFT less, or `top` itself where fp32 has no such number (from 2^24 on top - LIFT can lie 16
+// below it, and P = 2^16 is none of FP16).  Sums are held against this number, so that a lift that changes is no factor lost.
+__device__ __forceinline__ float against(float top) {
+    const float below = top - LIFT;
+    return top - below > LIFT ? top : below;
+}
+
 // ---- codes -> FP16 ----
 // two codes of INT8 in the bytes that sel picks, as FP16: 0x64xx is 1024 + xx, xx = code + 128
 __device__ __forceinline__ uint32_t i8x2_to_f16(uint32_t hi, uint32_t lo, uint32_t sel) {
@@ -300,12 +307,12 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
             top = max_of_groups16(top);
-            const float mn = fmaxf(m[rt], top), ms = mn > -INFINITY ? mn : 0.0f, sub = ms - LIFT;
+            const float mn = fmaxf(m[rt], against(top)), ms = mn > -INFINITY ? mn : 0.0f;
             const float resc = __builtin_amdgcn_exp2f(m[rt] - ms);
             float sum[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(x[j] - sub), e1 = __builtin_amdgcn_exp2f(x[j + 1] - sub);
+                const float e0 = __builtin_amdgcn_exp2f(x[j] - ms), e1 = __builtin_amdgcn_exp2f(x[j + 1] - ms);
                 p[rt][j >> 1] = f16x2(e0, e1);
                 sum[j >> 2] += e0 + e1;
             }
@@ -604,12 +611,12 @@ __global__ __launch_bounds__(64 * tile_waves(DH), DH == 64 ? 3 : 2) void kv_attn
         for (int r = 1; r < 16; ++r) top = fmaxf(top, acc[r]);
         const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-        const float mn = top > m + SLACK ? top : m;
+        const float mn = top - m > LIFT + SLACK ? against(top) : m;      // (m is -inf before the first key)
         resc = mn > m ? __builtin_amdgcn_exp2f(m - mn) : 1.0f;
         m = mn;
     };
     auto weigh = [&](const v16f& acc) __attribute__((always_inline)) {
-        const float sub = (m > -INFINITY ? m : 0.0f) - LIFT;
+        const float sub = m > -INFINITY ? m : 0.0f;
 #pragma unroll
         for (int g = 0; g < GH; ++g) {
             sum[g] = 0.0f;
