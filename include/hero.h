@@ -445,10 +445,10 @@ typedef struct {
  * row s < n (n = new_len[b] clamped to [0, S], or S without new_len) is the token at position kv_len[b] - n + s; positions
  * outside [0, max_blocks * block) are left out, and rows s >= n are not read.  For every block with a new token, per head, K and V apart:
  *   a     = max |x| over the block's new tokens
- *   s_new = max(s_old, a / qmax, 2^-64)          qmax 127 (INT8) or 448 (E4M3), IEEE fp32 division;
+ *   s_new = max(|s_old|, a / qmax, 2^-64)        qmax 127 (INT8) or 448 (E4M3), IEEE fp32 division;
  *                                                s_old = 0 if the block holds no token from before this call
  *   code  = sat(rne(x / s_new)) or e4m3(x / s_new), saturated          IEEE fp32 division
- *   and, where s_new > s_old, the tokens from before are coded anew: the code of fl(code s_old) at s_new.
+ *   and, where s_new != s_old, the tokens from before are coded anew: the code of fl(code s_old) at s_new.
  * A scale never shrinks while its block fills, so tokens cost their block a new coding only when they raise its largest value.  A NaN or
  * infinity among the new tokens makes the scale NaN, and what is read from that block and head is NaN until it is begun anew.
  *   k, v  [B, S, H, Dh] in dt (HERO_BF16 / HERO_F16), base pointer and 4 element strides (batch, token, head, channel);

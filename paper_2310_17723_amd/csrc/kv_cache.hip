@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
     }
     const bool finite = top < (DT == HERO_BF16 ? 0x7f80u : 0x7c00u);
     const float wanted = fmaxf(__fdiv_rn(hp_to_f32<DT>(top), Fmt<FMT>::most), SMALLEST);
-    const float s = !finite || s_old != s_old ? __builtin_nanf("") : fmaxf(s_old, wanted);
+    const float s = !finite || s_old != s_old ? __builtin_nanf("") : fmaxf(fabsf(s_old), wanted);      // (a scale from elsewhere may be negative: coded anew then)
     if (tid == 0) *scale = s;
     const Divisor by(s);                                                 // (codes at a scale that is NaN: 0, whatever the values)
     uint8_t* const out = sd.codes + (int64_t)blk * sd.s_block + (int64_t)h * sd.s_head;
