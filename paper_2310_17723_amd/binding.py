@@ -119,6 +119,15 @@ def _stream(stream=None):
     return _raw_stream(torch.cuda.current_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
 
 
+def _zeros(size, dtype, device, stream):
+    """Memory as for every other result, cleared on the stream of the call that goes on to write there."""
+    if stream is None:
+        return torch.zeros(size, dtype=dtype, device=device)
+    t = torch.empty(size, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return t.zero_()
+
+
 def _strides4(t):
     assert t.dim() == 4
     return (i64 * 4)(*t.stride())
@@ -423,9 +432,9 @@ class Hero:
         are left as they were in k_out / v_out, and are 0 in outputs made here."""
         B, H, Dh = cache.sizes
         if k_out is None:
-            k_out = torch.zeros((B, S, H, Dh), dtype=dtype if v_out is None else v_out.dtype, device=kv_len.device)
+            k_out = _zeros((B, S, H, Dh), dtype if v_out is None else v_out.dtype, kv_len.device, stream)
         if v_out is None:
-            v_out = torch.zeros((B, S, H, Dh), dtype=k_out.dtype, device=kv_len.device)
+            v_out = _zeros((B, S, H, Dh), k_out.dtype, kv_len.device, stream)
         assert k_out.dtype is v_out.dtype
         self._check(self.lib.hero_kv_read(cache, k_out.data_ptr(), _kv_rows(cache, k_out, S, H), v_out.data_ptr(), _kv_rows(cache, v_out, S, H),
                                           _DT[k_out.dtype], S, _kv_length(cache, start), _kv_length(cache, kv_len), _kv_stream(cache, stream)))

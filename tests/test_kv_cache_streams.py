@@ -1,0 +1,44 @@
+"""The block-scaled KV cache on another stream than the current one (no GPU needed: the library and the streams are stand-ins)."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+
+@pytest.fixture
+def hero(monkeypatch):
+    """A binding whose library launches nothing; .on is the stream that torch's own kernels would go to, .log what was done and where."""
+    from paper_2310_17723_amd.binding import Hero
+    h = object.__new__(Hero)
+    h.on, h.log = "current", []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *args: h.log.append((name, args[-1])) or 0
+    h.lib = Lib()
+
+    @contextlib.contextmanager
+    def stream(s):
+        was, h.on = h.on, s.cuda_stream
+        yield
+        h.on = was
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    for where, name in ((torch, "zeros"), (torch.Tensor, "zero_")):
+        monkeypatch.setattr(where, name, lambda *a, was=getattr(where, name), **k: h.log.append(("cleared", h.on)) or was(*a, **k))
+    return h
+
+
+def _cache(hero):
+    z = lambda *s, dt=torch.int8: torch.empty(s, dtype=dt)  # noqa: E731
+    return hero.kv_cache(z(4, 16, 2, 64), z(4, 16, 2, 64), z(4, 2, dt=torch.float32), z(4, 2, dt=torch.float32), max_blocks=2, batch=2)
+
+
+def test_rows_read_back_are_cleared_on_the_stream_that_writes_them(hero):
+    side = types.SimpleNamespace(cuda_stream="side", device_index=-1)
+    out = torch.ones((2, 5, 2, 64), dtype=torch.bfloat16)
+    for kw in (dict(), dict(v_out=out), dict(k_out=out)):
+        hero.log.clear()
+        k, v = hero.hero_kv_read(_cache(hero), 5, torch.empty(2, dtype=torch.int32), stream=side, **kw)
+        assert [w for _, w in hero.log] == ["side"] * len(hero.log) and hero.log[-1][0] == "hero_kv_read" and len(hero.log) == 3 - len(kw)
+        assert all(bool((t == 0).all()) or t is out for t in (k, v))
