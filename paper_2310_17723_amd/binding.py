@@ -221,7 +221,7 @@ class Hero:
         T, D = x.shape
         assert x.stride(1) == 1
         if col_absmax is None:
-            col_absmax = torch.zeros(D, dtype=torch.float32, device=x.device)
+            col_absmax = _zeros(D, torch.float32, x.device, stream)
         self._check(self.lib.hero_absmax_cols(_ptr(x), _DT[x.dtype], x.stride(0) if T > 1 else max(D, x.stride(0)), T, D,
                                               _ptr(col_absmax), _stream(stream)))
         return col_absmax

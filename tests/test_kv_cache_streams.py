@@ -1,4 +1,4 @@
-"""The block-scaled KV cache on another stream than the current one (no GPU needed: the library and the streams are stand-ins)."""
+"""The block-scaled KV cache, and what else clears its result itself, on another stream than the current one (no GPU needed: the library and the streams are stand-ins)."""
 import contextlib
 import types
 
@@ -42,3 +42,9 @@ def test_rows_read_back_are_cleared_on_the_stream_that_writes_them(hero):
         k, v = hero.hero_kv_read(_cache(hero), 5, torch.empty(2, dtype=torch.int32), stream=side, **kw)
         assert [w for _, w in hero.log] == ["side"] * len(hero.log) and hero.log[-1][0] == "hero_kv_read" and len(hero.log) == 3 - len(kw)
         assert all(bool((t == 0).all()) or t is out for t in (k, v))
+
+
+def test_column_maxima_are_cleared_on_the_stream_that_raises_them(hero):
+    side = types.SimpleNamespace(cuda_stream="side", device_index=-1)
+    hero.hero_absmax_cols(torch.ones((3, 8)), stream=side)
+    assert [w for _, w in hero.log] == ["side", "side"]
