@@ -154,8 +154,9 @@ def _kv_length(cache, t):
 
 
 def _kv_stream(cache, stream):
-    if stream is None and cache.device != torch.cuda.current_device():
-        raise ValueError(f"the cache lies on device {cache.device}, which is not the current one")
+    device = torch.cuda.current_device() if stream is None else stream.device_index
+    if cache.device != device:
+        raise ValueError(f"the cache lies on device {cache.device}, which is not the " + ("current one" if stream is None else f"stream's ({device})"))
     return _stream(stream)
 
 

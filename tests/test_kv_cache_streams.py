@@ -5,12 +5,13 @@ import types
 import pytest
 import torch
 
+from paper_2310_17723_amd import binding as HB
+
 
 @pytest.fixture
 def hero(monkeypatch):
     """A binding whose library launches nothing; .on is the stream that torch's own kernels would go to, .log what was done and where."""
-    from paper_2310_17723_amd.binding import Hero
-    h = object.__new__(Hero)
+    h = object.__new__(HB.Hero)
     h.on, h.log = "current", []
 
     class Lib:
@@ -48,3 +49,17 @@ def test_column_maxima_are_cleared_on_the_stream_that_raises_them(hero):
     side = types.SimpleNamespace(cuda_stream="side", device_index=-1)
     hero.hero_absmax_cols(torch.ones((3, 8)), stream=side)
     assert [w for _, w in hero.log] == ["side", "side"]
+
+
+def test_a_stream_of_another_device_than_the_cache(hero):
+    """The kernels would run on the stream's device, without the cache's memory."""
+    far = types.SimpleNamespace(cuda_stream="far", device_index=0)        # (the stand-in's tensors lie on the CPU, -1)
+    c, lens = _cache(hero), torch.empty(2, dtype=torch.int32)
+    q, ws = torch.empty((2, 1, 2, 64), dtype=torch.bfloat16), torch.empty(256, dtype=torch.uint8)
+    desc, w = hero.layer_desc(HB.ARCH_PRE_LN, 128, 2, 64, 256, 1e-5, HB.MASK_CAUSAL, HB.MODE_M1), HB.LayerWeights()
+    for call in (lambda: hero.hero_kv_write(c, q, q, lens, stream=far), lambda: hero.hero_kv_read(c, 1, lens, k_out=q, v_out=q, stream=far),
+                 lambda: hero.hero_kv_attn(c, q, 1.0, HB.MASK_CAUSAL, lens, stream=far),
+                 lambda: hero.hero_layer_fwd_kv(desc, w, c, 1, ws, kv_len=lens, stream=far)):
+        with pytest.raises(ValueError, match="stream"):
+            call()
+    assert not hero.log
