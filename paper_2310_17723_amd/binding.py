@@ -494,8 +494,11 @@ class Hero:
 
     def hero_layer_fwd_kv(self, desc, weights, cache, S, workspace, *, kv_len, new_len=None, x_q=None, x_scale=None, out_q=None, out_scale=None,
                           h=None, x_hp=None, out_hp=None, next_read=None, stream=None):
-        """hero_layer_fwd of a layer with 16-bit attention over a block-scaled cache (kv_cache)."""
+        """hero_layer_fwd of a layer with 16-bit attention over a block-scaled cache (kv_cache): batch * S rows, batch being the cache's."""
         ptr = lambda t: 0 if t is None else t.data_ptr()
+        T = cache.sizes[0] * S
+        for t in (x_q, x_scale, out_q, out_scale, h, x_hp, out_hp):
+            assert t is None or (len(t) == T and t.get_device() == cache.device), "a layer's rows are the cache's batch * S, on its device"
         assert workspace.get_device() == cache.device, "the workspace lies on the cache's device"
         io = _LAYER_IO.pack(cache.sizes[0], S, ptr(x_q), ptr(x_scale), ptr(out_q), ptr(out_scale), ptr(h), _kv_length(cache, kv_len) or 0, 0, 0, 0,
                             ptr(x_hp), ptr(out_hp), ptr(next_read), 0 if next_read is None else next_read.nbytes)

@@ -30,6 +30,11 @@ def hero(monkeypatch):
     return h
 
 
+class _Elsewhere(torch.Tensor):
+    def get_device(self):
+        return 1
+
+
 def _cache(hero):
     z = lambda *s, dt=torch.int8: torch.empty(s, dtype=dt)  # noqa: E731
     return hero.kv_cache(z(4, 16, 2, 64), z(4, 16, 2, 64), z(4, 2, dt=torch.float32), z(4, 2, dt=torch.float32), max_blocks=2, batch=2)
@@ -63,3 +68,18 @@ def test_a_stream_of_another_device_than_the_cache(hero):
         with pytest.raises(ValueError, match="stream"):
             call()
     assert not hero.log
+
+
+@pytest.mark.parametrize("name", ["x_q", "x_scale", "out_q", "out_scale", "h", "x_hp", "out_hp"])
+def test_rows_of_another_number_or_device_than_the_cache_has(hero, name):
+    """The kernels would read and write batch * S rows, the batch being the cache's, whatever the tensors hold."""
+    stream = types.SimpleNamespace(cuda_stream="side", device_index=-1)
+    c, lens, ws = _cache(hero), torch.empty(2, dtype=torch.int32), torch.empty(256, dtype=torch.uint8)
+    desc, w = hero.layer_desc(HB.ARCH_PRE_LN, 128, 2, 64, 256, 1e-5, HB.MASK_CAUSAL, HB.MODE_M1), HB.LayerWeights()
+    size = lambda n: (n,) if name.endswith("scale") else (n, 128)  # noqa: E731
+    for bad in (torch.empty(size(3)), torch.empty(size(7)), torch.empty(size(6)).as_subclass(_Elsewhere)):
+        with pytest.raises(AssertionError, match="rows"):
+            hero.hero_layer_fwd_kv(desc, w, c, 3, ws, kv_len=lens, stream=stream, **{name: bad})
+    assert not hero.log
+    hero.hero_layer_fwd_kv(desc, w, c, 3, ws, kv_len=lens, stream=stream, **{name: torch.empty(size(6))})
+    assert hero.log == [("hero_layer_fwd_kv", "side")]
