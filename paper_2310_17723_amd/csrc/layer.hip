@@ -136,6 +136,7 @@ static hero_status layer_run(const hero_layer_desc* desc, const hero_layer_weigh
     if (kv) {
         HERO_TRY(kv_check(kv));
         if ((desc->mode_mask & HERO_M_ATTN) || io->k_cache || io->v_cache) return HERO_ERR_UNSUPPORTED;   // (an INT8 attention reads SQ codes)
+        if (desc->mask != HERO_MASK_NONE && desc->mask != HERO_MASK_PADDING && desc->mask != HERO_MASK_CAUSAL) return HERO_ERR_UNSUPPORTED;
         if (kv->B != B || kv->H != desc->H || kv->Dh != desc->Dh || (!new_len && kv->max_blocks * kv->block < S)) return HERO_ERR_SHAPE;
     }
     if (T == 0) return HERO_OK;
