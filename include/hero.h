@@ -425,7 +425,8 @@ hero_status hero_bf16_attn(const void* q, const int64_t q_strides[4],
  *                     in one piece.  The blocks of K and of V lie apart from each other (two views of one buffer will do).
  *   k_scale, v_scale  f32 [n_blocks, H]: token t of a block stands for codes[t] * scale.  Nothing needs clearing: a write that
  *                     begins a block (its first position is the block's first) sets its scales, whatever was there.  V's scales are positive
- *                     where tokens lie (every write's are).
+ *                     where tokens lie, and V's E4M3 codes there are numbers (all that a write makes are; in a cache from elsewhere a NaN among
+ *                     V's codes may also reach rows that do not see its token).  K's scales may have either sign.
  *   block_table       int32 [B, max_blocks] (device): positions [j block, (j + 1) block) of sequence b lie in block block_table[b][j].
  *                     NULL: in block b max_blocks + j (n_blocks >= B max_blocks then).  An index outside [0, n_blocks) is no block:
  *                     nothing is written there, its keys are left out of the attention, its positions read as 0.  Sequences may
@@ -449,7 +450,9 @@ typedef struct {
  *                                                s_old = 0 if the block holds no token from before this call
  *   code  = sat(rne(x / s_new)) or e4m3(x / s_new), saturated          IEEE fp32 division
  *   and, where s_new != s_old, the tokens from before are coded anew: the code of fl(code s_old) at s_new.
- * A scale never shrinks while its block fills, so tokens cost their block a new coding only when they raise its largest value.  A NaN or
+ * A scale never shrinks while its block fills, so tokens cost their block a new coding only when they raise its largest value.  Each new
+ * coding rounds anew: a block filled token by token has 1.25 to 1.35 (INT8) or 1.35 to 1.45 times (E4M3) the rms error of one written at once where its
+ * tokens are of one size, 1.6 to 2.5 times where they grow from first to last.  A NaN or
  * infinity among the new tokens makes the scale NaN, and what is read from that block and head is NaN until it is begun anew.
  *   k, v  [B, S, H, Dh] in dt (HERO_BF16 / HERO_F16), base pointer and 4 element strides (batch, token, head, channel);
  *         channel stride 1, the others multiples of 8 (views into a fused QKV buffer will do).  B is the cache's.
@@ -484,7 +487,8 @@ hero_status hero_kv_read(const hero_kv_cache* cache, void* k_out, const int64_t 
  * V scale is more than 2^100 times smaller than another's that the row sees may be taken for one that it does not see.)
  * Few rows (Sq * Hq / H) over many keys are split along the keys when `workspace` has room: hero_kv_attn_workspace_bytes(cache,
  * Hq, Sq) bytes (0: this size is not split), device memory, 256-byte aligned (else HERO_ERR_WORKSPACE).  NULL or smaller: one piece (slower, and
- * fp32 sums are ordered otherwise).  Pure scratch, nothing is kept between calls: calls that may overlap on the GPU need
+ * fp32 sums are ordered otherwise).  Kernel and split go by max_blocks * block, not by the lengths: a table that is much wider than its
+ * sequences are long costs speed.  Pure scratch, nothing is kept between calls: calls that may overlap on the GPU need
  * their own.  The order of the sums depends on the sizes alone, so results are reproducible.
  * B * Sq * Hq < 2^31, and workgroups (B * H for every 16 rows, where rows are that few) for less than 2^32 threads: else HERO_ERR_SHAPE. */
 size_t hero_kv_attn_workspace_bytes(const hero_kv_cache* cache, int64_t Hq, int64_t Sq);
@@ -498,7 +502,7 @@ hero_status hero_kv_attn(const hero_kv_cache* cache, const void* q, const int64_
  *   kv       the layer's cache, for io->B sequences of desc->H heads of width desc->Dh (else HERO_ERR_SHAPE); io->k_cache and
  *            io->v_cache are NULL.  io->kv_len [B], required, counts this call's tokens.
  *   new_len  int32 [B] (device) or NULL: of the S rows of sequence b the first new_len[b] are tokens (a padded batch; the
- *            other rows are computed without a key to attend to).
+ *            other rows are computed without a key to attend to).  Without it S tokens have to fit the cache's positions (else HERO_ERR_SHAPE).
  *   workspace: hero_layer_kv_workspace_bytes(desc, kv, S) bytes; what hero_layer_fwd accepts without is accepted without here,
  *            and the attention of few rows is then not split. */
 size_t hero_layer_kv_workspace_bytes(const hero_layer_desc* desc, const hero_kv_cache* kv, int64_t S);

@@ -149,9 +149,10 @@ __device__ __forceinline__ int keys_seen(const AttnArgs& a, int row, int len, in
 // channels of its key; V: a lane's 8 (4) channels of 8 keys, paired up by byte permutes), and an online softmax of its own; the NW waves of
 // a workgroup split the keys of its piece and meet in LDS.
 // Bound by HBM: each code is read once for all rows that share its head (the matrix instructions work on 16 rows whether there are 1 or 16, 8 %
-// of the time at that).  K's next codes are asked for behind the first product and V's behind the second, which leaves registers for
-// four waves per SIMD.  4 x 8 heads x 4 rows over 131072 E4M3 keys: 1.03 GB in 174-179 us, 5.8-5.9 TB/s (a read-only stream 6.15); 64 x 32 heads x 1 row
-// over 1100 .. 2048 INT8 keys, 0.82 GB: 150 us, 5.5 TB/s; 16 x 8 heads x 20 rows over 3000 .. 4096: 26.6 us, 4.4 TB/s.
+// of the time at that).  K's next codes are asked for behind the first product and V's behind the second, which leaves registers for four waves per SIMD with one
+// row tile of heads of 128 (INT8 codes and FP16 rows: 132 registers, three), five with heads of 64; two row tiles of heads of 128 take 184-188, two waves.
+// 4 x 8 heads x 4 rows over 131072 E4M3 keys: 1.03 GB in 174 us, 5.9 TB/s (a read-only stream 6.15); 64 x 32 heads x 1 row
+// over 1100 .. 2048 INT8 keys, 0.82 GB: 152 us, 5.4 TB/s; 16 x 8 heads x 20 rows (two tiles) over 3000 .. 4096: 26-27 us, 4.4 TB/s.
 // ------------------------------------------------------------------------------------------
 template <int DH, int FMT, int DT, int RT, int NW>
 __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
@@ -414,11 +415,12 @@ __global__ __launch_bounds__(64 * NW) void kv_attn_rows_kernel(AttnArgs a) {
 // 182 / 198, 207 / 199.)
 // K's rows are 16 bytes longer than they need to be, V's 16-byte pieces XOR-swizzled by their row: fragment reads (turns of lanes 0-3, 12-15,
 // 20-27 and so on) meet no bank conflict.
-// 8 x 32 heads x 256 rows behind 2304 E4M3 keys 90-92 us (800-817 TFLOP/s; a library product of 8192^3 runs at 1250), 4 x 32 x 2048 causal INT8 182 us
-// (755).  In clocks per tile and CU, of 3793 (2048 of matrix instructions): without fragment reads 2783, without staging and loads 2877, without
-// exponentials 3528, without any of them 2335; but the clock the power limit allows falls with what is left (1.94 GHz -> 1.73), so that orders of
-// instructions, priorities, 32 vector instructions fewer and loads that nothing waits for changed a launch by 2 % or not at all.  64 rows to a wave halve the
-// reads, but leave one wave per SIMD and too few registers: 150 us.  Beside the loop a workgroup takes 7 us (arguments, lengths, first tile, result); two
+// 8 x 32 heads x 256 rows behind 2304 E4M3 keys 95-97 us (755 TFLOP/s; a library product of 8192^3 runs at 1270), 4 x 32 x 2048 causal INT8 197 us
+// (697), 4 x 32 heads of 64 x 2048 causal INT8 113.  In clocks per tile and CU of the first: 4600 at 2.14 GHz, 2048 of them matrix instructions, 310 rescaled sums (in two
+// steps of five; 120 with queries of a quarter of the size, 440 with 2.5 times).  Against a late maximum it was 3793 at 1.94 GHz, of which without fragment
+// reads 2783, without staging and loads 2877, without exponentials 3528, without any of them 2335; the clock that the power limit allows fell with what was left (1.73 GHz),
+// so that orders of instructions, priorities and loads that nothing waits for changed a launch by 2 % or not at all.  64 rows to a wave halve the
+// reads, but leave one wave per SIMD and too few registers: half as long again.  Beside the loop a workgroup takes 7 us (arguments, lengths, first tile, result); two
 // row tiles to a workgroup cost the loop more (8 %) than they saved.
 // ------------------------------------------------------------------------------------------
 constexpr float SLACK = 0.9375f;                            // P stays below 2^15.95, FP16's end is 65504
@@ -437,7 +439,7 @@ __device__ __forceinline__ void step_order() {
 }
 
 // A thread stages one unit of K and one of V per tile of 64 keys, which for heads of 64 gives work to 256 threads; three such workgroups fit a CU.  us against eight
-// waves whose halves stage the same: 4 x 32 heads of 64 x 2048 rows causal INT8 136 -> 105, 8 x 12 x 512 causal 20.1 -> 16.9, 16 x 12 x 128 over 1024 34.0 -> 26.9.
+// waves whose halves stage the same (both against a late maximum): 4 x 32 heads of 64 x 2048 rows causal INT8 136 -> 105, 8 x 12 x 512 causal 20.1 -> 16.9, 16 x 12 x 128 over 1024 34.0 -> 26.9.
 constexpr int tile_waves(int Dh) { return Dh == 64 ? 4 : 8; }
 
 template <int DH, int FMT, int DT, int NI>                   // NI: blocks that a tile's 64 keys lie in
@@ -847,11 +849,14 @@ __global__ void kv_attn_zero_kernel(uint16_t* out, int64_t rows, int64_t cols, i
 }
 
 // How a call is cut: 16 rt rows to a tile of the kernel of few rows, or 256 (heads of 64: 128) to one of that of many (rt = 0); the keys into pieces.
-// The kernel of many rows reads K and V once per such tile, and takes longer to begin and end.  us, few / many: 36 rows of 512 heads over 2048 keys of
-// 128 values 90 / 120, 64 of 8 over 65536 50 / 63, 80 of 512 over 1000 75 / 67, 128 of 8 over 2048 (0.3 G multiply-adds) 18 / 20, 256 of 8 over 2048 (0.5) 19 / 27, 160 of 8 over
-// 4000 (0.7) 25 / 26, 200 of 128 heads of 64 over 600 (1.0) 20 / 20, 128 of 128 heads of 64 over 1000 (1.0) 18 / 22,
-// 100 of 48 heads of 64 over 4096 (1.3) 32 / 26, 512 of 96 heads of 64 over 512 (1.6) 24 / 17, 300 of 24 heads of 64 over 4096 (1.9) 30 / 32, 128 of 32 over 4096 (2.1) 34 / 31,
-// 1024 of 32 over 1024 causal (4.3) 49 / 59, 512 of 8 over 8192 (4.3) 45 / 40, 160 of 128 over 4000 (10) 126 / 93, 2048 of 32 over 2048 causal (17) 137 / 76.
+// The kernel of many rows reads K and V once per such tile, and takes longer to begin and end.  us, few / many, by the multiply-adds of rows x keys (in G; neither the
+// mask nor the sequences' lengths are known here: the table's width stands for the keys):
+//   0.3: 128 rows of 8 heads over 2048 keys 16 / 24      0.5: 256 of 8 over 2048 18 / 32              0.7: 160 of 8 over 4000 24 / 32
+//   1.0: 200 of 128 heads of 64 over 600 21 / 19         1.0: 128 of 128 heads of 64 over 1000 20 / 24   1.3: 100 of 48 heads of 64 over 4096 33 / 28
+//   1.6: 512 of 96 heads of 64 over 512 25 / 21          1.9: 300 of 24 heads of 64 over 4096 33 / 36    2.1: 128 of 32 over 4096 30 / 29
+//   4.3: 1024 of 32 over 1024 causal 46 / 40             4.3: 512 of 8 over 8192 47 / 42              5.2: 80 of 512 over 1000 72 / 67
+//   10: 160 of 128 over 4000 126 / 83                    17: 2048 of 32 over 2048 causal 130 / 78     69: 4096 of 32 over 4096 causal 372 / 174
+// and up to 64 rows, which the kernel of few rows reads once too: 36 rows of 512 heads over 2048 keys 91 / 115, 64 of 8 over 65536 49 / 61.
 struct Plan { int rt, tiles, splits; };
 
 // forced: 0, or the rows of a tile (16, 32, 256 for the kernel of many rows)
@@ -864,8 +869,8 @@ Plan plan(const hero_kv_cache* c, int64_t Hq, int64_t Sq, int forced) {
     p.tiles = (int)((rows + tile - 1) / tile);
     const int64_t units = bh * p.tiles;
     // Pieces of 16 steps or more while there are fewer than two workgroups per CU (one, of many rows of heads of 128).  us, towards 256 / 512 / 1024 workgroups:
-    // 4 x 8 heads x 4 rows over 131072 keys 192 / 179 / 184, 16 x 8 heads x 20 rows over 4096 keys (its write with it) 49 / 41 / 46.  Many rows of heads of 64,
-    // towards 256 / 512 / 768: 4 x 8 x 512 rows over 8192 keys 79 / 61 / 61.
+    // 4 x 8 heads x 4 rows over 131072 keys 192 / 179 / 184, 16 x 8 heads x 20 rows over 4096 keys (its write with it) 49 / 41 / 46.  Many rows, towards
+    // 256 / 512 / 768: 4 x 8 heads of 64 x 512 rows over 8192 keys 89 / 69 / 69, heads of 128 94 / 108 / 124.
     // Pieces of 8 / 16 / 24 steps or more: 12 heads of 64 x 1 row over 512 keys 12.2 / 10.0 / 9.8, 4 x 8 x 4 rows over 2048 12.3 / 12.0 / 15.3, 3 x 2 x 539 over 1111 14.2 / 14.5 / 15.9.
     int64_t s = ((p.rt == 0 && c->Dh == 128 ? 256 : 512) + units - 1) / units;
     s = s < steps / 16 ? s : steps / 16;

@@ -63,7 +63,7 @@ __device__ __forceinline__ void values4(uint32_t w, float (&x)[4]) {
 // each), so that they are read once for the maximum and the codes.  The maximum is one of bit patterns: NaN > infinity > numbers.
 // A unit whose block holds older tokens and whose maximum grows codes those anew from the cache.
 // Up to 2048 values (a few tokens, or pages of 16) a unit is one wave's, else a workgroup's.  Bound by HBM and, in small calls, by the chain of length, block,
-// scale and rows: 8 x 2048 tokens of 32 heads of 128 in 80-87 us, 4.6-5.0 TB/s (and read back 156-159, a large copy's rate; with IEEE
+// scale and rows: 8 x 2048 tokens of 32 heads of 128 in 87 us, 4.6 TB/s (and read back 158, a large copy's rate; with IEEE
 // divisions 176); 64 x 1 token 5 us, 16 x 301 in pages of 16 9 us (12.5 with the divisions, the look-up in front of the rows and 64-bit index arithmetic).
 // ------------------------------------------------------------------------------------------
 template <int FMT, int DT, int DH, int TPU, int CH>
@@ -159,8 +159,8 @@ struct ReadArgs {
 };
 
 // A thread reads 16 codes of a row, a row being a head of a position, heads fastest (the order of the output).  Bound by HBM: 4 x 32768 positions of
-// 8 heads of 128 in 159 us, 5.0 TB/s, a large copy's rate (with the index taken apart by 64-bit divisions 207; two, four, eight rows to a thread
-// 156, 172, 184; with streaming stores 219 and more).
+// 8 heads of 128 in 139-140 us, 5.7 TB/s, above a large copy's rate (an earlier form in 159: with the index taken apart by 64-bit divisions 207; with two, four, eight rows to a
+// thread 156, 172, 184; with streaming stores 219 and more).
 template <int FMT, int DT, int DH>
 __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
     constexpr int CPR = DH / 16, RPB = 256 / CPR;
