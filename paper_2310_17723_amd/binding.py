@@ -498,7 +498,10 @@ class Hero:
         ptr = lambda t: 0 if t is None else t.data_ptr()
         T = cache.sizes[0] * S
         for t in (x_q, x_scale, out_q, out_scale, h, x_hp, out_hp):
-            assert t is None or (len(t) == T and t.get_device() == cache.device), "a layer's rows are the cache's batch * S, on its device"
+            if t is not None:
+                assert t.get_device() == cache.device, "a layer's rows lie on the cache's device"
+                if len(t) != T:
+                    raise HeroError(2, f"a layer's rows are the cache's batch * S, {T} here and not {len(t)}")     # HERO_ERR_SHAPE
         assert workspace.get_device() == cache.device, "the workspace lies on the cache's device"
         io = _LAYER_IO.pack(cache.sizes[0], S, ptr(x_q), ptr(x_scale), ptr(out_q), ptr(out_scale), ptr(h), _kv_length(cache, kv_len) or 0, 0, 0, 0,
                             ptr(x_hp), ptr(out_hp), ptr(next_read), 0 if next_read is None else next_read.nbytes)

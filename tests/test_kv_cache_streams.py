@@ -77,9 +77,12 @@ def test_rows_of_another_number_or_device_than_the_cache_has(hero, name):
     c, lens, ws = _cache(hero), torch.empty(2, dtype=torch.int32), torch.empty(256, dtype=torch.uint8)
     desc, w = hero.layer_desc(HB.ARCH_PRE_LN, 128, 2, 64, 256, 1e-5, HB.MASK_CAUSAL, HB.MODE_M1), HB.LayerWeights()
     size = lambda n: (n,) if name.endswith("scale") else (n, 128)  # noqa: E731
-    for bad in (torch.empty(size(3)), torch.empty(size(7)), torch.empty(size(6)).as_subclass(_Elsewhere)):
-        with pytest.raises(AssertionError, match="rows"):
+    for bad in (torch.empty(size(3)), torch.empty(size(7))):
+        with pytest.raises(HB.HeroError, match="rows") as e:
             hero.hero_layer_fwd_kv(desc, w, c, 3, ws, kv_len=lens, stream=stream, **{name: bad})
+        assert e.value.status == 2
+    with pytest.raises(AssertionError, match="rows"):
+        hero.hero_layer_fwd_kv(desc, w, c, 3, ws, kv_len=lens, stream=stream, **{name: torch.empty(size(6)).as_subclass(_Elsewhere)})
     assert not hero.log
     hero.hero_layer_fwd_kv(desc, w, c, 3, ws, kv_len=lens, stream=stream, **{name: torch.empty(size(6))})
     assert hero.log == [("hero_layer_fwd_kv", "side")]
