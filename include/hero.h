@@ -510,6 +510,78 @@ hero_status hero_layer_fwd_kv(const hero_layer_desc* desc, const hero_layer_weig
                               const hero_kv_cache* kv, const int32_t* new_len,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- the operators of a mixture-of-experts MLP (Sec. 2.2.3's two linears, one pair of weights per expert; the router and the weighted
+ * sum are not the paper's) ----
+ *
+ * A router gives every token k of E experts; the rows of an expert are computed together.  Nothing about which expert has how many rows is
+ * known to the host: `offsets` lies on the device, a call is enqueued for R rows at most, and no call waits for another's result.
+ *
+ *   LN^quant (codes, scales and y_hp) -> router logits (hero_hp_gemm of y_hp) -> hero_moe_route -> first linear, GELU^quant
+ *   (hero_int8_gemm_grouped, row_index = row_token) -> second linear (DEQUANT, no row_index) -> hero_moe_combine into the residual stream
+ *
+ * hero_moe_route: the experts of every token, and the order of their rows.
+ *   l[t][e]  = logits[t][e] in fp32; a NaN counts as -infinity, +infinity as the largest finite number
+ *   chosen   the (up to) top_k experts of the largest l[t][e] > -infinity, falling, ties to the lowest index:
+ *            expert[t][0], expert[t][1], ..; what is left of the top_k is -1 (a padding token: all its logits -infinity)
+ *   weight[t][j] = exp(l[t][expert[t][j]] - m) / sum exp(l[t][e] - m), m = max_e l[t][e]; the sum over the chosen experts (renorm != 0) or
+ *            over all E (renorm == 0), in fp32;  0 where expert[t][j] is -1
+ *   offsets  the rows of expert e are offsets[e] .. offsets[e + 1] - 1, in the order of t * top_k + j; offsets[E] is their number
+ *   slot[t][j]    the row of choice j of token t, or -1
+ *   row_token[r]  the token of row r, or -1 (r >= offsets[E])
+ *   logits [T,E] in dt (HERO_F32 / HERO_BF16 / HERO_F16), leading dimension ldl.  expert, slot int32 [T,top_k]; weight f32 [T,top_k];
+ *   row_token int32 [T*top_k]; offsets int32 [E+1]: all are written whole.
+ *   workspace: hero_moe_route_workspace_bytes(T, E, top_k) bytes (0 for few tokens), 256-byte aligned, else HERO_ERR_WORKSPACE.  Pure scratch:
+ *            calls that may overlap on the GPU need their own.
+ * Constraints: 1 <= E <= 512, 1 <= top_k <= 16, top_k <= E; T * top_k < 2^31.  T == 0: offsets are written, all 0.
+ * The results depend on the arguments alone (no order of atomics shows in them). */
+size_t hero_moe_route_workspace_bytes(int64_t T, int64_t E, int64_t top_k);
+hero_status hero_moe_route(const void* logits, hero_dtype dt, int64_t ldl, int64_t T, int64_t E, int64_t top_k, int renorm,
+                           int32_t* expert, float* weight, int32_t* slot, int32_t* row_token, int32_t* offsets,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* GeMM^quant of E experts in one call (Sec. 2.1, 2.2.3): the product of hero_int8_gemm with the weights, the column vectors and the number
+ * of rows of each expert.  For the rows offsets[e] <= r < offsets[e + 1]:
+ *   i = row_index ? row_index[r] : r
+ *   acc[r][j] = sum_k A[i][k] * Bt[e][j][k];  t = float(acc) * a_row_scale[i] (skipped if NULL)
+ *   y = fma(t, b_col_scale[e][j], bias[e][j]) (bias NULL = 0);  then the epilogue with out_col_scale[e][j]
+ *   A    [MA,K] int8 row-major, leading dimension lda; MA == R without row_index.  a_row_scale f32[MA] or NULL.
+ *   Bt   E matrices [N,K], K contiguous, leading dimension ldb, expert_stride elements apart.
+ *   b_col_scale, bias, out_col_scale  f32 [E,N], contiguous.
+ *   C    [R,N] in c_dt, leading dimension ldc; rows r >= offsets[E] are left as they were.
+ *   offsets  int32 [E+1] (device), rising from 0 to at most R.  (Others cannot be reported from an asynchronous call: each is taken
+ *        as the largest of those up to it, within [0, R], and the rows in front of offsets[0] belong to no expert.)
+ *   row_index int32 [R] (device) or NULL; an index outside [0, MA) is clamped.  It is read below offsets[E] only.
+ *   epi  HERO_EPI_DEQUANT, HERO_EPI_DEQUANT_GELU (C HERO_BF16 / HERO_F16), HERO_EPI_REQUANT, HERO_EPI_GELU_REQUANT (C HERO_I8);
+ *        no residual (hero_moe_combine adds it).
+ * Constraints: E <= 512; R < 2^23; K % 64 == 0; lda, ldb, expert_stride multiples of 16, ldc of 4; base pointers of A, Bt, C 16-byte aligned;
+ * R * N such that a launch holds it (else HERO_ERR_SHAPE).  R == 0, N == 0 or E == 0 is a no-op.
+ * Which kernel runs is chosen by R, E, N and K; results of 8-bit integer operands do not depend on it.
+ * hero_fp8_gemm_grouped: the same with OCP E4M3 operands (hero_fp8_gemm; 8-bit results are HERO_F8E4M3).
+ * hero_hp_gemm_grouped: 16-bit operands (hero_hp_gemm): C = act(A Bt[e]^T + bias[e]) in dt; K % 32 == 0, lda, ldb, expert_stride
+ * multiples of 8. */
+hero_status hero_int8_gemm_grouped(const int8_t* A, int64_t lda, int64_t MA, const float* a_row_scale, const int32_t* row_index,
+                                   const int8_t* Bt, int64_t ldb, int64_t expert_stride, const float* b_col_scale, const float* bias,
+                                   hero_epilogue epi, const float* out_col_scale, void* C, hero_dtype c_dt, int64_t ldc,
+                                   const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K, void* stream);
+hero_status hero_fp8_gemm_grouped(const void* A, int64_t lda, int64_t MA, const float* a_row_scale, const int32_t* row_index,
+                                  const void* Bt, int64_t ldb, int64_t expert_stride, const float* b_col_scale, const float* bias,
+                                  hero_epilogue epi, const float* out_col_scale, void* C, hero_dtype c_dt, int64_t ldc,
+                                  const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K, void* stream);
+hero_status hero_hp_gemm_grouped(const void* A, int64_t lda, int64_t MA, const int32_t* row_index,
+                                 const void* Bt, int64_t ldb, int64_t expert_stride, const float* bias, int gelu,
+                                 void* C, int64_t ldc, const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K,
+                                 hero_dtype dt, void* stream);
+
+/* The weighted sum of every token's rows:  out[t] = residual[t] + sum_j weight[t][j] * y[slot[t][j]], in fp32 (the choices in their
+ * order, the residual last), rounded once; a choice whose slot lies outside [0, R) is left out, whatever its weight.
+ *   y [R,D], residual [T,D] or NULL (= 0), out [T,D] in dt (HERO_BF16 / HERO_F16), leading dimensions ldy, ldr, ldo; out may be the residual
+ *   itself (ldo == ldr).  slot int32 [T,top_k], weight f32 [T,top_k].
+ * Constraints: D and the leading dimensions multiples of 8, base pointers 16-byte aligned, 1 <= top_k <= 16; T * D such that a launch holds it
+ * (else HERO_ERR_SHAPE).  T == 0 or D == 0 is a no-op. */
+hero_status hero_moe_combine(const void* y, int64_t ldy, int64_t R, const int32_t* slot, const float* weight,
+                             const void* residual, int64_t ldr, void* out, int64_t ldo,
+                             int64_t T, int64_t top_k, int64_t D, hero_dtype dt, void* stream);
+
 /* Model-load-time operators (not on the hot path): the pre-processing phase of the method on the GPU.
  *
  * hero_absmax_cols -- calibration statistic of the static scales (Sec. 2.1: FWQ / SQ scales are

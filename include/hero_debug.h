@@ -54,6 +54,14 @@ hero_status hero_kv_attn_tile(const hero_kv_cache* cache, const void* q, const i
                               int64_t Hq, int64_t Sq, float scale, hero_mask mask, const int32_t* kv_len, const int32_t* new_len,
                               void* out, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream, int tile);
 
+/* hero_int8_gemm_grouped, hero_fp8_gemm_grouped and hero_hp_gemm_grouped (dt HERO_I8, HERO_F8E4M3, HERO_BF16, HERO_F16; the 16-bit types
+ * take epi HERO_EPI_DEQUANT or HERO_EPI_DEQUANT_GELU, no scales, and c_dt == dt) with the kernel forced.  tile: 16 / 32 = the weight-streaming
+ * kernel of few rows with tiles of so many rows; 0 the library's own choice; else HERO_ERR_UNSUPPORTED. */
+hero_status hero_gemm_grouped_tile(hero_dtype dt, const void* A, int64_t lda, int64_t MA, const float* a_row_scale, const int32_t* row_index,
+                                   const void* Bt, int64_t ldb, int64_t expert_stride, const float* b_col_scale, const float* bias,
+                                   hero_epilogue epi, const float* out_col_scale, void* C, hero_dtype c_dt, int64_t ldc,
+                                   const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K, void* stream, int tile);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+from typing import NamedTuple
 
 import torch
 
@@ -91,10 +92,26 @@ SYMBOLS = {
     "hero_layer_fwd": (i32, [C.POINTER(LayerDesc), C.POINTER(LayerWeights), C.POINTER(LayerIO), vp, C.c_size_t, vp]),
     "hero_layer_kv_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDesc), C.POINTER(KvCache), i64]),
     "hero_layer_fwd_kv": (i32, [C.POINTER(LayerDesc), C.POINTER(LayerWeights), vp, C.POINTER(KvCache), vp, vp, C.c_size_t, vp]),
+    "hero_moe_route_workspace_bytes": (C.c_size_t, [i64, i64, i64]),
+    "hero_moe_route": (i32, [vp, i32, i64, i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]),
+    "hero_moe_combine": (i32, [vp, i64, i64, vp, vp, vp, i64, vp, i64, i64, i64, i64, i32, vp]),
+    "hero_int8_gemm_grouped": (i32, [vp, i64, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp, vp, i32, i64, vp, i64, i64, i64, i64, vp]),
+    "hero_fp8_gemm_grouped": (i32, [vp, i64, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp, vp, i32, i64, vp, i64, i64, i64, i64, vp]),
+    "hero_hp_gemm_grouped": (i32, [vp, i64, i64, vp, vp, i64, i64, vp, i32, vp, i64, vp, i64, i64, i64, i64, i32, vp]),
+    "hero_gemm_grouped_tile": (i32, [i32, vp, i64, i64, vp, vp, vp, i64, i64, vp, vp, i32, vp, vp, i32, i64, vp, i64, i64, i64, i64, vp, i32]),
     "hero_bf16_gemm": (i32, [vp, i64, vp, i64, vp, vp, i64, i32, vp, i64, i64, i64, i64, vp]),
     "hero_bf16_attn": (i32, [vp, C.POINTER(i64), vp, C.POINTER(i64), vp, C.POINTER(i64), i64, i64, i64, i64, i64,
                              f32, i32, vp, vp, i64, vp]),
 }
+
+
+class MoeRouting(NamedTuple):
+    """What hero_moe_route leaves behind: expert, slot int32 [T, top_k], weight f32 [T, top_k], row_token int32 [T * top_k], offsets int32 [E + 1]."""
+    expert: torch.Tensor
+    weight: torch.Tensor
+    slot: torch.Tensor
+    row_token: torch.Tensor
+    offsets: torch.Tensor
 
 
 class HeroError(RuntimeError):
@@ -158,6 +175,33 @@ def _kv_stream(cache, stream):
     if cache.device != device:
         raise ValueError(f"the cache lies on device {cache.device}, which is not the " + ("current one" if stream is None else f"stream's ({device})"))
     return _stream(stream)
+
+
+def _on_device(device, stream, *tensors):
+    """The stream of a call whose tensors all lie on `device` (an index), which has to be the stream's."""
+    at = torch.cuda.current_device() if stream is None else stream.device_index
+    if device != at:
+        raise ValueError(f"the tensors lie on device {device}, which is not the " + ("current one" if stream is None else f"stream's ({at})"))
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("the tensors of a call lie on one device")
+    return _stream(stream)
+
+
+def _vector(t, dtype, *shape):
+    """The address of a contiguous tensor of this type and shape."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} tensor {list(shape)}, not {t.dtype} {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _matrix(t, cols):
+    """The leading dimension of rows of `cols` elements (a single row may have any)."""
+    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"expected rows of {cols} neighbouring elements, not {list(t.shape)} with strides {list(t.stride())}")
+    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
 
 
 class Hero:
@@ -459,6 +503,107 @@ class Hero:
                 _kv_length(cache, kv_len), _kv_length(cache, new_len), out.data_ptr(), out.stride(0),
                 None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _kv_stream(cache, stream))
         self._check(self.lib.hero_kv_attn(*args) if tile is None else self.lib.hero_kv_attn_tile(*args, int(tile)))
+        return out
+
+    # ------------------------------------------------------------------ mixture of experts
+    def moe_routing(self, T, E, top_k, device="cuda") -> MoeRouting:
+        """Room for the results of hero_moe_route."""
+        new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)
+        return MoeRouting(new(T, top_k), torch.empty((T, top_k), dtype=torch.float32, device=device), new(T, top_k), new(T * top_k), new(E + 1))
+
+    def hero_moe_route_workspace_bytes(self, T, E, top_k) -> int:
+        return int(self.lib.hero_moe_route_workspace_bytes(T, E, top_k))
+
+    def hero_moe_route(self, logits, top_k, renorm=True, out=None, workspace=None, stream=None) -> MoeRouting:
+        """The top_k experts of every token (logits [T,E] f32 / bf16 / f16) and the order of their rows.  workspace: uint8 tensor
+        (hero_moe_route_workspace_bytes), made here if it is None and needed; out: a MoeRouting to write into (moe_routing)."""
+        T, E = logits.shape
+        if out is None:
+            out = self.moe_routing(T, E, top_k, logits.device)
+        if workspace is None:
+            need = self.hero_moe_route_workspace_bytes(T, E, top_k)
+            workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+        st = _on_device(logits.get_device(), stream, workspace, *out)
+        self._check(self.lib.hero_moe_route(
+            logits.data_ptr(), _DT[logits.dtype], _matrix(logits, E), T, E, top_k, int(bool(renorm)), _vector(out.expert, torch.int32, T, top_k),
+            _vector(out.weight, torch.float32, T, top_k), _vector(out.slot, torch.int32, T, top_k), _vector(out.row_token, torch.int32, T * top_k),
+            _vector(out.offsets, torch.int32, E + 1), _ptr(workspace), 0 if workspace is None else workspace.nbytes, st))
+        return out
+
+    def _grouped(self, A, W, offsets, row_index, vectors, out_dtype, C_out, stream):
+        """What the products by expert share: (the result, the arguments around the vectors)."""
+        E, N, K = W.shape
+        if E > 0 and N > 0 and (W.stride(2) != 1 or A.element_size() != W.element_size()):
+            raise ValueError("weights are [E, N, K] with K contiguous, of the rows' type")
+        R = A.shape[0] if row_index is None else row_index.shape[0]
+        if C_out is None:
+            C_out = torch.empty((R, N), dtype=out_dtype, device=A.device)
+        elif C_out.shape[0] != R:
+            raise ValueError(f"the result has a row for each of the {R} rows, not {C_out.shape[0]}")
+        st = _on_device(A.get_device(), stream, W, offsets, row_index, C_out, *vectors)
+        front = (A.data_ptr(), _matrix(A, K), A.shape[0])
+        weights = (W.data_ptr(), W.stride(1) if N > 1 else max(K, W.stride(1)), W.stride(0))
+        back = (C_out.data_ptr(), _DT[C_out.dtype], _matrix(C_out, N), _vector(offsets, torch.int32, E + 1), E, R, N, K)
+        return C_out, front, _vector(row_index, torch.int32, R), weights, back, st
+
+    def _gemm_grouped8(self, fn, dt, A, W, offsets, row_index, a_row_scale, b_col_scale, bias, epi, out_col_scale, out_dtype, C_out, stream, tile):
+        E, N, _ = W.shape
+        if out_dtype is None:
+            out_dtype = torch.bfloat16 if epi in (EPI_DEQUANT, EPI_DEQUANT_GELU) else torch.int8 if dt == I8 else torch.float8_e4m3fn
+        vectors = (a_row_scale, b_col_scale, bias, out_col_scale)
+        C_out, front, index, weights, back, st = self._grouped(A, W, offsets, row_index, vectors, out_dtype, C_out, stream)
+        args = (*front, _vector(a_row_scale, torch.float32, A.shape[0]), index, *weights, _vector(b_col_scale, torch.float32, E, N),
+                _vector(bias, torch.float32, E, N), int(epi), _vector(out_col_scale, torch.float32, E, N), *back, st)
+        self._check(fn(*args) if tile is None else self.lib.hero_gemm_grouped_tile(dt, *args, int(tile)))
+        return C_out
+
+    def hero_int8_gemm_grouped(self, A, W, offsets, row_index=None, a_row_scale=None, b_col_scale=None, bias=None, epi=EPI_DEQUANT,
+                               out_col_scale=None, out_dtype=None, C_out=None, stream=None, tile=None):
+        """Rows offsets[e] .. offsets[e+1] - 1 (int32 [E+1] on the device) of A [R,K] int8, or of A[row_index] (int32 [R]), times W[e]; W
+        [E,N,K] int8.  a_row_scale f32 [A's rows] or None; b_col_scale, bias, out_col_scale f32 [E,N].  Returns C [R,N]: bf16 (or
+        out_dtype float16) or, for the REQUANT epilogues, int8; rows from offsets[E] on are not written.  tile=<code> -> the test hook
+        hero_gemm_grouped_tile (include/hero_debug.h: the kernel forced)."""
+        if A.dtype is not torch.int8 or W.dtype is not torch.int8:
+            raise ValueError("rows and weights are int8")
+        return self._gemm_grouped8(self.lib.hero_int8_gemm_grouped, I8, A, W, offsets, row_index, a_row_scale, b_col_scale, bias, epi, out_col_scale,
+                                   out_dtype, C_out, stream, tile)
+
+    def hero_fp8_gemm_grouped(self, A, W, offsets, row_index=None, a_row_scale=None, b_col_scale=None, bias=None, epi=EPI_DEQUANT,
+                              out_col_scale=None, out_dtype=None, C_out=None, stream=None, tile=None):
+        """The FP8 variant: A, W hold E4M3 bytes (torch.float8_e4m3fn or uint8 storage); 8-bit results are float8_e4m3fn."""
+        if A.element_size() != 1 or W.element_size() != 1:
+            raise ValueError("rows and weights are E4M3 bytes")
+        return self._gemm_grouped8(self.lib.hero_fp8_gemm_grouped, F8E4M3, A, W, offsets, row_index, a_row_scale, b_col_scale, bias, epi, out_col_scale,
+                                   out_dtype, C_out, stream, tile)
+
+    def hero_hp_gemm_grouped(self, A, W, offsets, row_index=None, bias=None, gelu=False, C_out=None, stream=None, tile=None):
+        """The 16-bit side: A, W and the result in one type, bf16 or fp16."""
+        if A.dtype not in (torch.bfloat16, torch.float16) or W.dtype is not A.dtype or (C_out is not None and C_out.dtype is not A.dtype):
+            raise ValueError("rows, weights and result are of one 16-bit type")
+        E, N, _ = W.shape
+        C_out, front, index, weights, back, st = self._grouped(A, W, offsets, row_index, (bias,), A.dtype, C_out, stream)
+        b = _vector(bias, torch.float32, E, N)
+        if tile is None:
+            self._check(self.lib.hero_hp_gemm_grouped(*front, index, *weights, b, int(bool(gelu)), back[0], *back[2:], back[1], st))
+        else:
+            epi = EPI_DEQUANT_GELU if gelu else EPI_DEQUANT
+            self._check(self.lib.hero_gemm_grouped_tile(back[1], *front, None, index, *weights, None, b, epi, None, *back, st, int(tile)))
+        return C_out
+
+    def hero_moe_combine(self, y, slot, weight, residual=None, out=None, stream=None):
+        """out[t] = residual[t] + sum_j weight[t][j] y[slot[t][j]]; y [R,D], residual, out [T,D] bf16 / f16 (out may be the residual itself);
+        slot int32, weight f32 [T,top_k]; slots outside [0, R) are left out."""
+        R, D = y.shape
+        T, k = slot.shape
+        if out is None:
+            out = torch.empty((T, D), dtype=y.dtype, device=y.device)
+        for t in (residual, out):
+            if t is not None and (t.dtype is not y.dtype or t.shape[0] != T):
+                raise ValueError(f"residual and result are {y.dtype} rows of the {T} tokens")
+        st = _on_device(y.get_device(), stream, slot, weight, residual, out)
+        self._check(self.lib.hero_moe_combine(y.data_ptr(), _matrix(y, D), R, _vector(slot, torch.int32, T, k), _vector(weight, torch.float32, T, k),
+                                              _ptr(residual), 0 if residual is None else _matrix(residual, D), out.data_ptr(), _matrix(out, D),
+                                              T, k, D, _DT[y.dtype], st))
         return out
 
     # ------------------------------------------------------------------ layer

@@ -1,0 +1,96 @@
+// What the kernels of products grouped by expert share: their arguments, and which rows of which expert a tile holds.
+#pragma once
+#include "gemm_common.h"
+
+namespace hero_gemm {
+
+constexpr int MAX_EXPERTS = 512;
+
+// GemmArgs with g.M = R (rows of C); Bt, b_col_scale, bias and out_col_scale are expert 0's
+struct GroupedArgs {
+    GemmArgs g;
+    const int32_t* offsets; const int32_t* row_index;
+    int E, MA;                                  // experts, rows of A
+    int64_t expert_stride;                      // bytes between the weights of two experts
+    int epi, c_dt;                              // (for kernels that ask at run time)
+};
+
+// inclusive sum over the lanes of a wave
+__device__ __forceinline__ int wave_scan_sum(int x) {
+#define HERO_SHR(n) x += __builtin_amdgcn_update_dpp(0, x, 0x110 + n, 0xF, 0xF, true)
+    HERO_SHR(1); HERO_SHR(2); HERO_SHR(4); HERO_SHR(8);         // row_shr within 16 lanes
+#undef HERO_SHR
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // lane 15 of rows 0, 2 into rows 1, 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // lane 31 into rows 2, 3
+    return x;
+}
+__device__ __forceinline__ int wave_scan_max(int x, int lane) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o); if (lane >= o) x = max(x, y); }
+    return x;
+}
+
+// One piece of 64 experts, an expert to a lane: its rows [begin, end).  Offsets outside [0, R] and falling ones are taken as the largest
+// up to them (`carry`: the end of the piece in front), so that whatever is handed over the rows lie within [0, R] and no row has two experts.
+__device__ __forceinline__ void expert_rows(const GroupedArgs& a, int e0, int lane, int carry, int& begin, int& end) {
+    const int e = e0 + lane, R = a.g.M;
+    const int lo = a.offsets[min(e, a.E)], hi = a.offsets[min(e + 1, a.E)];
+    begin = min(max(lo, 0), R);
+    end = min(max(hi, 0), R);
+    if (__ballot(end < begin || begin < carry)) {               // (rare)
+        begin = wave_scan_max(max(begin, carry), lane);
+        end = max(end, begin);
+    }
+}
+
+// Rows of a tile: [row0, row0 + rows) of expert e; rows == 0: there is no such tile
+struct GroupTile { int e, row0, rows, col_tile; };
+
+// Tile `slot` of this XCD's share.  Tiles of BM rows; those of an expert lie together, and of them the row tiles of one column tile (they read the
+// same weights).  Every XCD takes a contiguous range of the list.  Every lane of the wave calls it, and `slot` is uniform.
+template <int BM>
+__device__ __forceinline__ GroupTile group_tile(const GroupedArgs& a, int xcd, int slot, int ntn, int lane) {
+    constexpr int PIECES = MAX_EXPERTS / 64;
+    int begin[PIECES], end[PIECES], upto[PIECES], carry = 0, tiles = 0;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        begin[p] = end[p] = 0; upto[p] = 0;
+        if (p * 64 < a.E) {
+            expert_rows(a, p * 64, lane, carry, begin[p], end[p]);
+            upto[p] = tiles + wave_scan_sum((end[p] - begin[p] + BM - 1) / BM);
+            carry = __builtin_amdgcn_readlane(end[p], 63);
+            tiles = __builtin_amdgcn_readlane(upto[p], 63);
+        }
+    }
+    const int per = (int)(((int64_t)tiles * ntn + NUM_XCD - 1) / NUM_XCD);
+    const int64_t seq = (int64_t)xcd * per + slot;
+    GroupTile t{0, 0, 0, 0};
+    if (slot >= per || seq >= (int64_t)tiles * ntn) return t;
+    const int at = (int)(seq / ntn);                            // the expert is the first whose tiles reach beyond this row tile
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        if (p * 64 < a.E && t.rows == 0) {
+            const unsigned long long beyond = __ballot(upto[p] > at);
+            if (beyond) {
+                const int l = __ffsll(beyond) - 1;
+                const int b = __builtin_amdgcn_readlane(begin[p], l), n = __builtin_amdgcn_readlane(end[p], l) - b, mt = (n + BM - 1) / BM;
+                const int first = __builtin_amdgcn_readlane(upto[p], l) - mt;
+                const int64_t in = seq - (int64_t)first * ntn;
+                const int m = (int)(in % mt);
+                t.e = p * 64 + l; t.col_tile = (int)(in / mt);
+                t.row0 = b + m * BM; t.rows = min(BM, n - m * BM);
+            }
+        }
+    }
+    return t;
+}
+
+// The most tiles of BM rows that R rows of E experts can make
+inline int64_t most_row_tiles(int64_t R, int64_t E, int BM) {
+    return (R + (E < R ? E : R) * (BM - 1)) / BM;
+}
+
+// gemm_grouped_rows.hip: tiles of 16 or 32 rows, every size
+hero_status launch_grouped_rows(const GroupedArgs& a, hero_dtype adt, int tile, hipStream_t st);
+
+}  // namespace hero_gemm

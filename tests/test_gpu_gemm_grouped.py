@@ -1,0 +1,253 @@
+"""The products grouped by expert against the oracle's product, expert by expert (INT8 element by element), and against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import moe_reference as R
+import oracle as O
+from paper_2310_17723_amd import binding as HB
+from parity import to_np
+
+pytestmark = pytest.mark.gpu
+
+TILES = [None, 16, 32]                                                    # the library's choice of a kernel, and each kernel
+HP = {"bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _offsets(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+
+
+class Problem:
+    """Rows of experts with `counts` rows each, `behind` more in the result that belong to none; tokens: rows to gather from."""
+
+    def __init__(self, fmt, counts, N, K, tokens=0, behind=3, seed=0, row_scale=None, bias=True, stride=0, ldc=0):
+        rng = np.random.default_rng(seed)
+        E = len(counts)
+        self.fmt, self.N, self.K, self.E = fmt, N, K, E
+        self.R = int(sum(counts)) + behind
+        self.offsets = _offsets(counts)
+        n = tokens or self.R
+        self.row_index = rng.integers(0, tokens, self.R).astype(np.int32) if tokens else None
+        if fmt == "i8":
+            self.A, self.W = (rng.integers(-127, 128, s).astype(np.int8) for s in ((n, K), (E, N, K)))
+        elif fmt == "e4m3":
+            self.A, self.W = (O.f32_to_e4m3((rng.standard_normal(s) * 60).astype(np.float32)) for s in ((n, K), (E, N, K)))
+        else:
+            self.A, self.W = torch.randn((n, K), generator=torch.Generator().manual_seed(seed)).to(HP[fmt]), \
+                (torch.randn((E, N, K), generator=torch.Generator().manual_seed(seed + 1)) / K ** 0.5).to(HP[fmt])
+        one = 1.0 / (73.0 * 73.0 * K ** 0.5) if fmt == "i8" else 1.0 / (60.0 * 60.0 * K ** 0.5)
+        self.rs = rng.uniform(0.5, 2.0, n).astype(np.float32) if (tokens if row_scale is None else row_scale) else None
+        self.cs = (rng.uniform(0.5, 2.0, (E, N)) * one).astype(np.float32)
+        self.bias = (rng.standard_normal((E, N)) * 0.3).astype(np.float32) if bias else None
+        self.os = rng.uniform(0.01, 0.05, (E, N)).astype(np.float32)
+        self.ldc, self.stride = ldc, stride
+
+    def _dev(self, a, pad=0):
+        if a is None:
+            return None
+        t = a.clone() if isinstance(a, torch.Tensor) else torch.from_numpy(np.ascontiguousarray(a))
+        if pad:                                                           # rows further apart, what lies between them is not to matter
+            wide = torch.full((*t.shape[:-1], t.shape[-1] + pad), 127, dtype=torch.uint8 if t.dtype == torch.uint8 else t.dtype)
+            wide[..., :t.shape[-1]] = t
+            return wide.cuda()[..., :t.shape[-1]]
+        return t.cuda()
+
+    def run(self, hero, epi="dequant", hp="bf16", tile=None, out=None, offsets=None, stream=None):
+        e = R.EPI_OF[epi]
+        A, W = self._dev(self.A, self.stride), self._dev(self.W, self.stride)
+        dt = HP[self.fmt] if self.fmt in HP else HP[hp] if epi in ("dequant", "gelu") else torch.int8 if self.fmt == "i8" else torch.float8_e4m3fn
+        if out is None:
+            wide = torch.full((self.R, (self.ldc or self.N) + (-(self.ldc or self.N)) % 4), 91, dtype=torch.uint8, device="cuda").repeat_interleave(dt.itemsize, 1)
+            out = wide.view(dt)[:, :self.N]
+        off = self._dev(self.offsets if offsets is None else offsets)
+        kw = dict(row_index=self._dev(self.row_index), bias=self._dev(self.bias), C_out=out, tile=tile, stream=stream)
+        if self.fmt in HP:
+            return hero.hero_hp_gemm_grouped(A, W, off, gelu=epi == "gelu", **kw)
+        fn = hero.hero_int8_gemm_grouped if self.fmt == "i8" else hero.hero_fp8_gemm_grouped
+        return fn(A, W, off, a_row_scale=self._dev(self.rs), b_col_scale=self._dev(self.cs), epi=e,
+                  out_col_scale=self._dev(self.os) if epi == "gelu_requant" else None, **kw)
+
+    def check(self, got, epi="dequant", offsets=None):
+        off = self.offsets if offsets is None else offsets
+        at = R.clean_offsets(off, self.R)
+        raw = got.view(torch.uint8) if got.dtype.itemsize == 1 else got.view(torch.int16)
+        sentinel = 91 if got.dtype.itemsize == 1 else 91 * 257
+        for rows in (slice(0, at[0]), slice(at[-1], self.R)):
+            assert (raw[rows] == sentinel).all(), "rows that belong to no expert"
+        base = got._base if got._base is not None else got
+        if base.dim() == 2 and base.view(torch.uint8).shape[1] > self.N * got.dtype.itemsize:
+            assert (base.view(torch.uint8)[:, self.N * got.dtype.itemsize:] == 91).all(), "columns behind the last"
+        if self.fmt in HP:
+            return self._check_hp(got, epi, off)
+        if self.fmt == "e4m3":
+            return self._check_f8(got, epi, off)
+        c_dt = {torch.bfloat16: O.BF16, torch.float16: O.F16, torch.int8: O.I8}[got.dtype]
+        ref = R.product8("i8", self.A, self.W, off, self.row_index, self.rs, self.cs, self.bias, R.EPI_OF[epi], self.os, c_dt)
+        g = to_np(got)
+        for e, (rows, want) in ref.items():
+            have = g[rows]
+            if epi in ("dequant", "requant"):                             # the bit-exact class
+                assert np.array_equal(have.view(np.uint8), want.view(np.uint8)), (e, rows, np.argwhere(have != want)[:4])
+            elif epi == "gelu_requant":                                   # one step, next to a border (GELU and 1 / S_a in fp32: a few 2^-24 of 127)
+                d = np.abs(have.astype(int) - want.astype(int))
+                assert d.max() <= 1 and (d > 0).mean() <= max(1e-3, 2.0 / d.size), (e, d.max(), (d > 0).mean())
+            else:                                                         # gelu's fp32 form is off by 1.1e-7, then the result's type
+                x, y = (O.hp_to_f32(v, c_dt).astype(np.float64) for v in (have, want))
+                assert (np.abs(x - y) <= 2 * R.EPS[got.dtype] * np.abs(y) + 2.0 ** -22).all(), e
+
+    def _check_f8(self, got, epi, off):
+        """The matrix cores add a group of eight products with 13 fractional bits below the largest: off by 8 * 2^-13 of it at most, so by 2^-10 of
+        sum |a w| over all; the additions between groups by K 2^-24 of it."""
+        at, src = R.clean_offsets(off, self.R), R.sources(self.row_index, self.R, self.A.shape[0])
+        for e in range(self.E):
+            if at[e] == at[e + 1]:
+                continue
+            rows = src[at[e]:at[e + 1]]
+            a, w = O.e4m3_to_f32(self.A[rows]).astype(np.float64), O.e4m3_to_f32(self.W[e]).astype(np.float64)
+            s = (self.rs[rows].astype(np.float64)[:, None] if self.rs is not None else 1.0) * self.cs[e].astype(np.float64)
+            y = a @ w.T * s + (self.bias[e] if self.bias is not None else 0.0)
+            slack = (2.0 ** -10 + (self.K + 4) * 2.0 ** -24) * (np.abs(a) @ np.abs(w).T) * s + 2.0 ** -23 * np.abs(y)
+            if epi in ("gelu", "gelu_requant"):                           # |GELU'| < 1.13
+                y, slack = R.gelu(torch.from_numpy(y)).numpy(), 1.13 * slack + 2.0 ** -22
+            if epi == "gelu_requant":
+                y, slack = y / self.os[e], slack / self.os[e] * (1 + 2.0 ** -22)
+            half = {torch.float8_e4m3fn: 2.0 ** -4, **R.EPS}[got.dtype]
+            tiny = 2.0 ** -10 if got.dtype == torch.float8_e4m3fn else 2.0 ** -25
+            if got.dtype == torch.float8_e4m3fn:
+                y = np.clip(y, -448, 448)
+            x = got[at[e]:at[e + 1]].float().cpu().double().numpy()
+            bound = slack + half * (np.abs(y) + slack) + tiny
+            assert (np.abs(x - y) <= bound).all(), (e, np.max(np.abs(x - y) / bound))
+
+    def _check_hp(self, got, epi, off):
+        bias = None if self.bias is None else torch.from_numpy(self.bias)
+        for e, (rows, y, mag) in R.product_hp(self.A, self.W, off, self.row_index, bias, epi == "gelu").items():
+            # fp32 sums of K products: (K + 2) 2^-24 of sum |a w|; GELU's slope is below 1.13 and its form off by 1.1e-7
+            bound = 1.13 * (self.K + 2) * 2.0 ** -24 * mag + (R.EPS[got.dtype] + 2.0 ** -23) * y.abs() + 2.0 ** -22
+            d = (got[rows].double().cpu() - y).abs()
+            assert bool((d <= bound).all()), (e, float((d / bound).max()))
+
+
+COUNTS = [[1], [0, 3, 0, 16, 1], [17, 0, 0, 40, 15, 33, 16], [5] * 70, [0, 0, 130], [257, 1, 64, 0]]
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("fmt", ["i8", "e4m3", "bf16", "f16"])
+@pytest.mark.parametrize("counts", COUNTS, ids=str)
+def test_rows_of_experts(hero, counts, fmt, tile):
+    for i, (N, K, tokens) in enumerate(((64, 256, 0), (100, 512, 50), (259, 128, 7))):
+        p = Problem(fmt, counts, N, K, tokens, seed=i)
+        for epi in ("dequant", "gelu"):
+            p.check(p.run(hero, epi, ("bf16", "f16")[i % 2], tile), epi)
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("epi", ["requant", "gelu_requant"])
+def test_8_bit_results(hero, fmt, epi, tile):
+    for i, (N, K, tokens) in enumerate(((64, 320, 0), (130, 1024, 33), (257, 576, 9))):
+        p = Problem(fmt, [20, 0, 1, 70], N, K, tokens, seed=i)
+        p.cs *= 30 if epi == "requant" else 1
+        p.check(p.run(hero, epi, tile=tile), epi)
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("fmt", ["i8", "e4m3", "bf16"])
+@pytest.mark.parametrize("K", [64, 128, 192, 448, 1088, 4096])
+def test_lengths_of_k(hero, fmt, K, tile):
+    """Odd numbers of 64-byte pieces, fewer pieces than waves, many."""
+    p = Problem(fmt, [9, 33], 72, K, 20, seed=K)
+    p.check(p.run(hero, tile=tile))
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("fmt", ["i8", "e4m3", "f16"])
+def test_strides_and_missing_vectors(hero, fmt, tile):
+    p = Problem(fmt, [9, 0, 33], 70, 320, 20, seed=1, stride=32, ldc=84)
+    p.check(p.run(hero, tile=tile))
+    p = Problem(fmt, [9, 0, 33], 70, 320, 0, seed=2, bias=False, row_scale=False)
+    p.check(p.run(hero, tile=tile))
+    p = Problem(fmt, [9, 0, 33], 70, 320, 0, seed=2, row_scale=True)
+    p.check(p.run(hero, tile=tile))
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("N", [1, 2, 3, 5, 15, 17, 31, 33])
+def test_few_columns(hero, N, tile):
+    for fmt in ("i8", "bf16"):
+        p = Problem(fmt, [3, 18], N, 192, 5, seed=N)
+        p.check(p.run(hero, tile=tile))
+    p = Problem("i8", [3, 18], N, 192, 5, seed=N)
+    p.cs *= 30
+    p.check(p.run(hero, "requant", tile=tile), "requant")
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_many_experts_and_empty_ones(hero, tile):
+    rng = np.random.default_rng(3)
+    for E in (63, 64, 65, 128, 300, 512):
+        counts = rng.integers(0, 4, E) * (rng.random(E) < 0.5)
+        p = Problem("i8", counts.tolist(), 32, 128, 11, seed=E)
+        p.check(p.run(hero, tile=tile))
+    p = Problem("i8", [0] * 12, 32, 128, behind=9)
+    p.check(p.run(hero, tile=tile))
+    p = Problem("i8", [0] * 511 + [40], 32, 128, behind=0)
+    p.check(p.run(hero, tile=tile))
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_offsets_and_indices_that_are_wrong_stay_in_bounds(hero, tile):
+    """Offsets are taken as their running maximum within [0, R], row indices clamped."""
+    p = Problem("i8", [10, 20, 30, 5], 48, 256, 13, behind=7, seed=1)
+    p.row_index[5], p.row_index[6], p.row_index[30] = -4, 13, 2 ** 31 - 1
+    for off in ([0, 10, 30, 60, 65], [3, 10, 10, 50, 60], [0, 30, 10, 60, 20], [-5, 7, -2 ** 31, 90, 2 ** 31 - 1], [72] * 5, [0] * 5, [5, 4, 3, 2, 1]):
+        off = np.array(off, np.int32)
+        p.check(p.run(hero, tile=tile, offsets=off), offsets=off)
+    p = Problem("i8", [1] * 200, 32, 128, behind=50, seed=1)
+    off = np.random.default_rng(1).integers(-20, 300, 201).astype(np.int32)
+    p.check(p.run(hero, tile=tile, offsets=off), offsets=off)
+
+
+def test_int8_results_do_not_depend_on_the_kernel_and_equal_the_ungrouped_product(hero):
+    p = Problem("i8", [70, 3, 0, 150], 200, 512, 40, seed=6)
+    p.cs *= 30
+    outs = [p.run(hero, "requant", tile=t) for t in TILES]
+    assert all(torch.equal(outs[0], o) for o in outs[1:])
+    A, idx = torch.from_numpy(p.A).cuda(), torch.from_numpy(p.row_index).cuda().long()
+    for e in range(p.E):
+        rows = slice(p.offsets[e], p.offsets[e + 1])
+        if rows.start < rows.stop:
+            want = hero.hero_int8_gemm(A[idx[rows]].contiguous(), torch.from_numpy(p.W[e]).cuda(), torch.from_numpy(p.rs).cuda()[idx[rows]].contiguous(),
+                                       torch.from_numpy(p.cs[e]).cuda(), torch.from_numpy(p.bias[e]).cuda(), epi=HB.EPI_REQUANT, out_dtype=torch.int8)
+            assert torch.equal(outs[0][rows], want)
+
+
+def test_other_stream_and_replayed_with_other_offsets(hero):
+    p = Problem("i8", [10, 0, 25, 7], 96, 256, 30, behind=20, seed=8)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        p.check(p.run(hero, stream=side))
+    A, W, cs, rs, b, idx = (torch.from_numpy(x).cuda() for x in (p.A, p.W, p.cs, p.rs, p.bias, p.row_index))
+    off = torch.from_numpy(p.offsets).cuda()
+    out = torch.empty((p.R, p.N), dtype=torch.bfloat16, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hero.hero_int8_gemm_grouped(A, W, off, row_index=idx, a_row_scale=rs, b_col_scale=cs, bias=b, C_out=out)
+    for counts in ([0, 0, 0, 62], [16, 16, 16, 14], [1, 0, 0, 0]):
+        o = _offsets(counts)
+        off.copy_(torch.from_numpy(o))
+        out.view(torch.int16).fill_(91 * 257)
+        graph.replay()
+        torch.cuda.synchronize()
+        p.check(out, offsets=o)
+
+
+def test_nothing_to_do(hero):
+    z = lambda *s, dt=torch.int8: torch.empty(s, dtype=dt, device="cuda")  # noqa: E731
+    off = torch.zeros(4, dtype=torch.int32, device="cuda")
+    cs = torch.ones((3, 8), device="cuda")
+    assert hero.hero_int8_gemm_grouped(z(0, 64), z(3, 8, 64), off, b_col_scale=cs).shape == (0, 8)
+    assert hero.hero_int8_gemm_grouped(z(5, 64), z(3, 0, 64), off, b_col_scale=cs[:, :0].contiguous()).shape == (5, 0)
+    assert hero.hero_int8_gemm_grouped(z(5, 64), z(0, 8, 64), off[:1], b_col_scale=cs[:0]).shape == (5, 8)
