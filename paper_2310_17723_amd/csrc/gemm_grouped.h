@@ -85,6 +85,44 @@ __device__ __forceinline__ GroupTile group_tile(const GroupedArgs& a, int xcd, i
     return t;
 }
 
+// The tables of the tile kernels (in LDS, whole waves): row_begin [E + 1], tiles_upto [E] filled up to a multiple of 64 with the number of all
+// row tiles, which is returned.
+template <int BM>
+__device__ __forceinline__ int expert_tables(const GroupedArgs& a, int* row_begin, int* tiles_upto, int lane) {
+    int carry = 0, tiles = 0;
+    for (int e0 = 0; e0 < a.E; e0 += 64) {
+        int begin, end;
+        expert_rows(a, e0, lane, carry, begin, end);
+        const int upto = tiles + wave_scan_sum((end - begin + BM - 1) / BM);
+        if (e0 + lane <= a.E) row_begin[e0 + lane] = begin;
+        if (e0 + lane + 1 == a.E) row_begin[a.E] = end;
+        tiles_upto[e0 + lane] = upto;
+        carry = __builtin_amdgcn_readlane(end, 63);
+        tiles = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return tiles;
+}
+
+// Tile number s: rows [m0, min(m0 + BM, end)) of expert e.  Eight row tiles of an expert run through its columns together (tile_from_seq's order).
+struct ExpertTile { int e, m0, end, col_tile; };
+template <int BM>
+__device__ __forceinline__ ExpertTile expert_tile(const GroupedArgs& a, const int* row_begin, const int* tiles_upto, int s, int lane) {
+    const int ntn = a.g.ntn, at = s / ntn;
+    int e0 = 0;
+    unsigned long long beyond = __ballot(tiles_upto[lane] > at);
+    while (!beyond) { e0 += 64; beyond = __ballot(tiles_upto[e0 + lane] > at); }       // (s is a tile: there is one)
+    const int e = e0 + __ffsll(beyond) - 1;
+    const int first = __builtin_amdgcn_readfirstlane(e ? tiles_upto[e - 1] : 0), mt = __builtin_amdgcn_readfirstlane(tiles_upto[e]) - first;
+    const int begin = __builtin_amdgcn_readfirstlane(row_begin[e]), in = s - first * ntn;
+    const int grp = in / (GROUP_M * ntn), rem = in - grp * (GROUP_M * ntn), rows = min(mt - grp * GROUP_M, GROUP_M);
+    ExpertTile t;
+    t.e = e;
+    t.m0 = begin + (grp * GROUP_M + rem % rows) * BM;
+    t.end = __builtin_amdgcn_readfirstlane(row_begin[e + 1]);
+    t.col_tile = rem / rows;
+    return t;
+}
+
 // The most tiles of BM rows that R rows of E experts can make
 inline int64_t most_row_tiles(int64_t R, int64_t E, int BM) {
     return (R + (E < R ? E : R) * (BM - 1)) / BM;
@@ -92,5 +130,11 @@ inline int64_t most_row_tiles(int64_t R, int64_t E, int BM) {
 
 // gemm_grouped_rows.hip: tiles of 16 or 32 rows, every size
 hero_status launch_grouped_rows(const GroupedArgs& a, hero_dtype adt, int tile, hipStream_t st);
+// gemm_persistent.h: tiles of 256 x 256 or 128 x 128 (`rows` 256 or 128)
+template <int ADT, int EPI, int CDT> hero_status launch_grouped_tile(const GroupedArgs& a, int rows, hipStream_t st);
+// The sizes that it takes: whole slabs, enough of them, and 32-bit offsets per lane (of a tile's rows, or of all rows that may be gathered)
+inline bool grouped_tile_ok(const GroupedArgs& a) {
+    return a.g.K % (2 * BK) == 0 && a.g.K >= 8 * BK && a.g.lda < (1 << 24) && a.g.ldb < (1 << 24) && (!a.row_index || (int64_t)a.MA * a.g.lda <= (1LL << 32));
+}
 
 }  // namespace hero_gemm

@@ -1,6 +1,6 @@
 // int8_gemm_persistent_kernel: large problems of every operand type (instantiated per type in gemm_persistent_*.hip).
 #pragma once
-#include "gemm_common.h"
+#include "gemm_grouped.h"
 
 namespace hero_gemm {
 
@@ -39,8 +39,20 @@ constexpr int pair_loads_behind(bool odd, int na, int nb, int la, int lb) {
     return c;
 }
 
-template <int BM, int BN, int WM, int WN, int NSA, int NSB, int EPI, int CDT, int RDT, int ADT = HERO_I8, bool PART = false, bool STEADY = false>
-__global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(GemmArgs g) {
+// GROUPED (hero_int8_gemm_grouped and its like): the tiles are those of every expert's rows.  Which rows an expert has lies on the device, so every
+// workgroup works out the list of row tiles for itself (two tables in LDS) and looks a tile up where a stream moves on to it.
+// GATHER: the activations' rows come from anywhere.  Their numbers and scales are fetched by direct loads too, a tile's numbers together with the
+// vectors of the tile before it, so that no wait for them stands in the loop (KT >= 8: they have landed when the streams move on).
+template <bool GROUPED> struct PersistentArgs { using type = GemmArgs; };
+template <> struct PersistentArgs<true> { using type = GroupedArgs; };
+__device__ __forceinline__ const GemmArgs& gemm_of(const GemmArgs& g) { return g; }
+__device__ __forceinline__ const GemmArgs& gemm_of(const GroupedArgs& a) { return a.g; }
+
+template <int BM, int BN, int WM, int WN, int NSA, int NSB, int EPI, int CDT, int RDT, int ADT = HERO_I8, bool PART = false, bool STEADY = false, bool GROUPED = false, bool GATHER = false>
+__global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(typename PersistentArgs<GROUPED>::type args) {
+    const GemmArgs& g = gemm_of(args);
+    static_assert(!GROUPED || (!PART && !STEADY && RDT < 0), "grouped products: whole, without a residual");
+    static_assert(GROUPED || !GATHER, "rows are gathered in grouped products");
     constexpr bool UNIT = ADT == HERO_BF16 || ADT == HERO_F16;      // 16-bit operands: no scales, y = acc + bias
     constexpr bool WIDE = ADT == HERO_F8E4M3;                       // 32 x 32 tiles; INT8 and 16 bits: 16 x 16 (mfma16_step)
     using ACC = typename std::conditional<WIDE, v16f, typename Acc4Of<ADT>::type>::type;
@@ -58,17 +70,40 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
     constexpr int SVF = 4 * BN;                                  // floats per vector set: column scale, bias, S_a, row scale
     static_assert(BM <= BN, "the row-scale vector shares the column vectors' length");
     constexpr int PF_OFF = RING + 2 * SVF * 4;                   // 256 bytes per wave where the prefetch requests land (never read)
-    static_assert(PF_OFF + NWAVE * 256 <= 160 * 1024, "LDS budget");
-    __shared__ __attribute__((aligned(1024))) int8_t smem[PF_OFF + NWAVE * 256];
+    constexpr int INDEX_OFF = PF_OFF, TABLE_OFF = INDEX_OFF + (GATHER ? 2 * BM * 4 : 0);    // GROUPED: row numbers of two tiles; the experts' tables
+    constexpr int LDS = GROUPED ? TABLE_OFF + (2 * MAX_EXPERTS + 1) * 4 : PF_OFF + NWAVE * 256;
+    static_assert(LDS <= 160 * 1024, "LDS budget");
+    __shared__ __attribute__((aligned(1024))) int8_t smem[LDS];
     float* const sv0 = reinterpret_cast<float*>(smem + RING);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int xcd = blockIdx.x % NUM_XCD, slot = blockIdx.x / NUM_XCD, nslot = gridDim.x / NUM_XCD;
-    const int ntiles = g.ntm * g.ntn;
-    const int seq_end = min((xcd + 1) * g.per_xcd, PART ? ntiles * g.ksplit : ntiles);
-    int seq = xcd * g.per_xcd + slot;                            // this workgroup's tiles: seq, seq + nslot, ...
+    int ntiles = g.ntm * g.ntn, per_xcd = g.per_xcd;
+    int* const row_begin = reinterpret_cast<int*>(smem + TABLE_OFF);     // GROUPED: expert e's rows are row_begin[e] .. row_begin[e + 1] - 1,
+    int* const tiles_upto = row_begin + MAX_EXPERTS + 1;                 // the row tiles of experts 0 .. e are tiles_upto[e] in number
+    int* const row_number = reinterpret_cast<int*>(smem + INDEX_OFF);    // GATHER: [parity of the tile][row]
+    if constexpr (GROUPED) {
+        ntiles = expert_tables<BM>(args, row_begin, tiles_upto, lane) * g.ntn;      // (every wave writes the same)
+        per_xcd = (ntiles + NUM_XCD - 1) / NUM_XCD;
+        __syncthreads();
+    }
+    const int seq_end = min((xcd + 1) * per_xcd, PART ? ntiles * g.ksplit : ntiles);
+    int seq = xcd * per_xcd + slot;                              // this workgroup's tiles: seq, seq + nslot, ...
     if (seq >= seq_end) return;
+    // tile number s: its origin, where its rows end, its expert
+    struct Tile { int m0, n0, end, e; };
+    auto tile_at = [&](int s) {
+        Tile t;
+        if constexpr (GROUPED) {
+            const ExpertTile x = expert_tile<BM>(args, row_begin, tiles_upto, s, lane);
+            t.e = x.e; t.m0 = x.m0; t.end = x.end; t.n0 = x.col_tile * BN;
+        } else {
+            tile_from_seq<BM, BN>(g, PART ? s % ntiles : s, t.m0, t.n0);
+            t.end = g.M; t.e = 0;
+        }
+        return t;
+    };
     // PART: sequence number s is tile s % ntiles of K range s / ntiles (g.kslabs pairs of slabs, the last range may be shorter)
     auto range_slabs = [&](int s) { return PART ? 2 * min(g.kslabs, g.K / (2 * BK) - s / ntiles * g.kslabs) : g.K / BK; };
     const bool has_last = A_EVEN || wave < A_LAST;
@@ -92,29 +127,40 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
     int aseq = seq, akt = 0, aKT, bseq = seq, bkt = 0, bKT, bpar = 0;
     const int8_t* ia; const int8_t* ib;                          // wave-uniform: tile base + slab offset
     uint32_t oa[A_UNITS], ob[B_UNITS];
-    int m0b = 0, n0b = 0;                                        // origin of B's tile
+    Tile tb{0, 0, 0, 0};                                         // B's tile
+    int apar = 0;                                                // GATHER: parity of A's tile
     auto range_start = [&](int s) { return PART ? (int64_t)(s / ntiles) * g.kslabs * (2 * BK) : (int64_t)0; };
+    auto source = [&](int r) {                                   // a row number, within the rows that there are
+        if constexpr (GROUPED) return (uint32_t)min(max(r, 0), args.MA - 1);
+        else return (uint32_t)r;
+    };
+    auto set_rows = [&](const Tile& t, int s, int p) {
+        if constexpr (GATHER) {
+            ia = g.A;
+#pragma unroll
+            for (int u = 0; u < A_UNITS; ++u)                    // (units beyond a tile of odd height are not loaded)
+                oa[u] = source(row_number[p * BM + min(lrow + u * (NWAVE * 16), BM - 1)]) * (uint32_t)g.lda + lc;
+        } else {
+            ia = g.A + (int64_t)t.m0 * g.lda + range_start(s);
+#pragma unroll
+            for (int u = 0; u < A_UNITS; ++u) oa[u] = (uint32_t)min(lrow + u * (NWAVE * 16), t.end - 1 - t.m0) * (uint32_t)g.lda + lc;
+        }
+    };
     auto set_tile_a = [&](int s) {
         if constexpr (!ONE) {
-            int m0, n0;
-            tile_from_seq<BM, BN>(g, PART ? s % ntiles : s, m0, n0);
+            const Tile t = tile_at(s);
             aKT = range_slabs(s);
-            ia = g.A + (int64_t)m0 * g.lda + range_start(s);
-#pragma unroll
-            for (int u = 0; u < A_UNITS; ++u) oa[u] = (uint32_t)min(lrow + u * (NWAVE * 16), g.M - 1 - m0) * (uint32_t)g.lda + lc;
+            set_rows(t, s, apar);
         }
     };
     auto set_tile_b = [&](int s) {
-        tile_from_seq<BM, BN>(g, PART ? s % ntiles : s, m0b, n0b);
-        if constexpr (ONE) {
-            ia = g.A + (int64_t)m0b * g.lda + range_start(s);
-#pragma unroll
-            for (int u = 0; u < A_UNITS; ++u) oa[u] = (uint32_t)min(lrow + u * (NWAVE * 16), g.M - 1 - m0b) * (uint32_t)g.lda + lc;
-        }
+        tb = tile_at(s);
+        if constexpr (ONE) set_rows(tb, s, bpar);
         bKT = range_slabs(s);
-        ib = g.Bt + (int64_t)n0b * g.ldb + range_start(s);
+        ib = g.Bt + (int64_t)tb.n0 * g.ldb + range_start(s);
+        if constexpr (GROUPED) ib += (int64_t)tb.e * args.expert_stride;
 #pragma unroll
-        for (int u = 0; u < B_UNITS; ++u) ob[u] = (uint32_t)min(lrow + u * (NWAVE * 16), g.N - 1 - n0b) * (uint32_t)g.ldb + lcb;
+        for (int u = 0; u < B_UNITS; ++u) ob[u] = (uint32_t)min(lrow + u * (NWAVE * 16), g.N - 1 - tb.n0) * (uint32_t)g.ldb + lcb;
     };
     // The epilogue vectors of B's tile go out together with its FIRST pair, not when the stream
     // moves on to the tile: their buffer (parity of the tile) is still being read by the epilogue of the tile
@@ -125,14 +171,24 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
         static_assert(NWAVE == 2 * CH, "two vectors per wave");
         const int ch = (wave % CH) * 64, which = wave / CH;
         const uint32_t dst = svbase + par * SVF * 4 + ch * 4;
-        const uint32_t cn = (uint32_t)min(ch + lane, g.N - 1 - n0b) * 4u, cm = (uint32_t)min(ch + lane, g.M - 1 - m0b) * 4u;
+        const int vm = GATHER ? 0 : tb.m0;
+        const int64_t vn = GROUPED ? (int64_t)tb.e * g.N + tb.n0 : (int64_t)tb.n0;
+        const uint32_t cn = (uint32_t)min(ch + lane, g.N - 1 - tb.n0) * 4u;
+        const uint32_t cm = GATHER ? source(row_number[par * BM + min(ch + lane, BM - 1)]) * 4u : (uint32_t)min(ch + lane, tb.end - 1 - tb.m0) * 4u;
         if (EPI == HERO_EPI_RAW_I32) return;
         if (which == 0) {
-            if (!UNIT) dma4s(cn, g.b_col_scale + n0b, dst);
-            if (EPI == HERO_EPI_GELU_REQUANT) dma4s(cn, g.out_col_scale + n0b, dst + 2 * BN * 4);
+            if (!UNIT) dma4s(cn, g.b_col_scale + vn, dst);
+            if (EPI == HERO_EPI_GELU_REQUANT) dma4s(cn, g.out_col_scale + vn, dst + 2 * BN * 4);
         } else {
-            if (has_bias) dma4s(cn, g.bias + n0b, dst + BN * 4);
-            if (has_rs) dma4s(cm, g.a_row_scale + m0b, dst + 3 * BN * 4);
+            if (has_bias) dma4s(cn, g.bias + vn, dst + BN * 4);
+            if (has_rs) dma4s(cm, g.a_row_scale + vm, dst + 3 * BN * 4);
+        }
+        if constexpr (GATHER) {                                  // the next tile's row numbers, a wave for every 64
+            if (which == 0 && ch < BM && bseq + nslot < seq_end) {
+                const Tile t = tile_at(bseq + nslot);
+                dma4s((uint32_t)min(ch + lane, t.end - 1 - t.m0) * 4u, reinterpret_cast<const float*>(args.row_index + t.m0),
+                      __builtin_amdgcn_readfirstlane(lds_offset(row_number + (par ^ 1) * BM + ch)));
+            }
         }
     };
     // A stream moves in PAIRS of slabs (128 bytes of every row = one cache line): the two 64-byte halves of a line are requested back
@@ -161,7 +217,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
         akt += 2;
         if (akt < aKT) { ia += 2 * BK; return; }
         if (aseq + nslot < seq_end) {
-            aseq += nslot; akt = 0;
+            aseq += nslot; akt = 0; apar ^= 1;
             set_tile_a(aseq);
         } else akt = aKT - 2;
     };
@@ -194,6 +250,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
 
     // prologue: what the iterations before the first would have issued, in their order; slab 0 landed
     constexpr int LA = 2 * A_UNITS, LB = 2 * B_UNITS;
+    if constexpr (GATHER) {                                      // the first tile's row numbers
+        const Tile t = tile_at(seq);
+        if (tid < BM) row_number[tid] = args.row_index[t.m0 + min(tid, t.end - 1 - t.m0)];
+        __syncthreads();
+    }
     set_tile_a(seq);
     set_tile_b(seq);
 #pragma unroll
@@ -217,8 +278,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
 
     int rda = 0, rdb = 0, par = 0;                                  // LDS offsets of the current slab
     for (;;) {
-        int m0, n0;
-        tile_from_seq<BM, BN>(g, PART ? seq % ntiles : seq, m0, n0);
+        const Tile tile = tile_at(seq);
+        const int m0 = tile.m0, n0 = tile.n0;
         const int KT = range_slabs(seq);
         constexpr int CI = WIDE ? TM : TI, CJ = WIDE ? TN : TJ, CR = WIDE ? 16 : 4;
         ACC acc[CI][CJ];
@@ -363,7 +424,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
         // waits of the next main loop only count loads issued after these, and the epilogue in between is far
         // longer than a miss).  What the request brings is the line: into this XCD's L2 and, on its way, into the
         // memory-side cache, where the next kernel's first tiles would otherwise all miss at once.
-        if (g.pf_lines > 0) {
+        if (!GROUPED && g.pf_lines > 0) {
             const int w0 = wave * 64;
             if (w0 < g.pf_lpt) {
                 const uint32_t line = (uint32_t)min(seq * g.pf_lpt + w0 + lane, g.pf_lines - 1);
@@ -384,7 +445,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(G
 #pragma unroll
         for (int i = 0; i < CI; ++i)
             rsr[i] = (EPI != HERO_EPI_RAW_I32 && has_rs) ? sv[3 * BN + wm * (BM / WM) + i * (WIDE ? 32 : 16) + (HP || STEADY ? el & 15 : WIDE ? ml : r16)] : 1.0f;
-        if constexpr (WIDE) epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, true, UNIT>(g, acc, sv, rsr, m0, n0, tid);
+        if constexpr (GROUPED) {
+            GemmArgs ge = g;
+            ge.M = tile.end;                                       // (the rows behind are another expert's)
+            if constexpr (WIDE) epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, true, UNIT>(ge, acc, sv, rsr, m0, n0, tid);
+            else if constexpr (HP) epilogue_rows16_hp<BM, BN, WM, WN, EPI, CDT, RDT, UNIT>(ge, acc, sv, rsr, m0, n0, wave, el);
+            else epilogue_rows16<BM, BN, WM, WN, EPI, CDT, UNIT>(ge, acc, sv, rsr, m0, n0, tid);
+        } else if constexpr (WIDE) epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, true, UNIT>(g, acc, sv, rsr, m0, n0, tid);
         else if constexpr (HP) epilogue_rows16_hp<BM, BN, WM, WN, EPI, CDT, RDT, UNIT>(g, acc, sv, rsr, m0, n0, wave, el);
         else if constexpr (PART) {
             GemmArgs gp = g;
@@ -477,7 +544,38 @@ hero_status launch_persistent_part(const GemmArgs& g, int rows, hipStream_t st) 
     }
 }
 
-// what gemm_persistent_*.hip instantiate for their operand type
+// Grouped products: 256 x 256, or 128 x 128 with two workgroups per CU.  K >= 512 bytes, a multiple of 128.
+template <int ADT, int EPI, int CDT>
+hero_status launch_grouped_tile(const GroupedArgs& ga, int rows, hipStream_t st) {
+    auto go = [&](auto R, auto GATHER) {
+        constexpr int BM = decltype(R)::value, BN = BM, W = BM == 256 ? 4 : 2, NA = 4, NB = BM == 256 ? 5 : 4, PER_CU = BM == 256 ? 1 : 2;
+        GroupedArgs a = ga;
+        a.g.ntn = (a.g.N + BN - 1) / BN;
+        const int64_t tiles = most_row_tiles(a.g.M, a.E, BM) * a.g.ntn, per = (tiles + NUM_XCD - 1) / NUM_XCD;
+        if (tiles > 0x7fffff00LL) return HERO_ERR_SHAPE;
+        const int nslot = per < 32 * PER_CU ? (int)per : 32 * PER_CU;
+        hipLaunchKernelGGL((int8_gemm_persistent_kernel<BM, BN, 2, W, NA, NB, EPI, CDT, -1, ADT, false, false, true, decltype(GATHER)::value>),
+                           dim3((unsigned)(nslot * NUM_XCD)), dim3(2 * W * 64), 0, st, a);
+        return hero_launch_status();
+    };
+    using T256 = std::integral_constant<int, 256>;
+    using T128 = std::integral_constant<int, 128>;
+    if (rows == 256) return ga.row_index ? go(T256{}, std::true_type{}) : go(T256{}, std::false_type{});
+    if (rows == 128) return ga.row_index ? go(T128{}, std::true_type{}) : go(T128{}, std::false_type{});
+    return HERO_ERR_UNSUPPORTED;
+}
+
+// what gemm_persistent_*.hip and gemm_grouped_*.hip instantiate for their operand type
+#define HERO_GROUPED_8BIT(ADT, CDT8) \
+    template hero_status launch_grouped_tile<ADT, HERO_EPI_REQUANT, CDT8>(const GroupedArgs&, int, hipStream_t); \
+    template hero_status launch_grouped_tile<ADT, HERO_EPI_GELU_REQUANT, CDT8>(const GroupedArgs&, int, hipStream_t); \
+    template hero_status launch_grouped_tile<ADT, HERO_EPI_DEQUANT, HERO_BF16>(const GroupedArgs&, int, hipStream_t); \
+    template hero_status launch_grouped_tile<ADT, HERO_EPI_DEQUANT, HERO_F16>(const GroupedArgs&, int, hipStream_t); \
+    template hero_status launch_grouped_tile<ADT, HERO_EPI_DEQUANT_GELU, HERO_BF16>(const GroupedArgs&, int, hipStream_t); \
+    template hero_status launch_grouped_tile<ADT, HERO_EPI_DEQUANT_GELU, HERO_F16>(const GroupedArgs&, int, hipStream_t);
+#define HERO_GROUPED_16BIT(DT) \
+    template hero_status launch_grouped_tile<DT, HERO_EPI_DEQUANT, DT>(const GroupedArgs&, int, hipStream_t); \
+    template hero_status launch_grouped_tile<DT, HERO_EPI_DEQUANT_GELU, DT>(const GroupedArgs&, int, hipStream_t);
 #define HERO_PERSISTENT_8BIT(ADT, CDT8) \
     template hero_status launch_persistent_tile<ADT, HERO_EPI_REQUANT, CDT8, -1>(const GemmArgs&, int, hipStream_t); \
     template hero_status launch_persistent_tile<ADT, HERO_EPI_GELU_REQUANT, CDT8, -1>(const GemmArgs&, int, hipStream_t); \
