@@ -12,8 +12,16 @@ struct GroupedArgs {
     const int32_t* offsets; const int32_t* row_index;
     int E, MA;                                  // experts, rows of A
     int64_t expert_stride;                      // bytes between the weights of two experts
-    int epi, c_dt;                              // (for kernels that ask at run time)
+    int epi, c_dt;                              // (for the kernel that asks at run time)
 };
+
+// what a kernel takes that has a grouped form
+template <bool GROUPED> struct ArgsOf { using type = GemmArgs; };
+template <> struct ArgsOf<true> { using type = GroupedArgs; };
+__device__ __forceinline__ const GemmArgs& gemm_of(const GemmArgs& g) { return g; }
+__device__ __forceinline__ const GemmArgs& gemm_of(const GroupedArgs& a) { return a.g; }
+__device__ __forceinline__ bool source_is_gathered(const GemmArgs&) { return false; }
+__device__ __forceinline__ bool source_is_gathered(const GroupedArgs& a) { return a.row_index != nullptr; }
 
 // inclusive sum over the lanes of a wave
 __device__ __forceinline__ int wave_scan_sum(int x) {
@@ -128,13 +136,36 @@ inline int64_t most_row_tiles(int64_t R, int64_t E, int BM) {
     return (R + (E < R ? E : R) * (BM - 1)) / BM;
 }
 
-// gemm_grouped_rows.hip: tiles of 16 or 32 rows, every size
-hero_status launch_grouped_rows(const GroupedArgs& a, hero_dtype adt, int tile, hipStream_t st);
+// Which kernel: the numbers of include/hero_debug.h (hero_gemm_grouped_tile)
+enum GroupedForm { GROUPED_ANY = 1, GROUPED_RING = 16 /* + RingForm */, GROUPED_128 = 128, GROUPED_256 = 256 };
+// gemm_grouped_rows.hip: every size
+hero_status launch_grouped_rows(const GroupedArgs& a, hero_dtype adt, hipStream_t st);
+// gemm_ring.h: one tile per workgroup
+template <int ADT, int EPI, int CDT> hero_status launch_grouped_ring(const GroupedArgs& a, RingForm f, hipStream_t st);
 // gemm_persistent.h: tiles of 256 x 256 or 128 x 128 (`rows` 256 or 128)
 template <int ADT, int EPI, int CDT> hero_status launch_grouped_tile(const GroupedArgs& a, int rows, hipStream_t st);
-// The sizes that it takes: whole slabs, enough of them, and 32-bit offsets per lane (of a tile's rows, or of all rows that may be gathered)
-inline bool grouped_tile_ok(const GroupedArgs& a) {
-    return a.g.K % (2 * BK) == 0 && a.g.K >= 8 * BK && a.g.lda < (1 << 24) && a.g.ldb < (1 << 24) && (!a.row_index || (int64_t)a.MA * a.g.lda <= (1LL << 32));
+// The sizes that the ring kernel takes: whole slabs, and 32-bit offsets per lane (of a tile's rows, or of all rows that may be gathered)
+inline bool grouped_ring_ok(const GroupedArgs& a) {
+    return a.g.K % (2 * BK) == 0 && ring_ok(a.g.lda, a.g.ldb) && (!a.row_index || (int64_t)a.MA * a.g.lda <= (1LL << 32));
+}
+// .. and the persistent kernel, which looks ahead
+inline bool grouped_tile_ok(const GroupedArgs& a) { return grouped_ring_ok(a) && a.g.K >= 8 * BK; }
+
+inline int grouped_form(const GroupedArgs& a) {
+    const int64_t R = a.g.M, N = a.g.N, active = a.E < R ? a.E : R, n = R / active;       // rows of an expert, were none empty
+    auto cols = [&](int bn) { return (N + bn - 1) / bn; };
+    auto tiles = [&](int bm, int bn) { return (n <= bm / 2 ? active : (R + active * bm / 2) / bm) * cols(bn); };      // (the last tile of an expert: half full)
+    if (!grouped_ring_ok(a)) return GROUPED_ANY;
+    const bool pers = grouped_tile_ok(a);
+    if (n <= 32) {
+        if (active * cols(32) <= 320) return GROUPED_RING + RING_32x32_K4;
+        if (active * cols(64) <= 256) return GROUPED_RING + RING_32x64_K2;
+    }
+    if (n <= 48 && active * cols(64) <= 256) return GROUPED_RING + RING_64x64_K2;
+    if (n <= 20 || (n <= 48 && active * cols(128) < 512) || !pers) return GROUPED_RING + (n <= 48 ? RING_64x64 : RING_128x64);
+    const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
+    if (n <= 160 && t128 < 512) return GROUPED_RING + RING_128x64;
+    return 9 * ((t128 + 255) / 256) <= 25 * ((t256 + 255) / 256) ? GROUPED_128 : GROUPED_256;
 }
 
 }  // namespace hero_gemm

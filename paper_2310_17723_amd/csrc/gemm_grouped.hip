@@ -46,19 +46,23 @@ hero_status check(const Request& q, hero_dtype dt, bool* noop) {
     return HERO_OK;
 }
 
+template <int ADT, int EPI, int CDT>
+hero_status launch_tile(const GroupedArgs& a, int tile, hipStream_t st) {
+    return tile < GROUPED_128 ? launch_grouped_ring<ADT, EPI, CDT>(a, (RingForm)(tile - GROUPED_RING), st) : launch_grouped_tile<ADT, EPI, CDT>(a, tile, st);
+}
 template <int ADT, int CDT8>
 hero_status launch_tile8(const GroupedArgs& a, int tile, hipStream_t st) {
     const bool bf = a.c_dt == HERO_BF16;
     switch (a.epi) {
-    case HERO_EPI_REQUANT: return launch_grouped_tile<ADT, HERO_EPI_REQUANT, CDT8>(a, tile, st);
-    case HERO_EPI_GELU_REQUANT: return launch_grouped_tile<ADT, HERO_EPI_GELU_REQUANT, CDT8>(a, tile, st);
-    case HERO_EPI_DEQUANT: return bf ? launch_grouped_tile<ADT, HERO_EPI_DEQUANT, HERO_BF16>(a, tile, st) : launch_grouped_tile<ADT, HERO_EPI_DEQUANT, HERO_F16>(a, tile, st);
-    default: return bf ? launch_grouped_tile<ADT, HERO_EPI_DEQUANT_GELU, HERO_BF16>(a, tile, st) : launch_grouped_tile<ADT, HERO_EPI_DEQUANT_GELU, HERO_F16>(a, tile, st);
+    case HERO_EPI_REQUANT: return launch_tile<ADT, HERO_EPI_REQUANT, CDT8>(a, tile, st);
+    case HERO_EPI_GELU_REQUANT: return launch_tile<ADT, HERO_EPI_GELU_REQUANT, CDT8>(a, tile, st);
+    case HERO_EPI_DEQUANT: return bf ? launch_tile<ADT, HERO_EPI_DEQUANT, HERO_BF16>(a, tile, st) : launch_tile<ADT, HERO_EPI_DEQUANT, HERO_F16>(a, tile, st);
+    default: return bf ? launch_tile<ADT, HERO_EPI_DEQUANT_GELU, HERO_BF16>(a, tile, st) : launch_tile<ADT, HERO_EPI_DEQUANT_GELU, HERO_F16>(a, tile, st);
     }
 }
 template <int DT>
 hero_status launch_tile16(const GroupedArgs& a, int tile, hipStream_t st) {
-    return a.epi == HERO_EPI_DEQUANT_GELU ? launch_grouped_tile<DT, HERO_EPI_DEQUANT_GELU, DT>(a, tile, st) : launch_grouped_tile<DT, HERO_EPI_DEQUANT, DT>(a, tile, st);
+    return a.epi == HERO_EPI_DEQUANT_GELU ? launch_tile<DT, HERO_EPI_DEQUANT_GELU, DT>(a, tile, st) : launch_tile<DT, HERO_EPI_DEQUANT, DT>(a, tile, st);
 }
 
 hero_status run(const Request& q, hero_dtype dt, int tile, void* stream) {
@@ -76,11 +80,9 @@ hero_status run(const Request& q, hero_dtype dt, int tile, void* stream) {
     a.offsets = q.offsets; a.row_index = q.row_index; a.E = (int)q.E; a.MA = (int)q.MA;
     a.expert_stride = q.expert_stride * es; a.epi = q.epi; a.c_dt = q.c_dt;
     hipStream_t st = (hipStream_t)stream;
-    const bool tile_ok = grouped_tile_ok(a);
-    const int64_t active = q.E < q.R ? q.E : q.R, rows = q.R / active;      // rows of an expert on average, were none empty
-    if (tile == 0) tile = tile_ok && rows > 24 ? (rows > 160 ? 256 : 128) : rows <= 16 ? 16 : 32;
-    if (tile < 128) return launch_grouped_rows(a, dt, tile, st);
-    if (!tile_ok) return HERO_ERR_UNSUPPORTED;
+    if (tile == 0) tile = grouped_form(a);
+    if (tile == GROUPED_ANY) return launch_grouped_rows(a, dt, st);
+    if (!(tile < GROUPED_128 ? grouped_ring_ok(a) : grouped_tile_ok(a))) return HERO_ERR_UNSUPPORTED;
     switch (dt) {
     case HERO_I8: return launch_tile8<HERO_I8, HERO_I8>(a, tile, st);
     case HERO_F8E4M3: return launch_tile8<HERO_F8E4M3, HERO_F8E4M3>(a, tile, st);
@@ -122,7 +124,8 @@ extern "C" hero_status hero_gemm_grouped_tile(hero_dtype dt, const void* A, int6
                                               hero_epilogue epi, const float* out_col_scale, void* C, hero_dtype c_dt, int64_t ldc,
                                               const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K, void* stream, int tile) {
     if (dt != HERO_I8 && dt != HERO_F8E4M3 && dt != HERO_BF16 && dt != HERO_F16) return HERO_ERR_UNSUPPORTED;
-    if (tile != 0 && tile != 16 && tile != 32 && tile != 128 && tile != 256) return HERO_ERR_UNSUPPORTED;
+    if (tile < 0 || (tile > GROUPED_ANY && tile < GROUPED_RING) || (tile >= GROUPED_RING + RING_128x256 && tile != GROUPED_128 && tile != GROUPED_256)) return HERO_ERR_UNSUPPORTED;
+
     const Request q{A, lda, MA, a_row_scale, row_index, Bt, ldb, expert_stride, b_col_scale, bias, epi, out_col_scale, C, c_dt, ldc, offsets, E, R, N, K};
     return run(q, dt, tile, stream);
 }

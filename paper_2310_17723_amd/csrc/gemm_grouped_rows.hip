@@ -1,5 +1,5 @@
-// Products grouped by expert, few rows to each (a generation step): every expert's weights are read once, by the workgroups that
-// own its columns, straight from memory into the operands of the matrix instructions.
+// Products grouped by expert, of every size: what the faster kernels do not take (a K that ends in half a slab, rows that lie 16 MB or more apart, rows
+// gathered from more than 4 GB).  Both operands come straight from memory into the operands of the matrix instructions, by 64-bit addresses.
 #include "gemm_grouped.h"
 
 using namespace hero_gemm;
@@ -140,20 +140,16 @@ hero_status launch(const GroupedArgs& ga, hipStream_t st) {
     hipLaunchKernelGGL((grouped_rows_kernel<ADT, TM, CT, DEPTH>), dim3((unsigned)(per * NUM_XCD)), dim3(ROW_WAVES * 64), 0, st, a);
     return hero_launch_status();
 }
-template <int ADT>
-hero_status launch_rows(const GroupedArgs& a, int tile, hipStream_t st) {
-    return tile == 16 ? launch<ADT, 1, 2, 3>(a, st) : launch<ADT, 2, 2, 2>(a, st);
-}
 
 }  // namespace
 
 namespace hero_gemm {
-hero_status launch_grouped_rows(const GroupedArgs& a, hero_dtype adt, int tile, hipStream_t st) {
+hero_status launch_grouped_rows(const GroupedArgs& a, hero_dtype adt, hipStream_t st) {
     switch (adt) {
-    case HERO_I8: return launch_rows<HERO_I8>(a, tile, st);
-    case HERO_F8E4M3: return launch_rows<HERO_F8E4M3>(a, tile, st);
-    case HERO_BF16: return launch_rows<HERO_BF16>(a, tile, st);
-    case HERO_F16: return launch_rows<HERO_F16>(a, tile, st);
+    case HERO_I8: return launch<HERO_I8, 2, 2, 2>(a, st);
+    case HERO_F8E4M3: return launch<HERO_F8E4M3, 2, 2, 2>(a, st);
+    case HERO_BF16: return launch<HERO_BF16, 2, 2, 2>(a, st);
+    case HERO_F16: return launch<HERO_F16, 2, 2, 2>(a, st);
     default: return HERO_ERR_UNSUPPORTED;
     }
 }

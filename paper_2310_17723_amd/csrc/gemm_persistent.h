@@ -43,13 +43,8 @@ constexpr int pair_loads_behind(bool odd, int na, int nb, int la, int lb) {
 // workgroup works out the list of row tiles for itself (two tables in LDS) and looks a tile up where a stream moves on to it.
 // GATHER: the activations' rows come from anywhere.  Their numbers and scales are fetched by direct loads too, a tile's numbers together with the
 // vectors of the tile before it, so that no wait for them stands in the loop (KT >= 8: they have landed when the streams move on).
-template <bool GROUPED> struct PersistentArgs { using type = GemmArgs; };
-template <> struct PersistentArgs<true> { using type = GroupedArgs; };
-__device__ __forceinline__ const GemmArgs& gemm_of(const GemmArgs& g) { return g; }
-__device__ __forceinline__ const GemmArgs& gemm_of(const GroupedArgs& a) { return a.g; }
-
 template <int BM, int BN, int WM, int WN, int NSA, int NSB, int EPI, int CDT, int RDT, int ADT = HERO_I8, bool PART = false, bool STEADY = false, bool GROUPED = false, bool GATHER = false>
-__global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(typename PersistentArgs<GROUPED>::type args) {
+__global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(typename ArgsOf<GROUPED>::type args) {
     const GemmArgs& g = gemm_of(args);
     static_assert(!GROUPED || (!PART && !STEADY && RDT < 0), "grouped products: whole, without a residual");
     static_assert(GROUPED || !GATHER, "rows are gathered in grouped products");
@@ -129,14 +124,16 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     uint32_t oa[A_UNITS], ob[B_UNITS];
     Tile tb{0, 0, 0, 0};                                         // B's tile
     int apar = 0;                                                // GATHER: parity of A's tile
-    auto range_start = [&](int s) { return PART ? (int64_t)(s / ntiles) * g.kslabs * (2 * BK) : (int64_t)0; };
+    // GROUPED: every XCD starts an eighth of K further on and turns round at its end (at slab `turn` of a tile)
+    const int begin_k = GROUPED ? xcd * (g.K / (2 * BK)) / NUM_XCD * (2 * BK) : 0, turn = GROUPED ? (g.K - begin_k) / BK : 0;
+    auto range_start = [&](int s) { return GROUPED ? (int64_t)begin_k : PART ? (int64_t)(s / ntiles) * g.kslabs * (2 * BK) : (int64_t)0; };
     auto source = [&](int r) {                                   // a row number, within the rows that there are
         if constexpr (GROUPED) return (uint32_t)min(max(r, 0), args.MA - 1);
         else return (uint32_t)r;
     };
     auto set_rows = [&](const Tile& t, int s, int p) {
         if constexpr (GATHER) {
-            ia = g.A;
+            ia = g.A + range_start(s);
 #pragma unroll
             for (int u = 0; u < A_UNITS; ++u)                    // (units beyond a tile of odd height are not loaded)
                 oa[u] = source(row_number[p * BM + min(lrow + u * (NWAVE * 16), BM - 1)]) * (uint32_t)g.lda + lc;
@@ -215,7 +212,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         wra = next_slot(next_slot(wra, A_BYTES, A_RING), A_BYTES, A_RING);
         if constexpr (STEADY) { ia += 2 * BK; return; }
         akt += 2;
-        if (akt < aKT) { ia += 2 * BK; return; }
+        if (akt < aKT) { ia += 2 * BK; if (GROUPED && akt == turn) ia -= g.K; return; }
         if (aseq + nslot < seq_end) {
             aseq += nslot; akt = 0; apar ^= 1;
             set_tile_a(aseq);
@@ -225,7 +222,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         wrb = next_slot(next_slot(wrb, B_BYTES, B_RING), B_BYTES, B_RING);
         if constexpr (STEADY) { ib += 2 * BK; return; }
         bkt += 2;
-        if (bkt < bKT) { ib += 2 * BK; if constexpr (ONE) ia += 2 * BK; return; }
+        if (bkt < bKT) {
+            ib += 2 * BK;
+            if constexpr (ONE) ia += 2 * BK;
+            if (GROUPED && bkt == turn) { ib -= g.K; if constexpr (ONE) ia -= g.K; }
+            return;
+        }
         if (bseq + nslot < seq_end) {
             bseq += nslot; bkt = 0; bpar ^= 1;
             set_tile_b(bseq);

@@ -1,6 +1,6 @@
 // The ring kernel (see the comment in front of it) and its forms; instantiated once per operand type, in gemm_ring_*.hip.
 #pragma once
-#include "gemm_common.h"
+#include "gemm_grouped.h"
 
 namespace hero_gemm {
 
@@ -24,8 +24,11 @@ __device__ __forceinline__ void ring_wait(int left) {                // at most 
     } else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
 }
 
-template <int BM, int BN, int WM, int WN, int KG, int NS, int EPI, int CDT, int RDT, int ADT, bool PART, bool HALF>
-__global__ __launch_bounds__(WM * WN * 64 * KG) void int8_gemm_ring_kernel(GemmArgs g) {
+// GROUPED: a tile of one expert's rows (gemm_grouped.h), which may come from anywhere.
+template <int BM, int BN, int WM, int WN, int KG, int NS, int EPI, int CDT, int RDT, int ADT, bool PART, bool HALF, bool GROUPED = false>
+__global__ __launch_bounds__(WM * WN * 64 * KG) void int8_gemm_ring_kernel(typename ArgsOf<GROUPED>::type args) {
+    static_assert(!GROUPED || (!PART && !HALF && RDT < 0), "grouped products: whole slabs, without a residual");
+    const GemmArgs& g = gemm_of(args);
     using ACC = typename AccOf<ADT>::type;
     constexpr bool UNIT = ADT == HERO_BF16 || ADT == HERO_F16;      // 16-bit operands: no scales, y = acc + bias
     constexpr int SK = 2 * BK;                                      // bytes of K per slab
@@ -40,8 +43,18 @@ __global__ __launch_bounds__(WM * WN * 64 * KG) void int8_gemm_ring_kernel(GemmA
     __shared__ __attribute__((aligned(1024))) int8_t smem[KG * RING + 3 * BN * 4];
     float* const sv = reinterpret_cast<float*>(smem + KG * RING);
 
-    int m0, n0;
-    if (!tile_origin<BM, BN>(g, m0, n0)) return;
+    int m0, n0, end = g.M, expert = 0;                              // the tile's origin, the end of its rows
+    if constexpr (GROUPED) {
+        const GroupTile t = group_tile<BM>(args, blockIdx.x % NUM_XCD, blockIdx.x / NUM_XCD, g.ntn, (int)threadIdx.x & 63);
+        if (t.rows == 0) return;
+        m0 = t.row0; n0 = t.col_tile * BN; end = m0 + t.rows; expert = t.e;
+    } else if (!tile_origin<BM, BN>(g, m0, n0)) return;
+    // a row's place in A, from the tile's first (grouped: from A's)
+    auto source = [&](int row) {
+        if constexpr (GROUPED) return args.row_index ? min(max(args.row_index[row], 0), args.MA - 1) : row;
+        else return row;
+    };
+    const bool gathered = GROUPED && source_is_gathered(args);
     const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
     const int tid = KG == 1 ? (int)threadIdx.x : (int)threadIdx.x % NT, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
@@ -55,18 +68,25 @@ __global__ __launch_bounds__(WM * WN * 64 * KG) void int8_gemm_ring_kernel(GemmA
     // cold weights, us, register-staged tile -> here: INT8 1 x 4096 x 4160 20.5 -> 8, 64 x 4096 x 16448 with the K split 72 -> 24,
     // E4M3 64 x 4096 x 16448 100 -> 27, BF16 1000 x 4096 x 8256 bytes 92 -> 46.
     const int half = HALF && KT > 0 && k0 + KT == kall ? 1 : 0;
-    const int8_t* ia = g.A + (int64_t)m0 * g.lda + (int64_t)(k0 - half) * SK;        // slab kt of this group: + kt * SK
+    const int8_t* ia = g.A + (gathered ? 0 : (int64_t)m0 * g.lda) + (int64_t)(k0 - half) * SK;        // slab kt of this group: + kt * SK
     const int8_t* ib = g.Bt + (int64_t)n0 * g.ldb + (int64_t)(k0 - half) * SK;
+    if constexpr (GROUPED) ib += (int64_t)expert * args.expert_stride;
     const int lrow = wave * 8 + (lane >> 3);                        // row of this lane in a load's 8 rows; the next load: + 8 * NWAVE
     auto lc = [&](int u) { return (uint32_t)(((lane & 7) ^ (((lrow + u * 8 * NWAVE) >> 1) & 7)) * 16); };    // this lane's chunk of load u
     uint32_t oa[AU], ob[BU];
 #pragma unroll
-    for (int u = 0; u < AU; ++u) oa[u] = (uint32_t)min(lrow + u * 8 * NWAVE, g.M - 1 - m0) * (uint32_t)g.lda + lc(u);
+    for (int u = 0; u < AU; ++u) {
+        const int row = min(lrow + u * 8 * NWAVE, end - 1 - m0);
+        oa[u] = (uint32_t)(gathered ? source(m0 + row) : row) * (uint32_t)g.lda + lc(u);
+    }
 #pragma unroll
     for (int u = 0; u < BU; ++u) ob[u] = (uint32_t)min(lrow + u * 8 * NWAVE, g.N - 1 - n0) * (uint32_t)g.ldb + lc(u);
+    // GROUPED: every XCD starts an eighth of K further on (see the persistent kernel)
+    const int turn = GROUPED ? (int)(blockIdx.x % NUM_XCD) * KT / NUM_XCD : 0;
     const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_offset(smem) + kg * RING);
     auto issue = [&](int kt, int stage) {
         const uint32_t dst = ring + stage * STAGE + wave * 1024;
+        if constexpr (GROUPED) { kt += turn; if (kt >= KT) kt -= KT; }
         const int8_t* a = ia + (int64_t)kt * SK;
         const int8_t* b = ib + (int64_t)kt * SK;
 #pragma unroll
@@ -80,7 +100,7 @@ __global__ __launch_bounds__(WM * WN * 64 * KG) void int8_gemm_ring_kernel(GemmA
     constexpr bool VECS = !PART && EPI != HERO_EPI_RAW_I32;         // raw sums: the caller may have no vectors at all
     float vcs = 0.0f, vbs = 0.0f, vos = 1.0f;
     if (VECS && (int)threadIdx.x < BN) {
-        const int n = min(n0 + (int)threadIdx.x, g.N - 1);
+        const int64_t n = (int64_t)expert * g.N + min(n0 + (int)threadIdx.x, g.N - 1);
         if (!UNIT) vcs = g.b_col_scale[n];
         if (g.bias) vbs = g.bias[n];
         if (EPI == HERO_EPI_GELU_REQUANT) vos = g.out_col_scale[n];
@@ -88,7 +108,7 @@ __global__ __launch_bounds__(WM * WN * 64 * KG) void int8_gemm_ring_kernel(GemmA
     float rsr[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
-        rsr[i] = (VECS && !UNIT && g.a_row_scale) ? g.a_row_scale[min(m0 + wm * TM * 32 + i * 32 + (lane & 31), g.M - 1)] : 1.0f;
+        rsr[i] = (VECS && !UNIT && g.a_row_scale) ? g.a_row_scale[source(min(m0 + wm * TM * 32 + i * 32 + (lane & 31), end - 1))] : 1.0f;
     if (HALF && half) {
 #pragma unroll
         for (int u = 0; u < BU; ++u) dma16s(ob[u] - (lc(u) & (uint32_t)BK), ib + (int64_t)KT * SK, ring + wave * 1024 + BM * SK + u * NWAVE * 1024);
@@ -194,6 +214,10 @@ __global__ __launch_bounds__(WM * WN * 64 * KG) void int8_gemm_ring_kernel(GemmA
         GemmArgs gp = g;
         gp.C = (int32_t*)g.C + (int64_t)blockIdx.y * g.M * g.ldc;
         epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, false, false>(gp, acc, sv, rsr, m0, n0, tid);
+    } else if constexpr (GROUPED) {
+        GemmArgs ge = g;
+        ge.M = end;                                                 // (the rows behind are another expert's)
+        epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, false, UNIT>(ge, acc, sv, rsr, m0, n0, tid);
     } else {
         epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, false, UNIT>(g, acc, sv, rsr, m0, n0, tid);
     }
@@ -235,6 +259,30 @@ hero_status launch_ring_part_slabs(GemmArgs g, RingForm f, hipStream_t st) {
     return HERO_ERR_UNSUPPORTED;
 }
 
+template <int ADT, int EPI, int CDT>
+hero_status launch_grouped_ring(const GroupedArgs& ga, RingForm f, hipStream_t st) {
+    auto go = [&](int BM, int BN, int threads, auto kernel) -> hero_status {
+        GroupedArgs a = ga;
+        a.g.ntn = (a.g.N + BN - 1) / BN;
+        const int64_t tiles = most_row_tiles(a.g.M, a.E, BM) * a.g.ntn, per = (tiles + NUM_XCD - 1) / NUM_XCD;
+        if (per * NUM_XCD * threads > 0xffffffffLL) return HERO_ERR_SHAPE;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(per * NUM_XCD)), dim3(threads), 0, st, a);
+        return hero_launch_status();
+    };
+#define HERO_RING(BM, BN, WM, WN, KG, NS) \
+    return go(BM, BN, WM * WN * KG * 64, int8_gemm_ring_kernel<BM, BN, WM, WN, KG, NS, EPI, CDT, -1, ADT, false, false, true>)
+    switch (f) {
+    case RING_32x32_K4: HERO_RING(32, 32, 1, 1, 4, 4);
+    case RING_32x64_K2: HERO_RING(32, 64, 1, 2, 2, 4);
+    case RING_64x64_K2: HERO_RING(64, 64, 2, 2, 2, 3);
+    case RING_64x64:    HERO_RING(64, 64, 2, 2, 1, 3);
+    case RING_128x64:   HERO_RING(128, 64, 2, 2, 1, 3);
+    case RING_128x128:  HERO_RING(128, 128, 4, 2, 1, 4);
+    default: return HERO_ERR_UNSUPPORTED;
+    }
+#undef HERO_RING
+}
+
 // what gemm_ring_*.hip (K of whole slabs) and gemm_ring_*_half.hip instantiate for their operand type
 #define HERO_RING_8BIT(ADT, CDT8, HALF) \
     template hero_status launch_ring_part_slabs<ADT, HALF>(GemmArgs, RingForm, hipStream_t); \
@@ -252,5 +300,15 @@ hero_status launch_ring_part_slabs(GemmArgs g, RingForm f, hipStream_t st) {
     template hero_status launch_ring_slabs<DT, HERO_EPI_DEQUANT, DT, DT, HALF>(const GemmArgs&, RingForm, hipStream_t); \
     template hero_status launch_ring_slabs<DT, HERO_EPI_DEQUANT_GELU, DT, -1, HALF>(const GemmArgs&, RingForm, hipStream_t); \
     template hero_status launch_ring_slabs<DT, HERO_EPI_DEQUANT_GELU, DT, DT, HALF>(const GemmArgs&, RingForm, hipStream_t);
+#define HERO_GROUPED_RING_8BIT(ADT, CDT8) \
+    template hero_status launch_grouped_ring<ADT, HERO_EPI_REQUANT, CDT8>(const GroupedArgs&, RingForm, hipStream_t); \
+    template hero_status launch_grouped_ring<ADT, HERO_EPI_GELU_REQUANT, CDT8>(const GroupedArgs&, RingForm, hipStream_t); \
+    template hero_status launch_grouped_ring<ADT, HERO_EPI_DEQUANT, HERO_BF16>(const GroupedArgs&, RingForm, hipStream_t); \
+    template hero_status launch_grouped_ring<ADT, HERO_EPI_DEQUANT, HERO_F16>(const GroupedArgs&, RingForm, hipStream_t); \
+    template hero_status launch_grouped_ring<ADT, HERO_EPI_DEQUANT_GELU, HERO_BF16>(const GroupedArgs&, RingForm, hipStream_t); \
+    template hero_status launch_grouped_ring<ADT, HERO_EPI_DEQUANT_GELU, HERO_F16>(const GroupedArgs&, RingForm, hipStream_t);
+#define HERO_GROUPED_RING_16BIT(DT) \
+    template hero_status launch_grouped_ring<DT, HERO_EPI_DEQUANT, DT>(const GroupedArgs&, RingForm, hipStream_t); \
+    template hero_status launch_grouped_ring<DT, HERO_EPI_DEQUANT_GELU, DT>(const GroupedArgs&, RingForm, hipStream_t);
 
 }  // namespace hero_gemm

@@ -70,7 +70,7 @@ def test_products_that_are_refused(lib, dt):
 
 
 def test_the_forced_kernel_is_one_of_them(lib):
-    for tile in (-1, 1, 17, 64, 1000, 128, 256):                          # (the last two: a K of 64 bytes is not theirs)
+    for tile in (-1, 2, 15, 26, 27, 64, 1000, 17, 22, 128, 256):          # (the last four: a K of 64 bytes is not theirs)
         assert lib.hero_gemm_grouped_tile(HB.I8, P, 64, 10, None, None, P, 64, 1024, P, None, HB.EPI_DEQUANT, None, P, HB.BF16, 16, P, 3, 10, 16, 64, None, tile) == UNSUPPORTED
     assert lib.hero_gemm_grouped_tile(HB.F32, P, 64, 10, None, None, P, 64, 1024, P, None, HB.EPI_DEQUANT, None, P, HB.BF16, 16, P, 3, 10, 16, 64, None, 0) == UNSUPPORTED
     assert lib.hero_gemm_grouped_tile(HB.BF16, P, 64, 10, None, None, P, 64, 1024, P, None, HB.EPI_DEQUANT, None, P, HB.F16, 16, P, 3, 10, 16, 64, None, 0) == UNSUPPORTED
