@@ -177,15 +177,26 @@ def _kv_stream(cache, stream):
     return _stream(stream)
 
 
-def _on_device(device, stream, *tensors):
-    """The stream of a call whose tensors all lie on `device` (an index), which has to be the stream's."""
-    at = torch.cuda.current_device() if stream is None else stream.device_index
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_on(device, stream):
+    """The stream of a call whose tensors lie on `device` (an index), which has to be the stream's."""
+    if stream is None:
+        at = _get_device()
+        if device == at and _raw_stream:
+            return _raw_stream(at)
+    else:
+        at = stream.device_index
     if device != at:
         raise ValueError(f"the tensors lie on device {device}, which is not the " + ("current one" if stream is None else f"stream's ({at})"))
+    return _stream(stream)
+
+
+def _one_device(device, *tensors):
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise ValueError("the tensors of a call lie on one device")
-    return _stream(stream)
 
 
 def _vector(t, dtype, *shape):
@@ -197,11 +208,22 @@ def _vector(t, dtype, *shape):
     return t.data_ptr()
 
 
+def _floats(t, shape, device):
+    """The address of a contiguous float32 tensor of this shape on this device, or None."""
+    if t is None:
+        return None
+    if t.dtype is torch.float32 and t.shape == shape and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
+    _one_device(device, t)
+    return _vector(t, torch.float32, *shape)
+
+
 def _matrix(t, cols):
     """The leading dimension of rows of `cols` elements (a single row may have any)."""
-    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"expected rows of {cols} neighbouring elements, not {list(t.shape)} with strides {list(t.stride())}")
-    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] != cols or (stride[1] != 1 and cols > 1):
+        raise ValueError(f"expected rows of {cols} neighbouring elements, not {list(shape)} with strides {list(stride)}")
+    return stride[0] if shape[0] > 1 else max(cols, stride[0])
 
 
 class Hero:
@@ -514,6 +536,8 @@ class Hero:
     def hero_moe_route_workspace_bytes(self, T, E, top_k) -> int:
         return int(self.lib.hero_moe_route_workspace_bytes(T, E, top_k))
 
+    # (A small call is its host call: in the calls below everything is asked once, in plain comparisons, and the functions that say what is
+    # wrong run only where something is.  us of host time, a check for each tensor by functions of its own -> so: route 7.1 -> 4.7, sum 7.9 -> 5.0, product 11.8 -> 8.0.)
     def hero_moe_route(self, logits, top_k, renorm=True, out=None, workspace=None, stream=None) -> MoeRouting:
         """The top_k experts of every token (logits [T,E] f32 / bf16 / f16) and the order of their rows.  workspace: uint8 tensor
         (hero_moe_route_workspace_bytes), made here if it is None and needed; out: a MoeRouting to write into (moe_routing)."""
@@ -523,37 +547,50 @@ class Hero:
         if workspace is None:
             need = self.hero_moe_route_workspace_bytes(T, E, top_k)
             workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
-        st = _on_device(logits.get_device(), stream, workspace, *out)
+        expert, weight, slot, token, offsets = out
+        dev = logits.get_device()
+        if not (expert.get_device() == weight.get_device() == slot.get_device() == token.get_device() == offsets.get_device() == dev) or (
+                workspace is not None and workspace.get_device() != dev):
+            _one_device(dev, workspace, *out)
+        per = (T, top_k)
+        if not (expert.shape == per and weight.shape == per and slot.shape == per and token.shape == (T * top_k,) and offsets.shape == (E + 1,)
+                and expert.dtype is slot.dtype is token.dtype is offsets.dtype is torch.int32 and weight.dtype is torch.float32
+                and expert.is_contiguous() and weight.is_contiguous() and slot.is_contiguous() and token.is_contiguous() and offsets.is_contiguous()):
+            for t, dt, shape in ((expert, torch.int32, per), (weight, torch.float32, per), (slot, torch.int32, per), (token, torch.int32, (T * top_k,)),
+                                 (offsets, torch.int32, (E + 1,))):
+                _vector(t, dt, *shape)
         self._check(self.lib.hero_moe_route(
-            logits.data_ptr(), _DT[logits.dtype], _matrix(logits, E), T, E, top_k, int(bool(renorm)), _vector(out.expert, torch.int32, T, top_k),
-            _vector(out.weight, torch.float32, T, top_k), _vector(out.slot, torch.int32, T, top_k), _vector(out.row_token, torch.int32, T * top_k),
-            _vector(out.offsets, torch.int32, E + 1), _ptr(workspace), 0 if workspace is None else workspace.nbytes, st))
+            logits.data_ptr(), _DT[logits.dtype], _matrix(logits, E), T, E, top_k, 1 if renorm else 0, expert.data_ptr(), weight.data_ptr(), slot.data_ptr(),
+            token.data_ptr(), offsets.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream_on(dev, stream)))
         return out
 
-    def _grouped(self, A, W, offsets, row_index, vectors, out_dtype, C_out, stream):
-        """What the products by expert share: (the result, the arguments around the vectors)."""
+    def _grouped(self, A, W, offsets, row_index, out_dtype, C_out):
+        """What the products by expert share: (the result, their device, the arguments in front of, between and behind the vectors)."""
         E, N, K = W.shape
-        if E > 0 and N > 0 and (W.stride(2) != 1 or A.element_size() != W.element_size()):
+        expert_stride, ldb, step = W.stride()
+        if E > 0 and N > 0 and (step != 1 or A.element_size() != W.element_size()):
             raise ValueError("weights are [E, N, K] with K contiguous, of the rows' type")
-        R = A.shape[0] if row_index is None else row_index.shape[0]
+        R = MA = A.shape[0]
+        dev, index = A.get_device(), None
+        if row_index is not None:
+            R = row_index.shape[0]
+            index = _vector(row_index, torch.int32, R)
         if C_out is None:
             C_out = torch.empty((R, N), dtype=out_dtype, device=A.device)
         elif C_out.shape[0] != R:
             raise ValueError(f"the result has a row for each of the {R} rows, not {C_out.shape[0]}")
-        st = _on_device(A.get_device(), stream, W, offsets, row_index, C_out, *vectors)
-        front = (A.data_ptr(), _matrix(A, K), A.shape[0])
-        weights = (W.data_ptr(), W.stride(1) if N > 1 else max(K, W.stride(1)), W.stride(0))
-        back = (C_out.data_ptr(), _DT[C_out.dtype], _matrix(C_out, N), _vector(offsets, torch.int32, E + 1), E, R, N, K)
-        return C_out, front, _vector(row_index, torch.int32, R), weights, back, st
+        if not (W.get_device() == offsets.get_device() == C_out.get_device() == dev) or (index is not None and row_index.get_device() != dev):
+            _one_device(dev, W, offsets, row_index, C_out)
+        return (C_out, dev, (A.data_ptr(), _matrix(A, K), MA), (index, W.data_ptr(), ldb if N > 1 else max(K, ldb), expert_stride),
+                (C_out.data_ptr(), _DT[C_out.dtype], _matrix(C_out, N), _vector(offsets, torch.int32, E + 1), E, R, N, K))
 
     def _gemm_grouped8(self, fn, dt, A, W, offsets, row_index, a_row_scale, b_col_scale, bias, epi, out_col_scale, out_dtype, C_out, stream, tile):
-        E, N, _ = W.shape
-        if out_dtype is None:
+        if out_dtype is None and C_out is None:
             out_dtype = torch.bfloat16 if epi in (EPI_DEQUANT, EPI_DEQUANT_GELU) else torch.int8 if dt == I8 else torch.float8_e4m3fn
-        vectors = (a_row_scale, b_col_scale, bias, out_col_scale)
-        C_out, front, index, weights, back, st = self._grouped(A, W, offsets, row_index, vectors, out_dtype, C_out, stream)
-        args = (*front, _vector(a_row_scale, torch.float32, A.shape[0]), index, *weights, _vector(b_col_scale, torch.float32, E, N),
-                _vector(bias, torch.float32, E, N), int(epi), _vector(out_col_scale, torch.float32, E, N), *back, st)
+        C_out, dev, front, weights, back = self._grouped(A, W, offsets, row_index, out_dtype, C_out)
+        EN = W.shape[:2]
+        args = (*front, None if a_row_scale is None else _floats(a_row_scale, A.shape[:1], dev), *weights, _floats(b_col_scale, EN, dev),
+                _floats(bias, EN, dev), epi, _floats(out_col_scale, EN, dev), *back, _stream_on(dev, stream))
         self._check(fn(*args) if tile is None else self.lib.hero_gemm_grouped_tile(dt, *args, int(tile)))
         return C_out
 
@@ -580,14 +617,13 @@ class Hero:
         """The 16-bit side: A, W and the result in one type, bf16 or fp16."""
         if A.dtype not in (torch.bfloat16, torch.float16) or W.dtype is not A.dtype or (C_out is not None and C_out.dtype is not A.dtype):
             raise ValueError("rows, weights and result are of one 16-bit type")
-        E, N, _ = W.shape
-        C_out, front, index, weights, back, st = self._grouped(A, W, offsets, row_index, (bias,), A.dtype, C_out, stream)
-        b = _vector(bias, torch.float32, E, N)
+        C_out, dev, front, weights, back = self._grouped(A, W, offsets, row_index, A.dtype, C_out)
+        b, st = _floats(bias, W.shape[:2], dev), _stream_on(dev, stream)
         if tile is None:
-            self._check(self.lib.hero_hp_gemm_grouped(*front, index, *weights, b, int(bool(gelu)), back[0], *back[2:], back[1], st))
+            self._check(self.lib.hero_hp_gemm_grouped(*front, *weights, b, int(bool(gelu)), back[0], *back[2:], back[1], st))
         else:
             epi = EPI_DEQUANT_GELU if gelu else EPI_DEQUANT
-            self._check(self.lib.hero_gemm_grouped_tile(back[1], *front, None, index, *weights, None, b, epi, None, *back, st, int(tile)))
+            self._check(self.lib.hero_gemm_grouped_tile(back[1], *front, None, *weights, None, b, epi, None, *back, st, int(tile)))
         return C_out
 
     def hero_moe_combine(self, y, slot, weight, residual=None, out=None, stream=None):
@@ -595,15 +631,19 @@ class Hero:
         slot int32, weight f32 [T,top_k]; slots outside [0, R) are left out."""
         R, D = y.shape
         T, k = slot.shape
+        dt, dev = y.dtype, y.get_device()
         if out is None:
-            out = torch.empty((T, D), dtype=y.dtype, device=y.device)
-        for t in (residual, out):
-            if t is not None and (t.dtype is not y.dtype or t.shape[0] != T):
-                raise ValueError(f"residual and result are {y.dtype} rows of the {T} tokens")
-        st = _on_device(y.get_device(), stream, slot, weight, residual, out)
-        self._check(self.lib.hero_moe_combine(y.data_ptr(), _matrix(y, D), R, _vector(slot, torch.int32, T, k), _vector(weight, torch.float32, T, k),
-                                              _ptr(residual), 0 if residual is None else _matrix(residual, D), out.data_ptr(), _matrix(out, D),
-                                              T, k, D, _DT[y.dtype], st))
+            out = torch.empty((T, D), dtype=dt, device=y.device)
+        if out.dtype is not dt or out.shape[0] != T or (residual is not None and (residual.dtype is not dt or residual.shape[0] != T)):
+            raise ValueError(f"residual and result are {dt} rows of the {T} tokens")
+        if not (slot.get_device() == weight.get_device() == out.get_device() == dev) or (residual is not None and residual.get_device() != dev):
+            _one_device(dev, slot, weight, residual, out)
+        if not (slot.dtype is torch.int32 and weight.dtype is torch.float32 and weight.shape == slot.shape and slot.is_contiguous() and weight.is_contiguous()):
+            _vector(slot, torch.int32, T, k)
+            _vector(weight, torch.float32, T, k)
+        self._check(self.lib.hero_moe_combine(y.data_ptr(), _matrix(y, D), R, slot.data_ptr(), weight.data_ptr(), _ptr(residual),
+                                              0 if residual is None else _matrix(residual, D), out.data_ptr(), _matrix(out, D), T, k, D, _DT[dt],
+                                              _stream_on(dev, stream)))
         return out
 
     # ------------------------------------------------------------------ layer

@@ -146,7 +146,8 @@ __device__ __forceinline__ void store_piece(int8_t* cp, const uint32_t (&d)[ND],
 }
 
 // ACC is v16i (INT8 operands) or v16f (bf16 operands: UNIT, no scales, y = acc + bias).
-template <int BM, int BN, int WM, int WN, int EPI, int CDT, int RDT, bool OS_RAW = false, bool UNIT = false, typename ACC = v16i>
+// SPREAD, here and below: a wave's fragments lie WM fragments apart (they share a tile that is not full), and those behind g.M are left out whole.
+template <int BM, int BN, int WM, int WN, int EPI, int CDT, int RDT, bool OS_RAW = false, bool UNIT = false, bool SPREAD = false, typename ACC = v16i>
 __device__ __forceinline__ void epilogue_direct(const GemmArgs& g, ACC (&acc)[BM / WM / 32][BN / WN / 32],
                                                 const float* sv, const float (&rsr)[BM / WM / 32],
                                                 int m0, int n0, int tid) {
@@ -173,7 +174,8 @@ __device__ __forceinline__ void epilogue_direct(const GemmArgs& g, ACC (&acc)[BM
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int row = m0 + wm * TM * 32 + i * 32 + ml;
+        const int row = m0 + (SPREAD ? (i * WM + wm) * 32 : wm * TM * 32 + i * 32) + ml;
+        if (SPREAD && m0 + (i * WM + wm) * 32 >= g.M) break;
         const bool rowok = row < g.M;
         const float rs = rsr[i];
         if constexpr (EPI == HERO_EPI_RAW_I32) {                  // 16 bytes per group: stored as they are
@@ -279,7 +281,7 @@ __device__ __forceinline__ void epilogue_direct(const GemmArgs& g, ACC (&acc)[BM
 // The epilogue behind 16 x 16 tiles whose weight rows were taken in the order 16 (r / 4) + 4 j + r % 4 (r: row of the instruction, j: its
 // tile of the wave's 64 columns): lane l then holds, for ONE output row (l % 16 of each of the TI tiles), the 16 consecutive columns
 // 16 (l / 16) .. + 15, column 4 j + t in acc[i][j][t], and nothing has to change lanes.  8-bit results and raw sums.
-template <int BM, int BN, int WM, int WN, int EPI, int CDT, bool UNIT, typename ACC, int TI>
+template <int BM, int BN, int WM, int WN, int EPI, int CDT, bool UNIT, bool SPREAD = false, typename ACC, int TI>
 __device__ __forceinline__ void epilogue_rows16(const GemmArgs& g, ACC (&acc)[TI][4], const float* sv, const float (&rsr)[TI], int m0, int n0, int tid) {
     static_assert(BN / WN == 64 && BM / WM == 16 * TI, "a wave owns 64 columns");
     constexpr int ES = ElemSize<CDT>::v;
@@ -302,7 +304,8 @@ __device__ __forceinline__ void epilogue_rows16(const GemmArgs& g, ACC (&acc)[TI
     }
 #pragma unroll
     for (int i = 0; i < TI; ++i) {
-        const int row = m0 + wm * TI * 16 + i * 16 + (lane & 15);
+        const int row = m0 + (SPREAD ? (i * WM + wm) * 16 : wm * TI * 16 + i * 16) + (lane & 15);
+        if (SPREAD && m0 + (i * WM + wm) * 16 >= g.M) break;
         const bool ok = row < g.M && col0 < g.N;
         if constexpr (EPI == HERO_EPI_RAW_I32) {
             uint32_t d[16];                                       // int32 sums, or the bits of fp32 ones
@@ -347,11 +350,12 @@ __device__ __forceinline__ void epilogue_rows16(const GemmArgs& g, ACC (&acc)[TI
 // are not stored): a test is a branch, and every second element was waited for by itself, row after row of the tile that ends the launch.  us, a test per element
 // before this form of the epilogue, with it -> now: off 16 bytes INT8 16384 x 1024 x 1024 (rows 1028 apart) 40.0, 40.4 -> 24.8, BF16 16384 x 3076 x 1024 168.8, 171.3 -> 118.8;
 // cut FP16 + GELU 2049 x 2303 x 512 15.6, 16.1 -> 14.6, INT8 -> BF16 3000 x 3000 x 1024 21.4, 21.6 -> 20.3, 7000 x 1500 x 1024 25.1, 25.4 -> 23.6.
-template <int BM, int BN, int WM, int WN, int EPI, int CDT, int RDT, bool UNIT, typename ACC, int TI>
+template <int BM, int BN, int WM, int WN, int EPI, int CDT, int RDT, bool UNIT, bool SPREAD = false, typename ACC, int TI>
 __device__ __forceinline__ void epilogue_rows16_hp(const GemmArgs& g, ACC (&acc)[TI][4], const float* sv, const float (&rsr)[TI], int m0, int n0, int wave, int lane) {
     static_assert(BN / WN == 64 && BM / WM == 16 * TI && ElemSize<CDT>::v == 2, "a wave owns 64 columns, 16-bit results");
     const int wm = wave / WN, wn = wave % WN, nl = wn * 64 + (lane >> 4) * 16;
-    const int col0 = n0 + nl, mw = m0 + wm * TI * 16;
+    constexpr int ROWS = SPREAD ? WM * 16 : 16;                   // between the wave's fragments
+    const int col0 = n0 + nl, mw = m0 + (SPREAD ? wm * 16 : wm * TI * 16);
     const bool al16 = (g.ldc * 2) % 16 == 0, full = col0 + 16 <= g.N;
     const bool rl16 = RDT >= 0 && (g.ldr * 2) % 16 == 0 && ((uintptr_t)g.residual & 15) == 0;
     v4f cs[4], bs[4];
@@ -365,7 +369,8 @@ __device__ __forceinline__ void epilogue_rows16_hp(const GemmArgs& g, ACC (&acc)
         int8_t* cp = (int8_t*)g.C + ((int64_t)(mw + (lane & 15)) * g.ldc + col0) * 2;
         const uint16_t* rp = RDT >= 0 ? (const uint16_t*)g.residual + (int64_t)(mw + (lane & 15)) * g.ldr + col0 : nullptr;
 #pragma unroll
-        for (int i = 0; i < TI; ++i, cp += 32 * g.ldc, rp += RDT >= 0 ? 16 * g.ldr : 0) {
+        for (int i = 0; i < TI; ++i, cp += 2 * ROWS * g.ldc, rp += RDT >= 0 ? ROWS * g.ldr : 0) {
+            if (SPREAD && mw + i * ROWS >= g.M) break;
             float y[16];
 #pragma unroll
             for (int h = 0; h < 16; h += 8) {
@@ -381,7 +386,7 @@ __device__ __forceinline__ void epilogue_rows16_hp(const GemmArgs& g, ACC (&acc)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[h + e] = v[e];
             }
-            if (!whole && (mw + i * 16 + (lane & 15) >= g.M || col0 >= g.N)) continue;
+            if (!whole && (mw + i * ROWS + (lane & 15) >= g.M || col0 >= g.N)) continue;
             if constexpr (RDT >= 0) {
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
@@ -413,7 +418,7 @@ __device__ __forceinline__ void epilogue_rows16_hp(const GemmArgs& g, ACC (&acc)
     // (Not for a plain result of 128 x 128 tiles, where it gains nothing and the loop in front of it comes out slower.  us, without / with: INT8 -> FP16 1500 x 3072 x 4096 29.1 /
     // 29.5, 1500 x 3001 x 4096 29.1 / 29.5, 2049 x 2303 x 4096 29.8 / 30.0, FP16 1500 x 3072 x 2048 28.9 / 29.0.)
     constexpr bool ASK = BM > 128 || RDT >= 0 || EPI == HERO_EPI_DEQUANT_GELU;
-    if (ASK && mw + TI * 16 <= g.M && n0 + wn * 64 + 64 <= g.N && al16 && (RDT < 0 || rl16)) rows(std::true_type{});
+    if (ASK && mw + (TI - 1) * ROWS + 16 <= g.M && n0 + wn * 64 + 64 <= g.N && al16 && (RDT < 0 || rl16)) rows(std::true_type{});
     else rows(std::false_type{});
 }
 

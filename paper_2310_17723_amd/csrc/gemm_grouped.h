@@ -13,6 +13,7 @@ struct GroupedArgs {
     int E, MA;                                  // experts, rows of A
     int64_t expert_stride;                      // bytes between the weights of two experts
     int epi, c_dt;                              // (for the kernel that asks at run time)
+    int height;                                 // persistent kernel: rows of a tile, 0: each workgroup works it out from the experts' rows
 };
 
 // what a kernel takes that has a grouped form
@@ -94,14 +95,13 @@ __device__ __forceinline__ GroupTile group_tile(const GroupedArgs& a, int xcd, i
 }
 
 // The tables of the tile kernels (in LDS, whole waves): row_begin [E + 1], tiles_upto [E] filled up to a multiple of 64 with the number of all
-// row tiles, which is returned.
-template <int BM>
-__device__ __forceinline__ int expert_tables(const GroupedArgs& a, int* row_begin, int* tiles_upto, int lane) {
+// row tiles, which is returned.  Tiles have `height` rows.
+__device__ __forceinline__ int expert_tables(const GroupedArgs& a, int height, int* row_begin, int* tiles_upto, int lane) {
     int carry = 0, tiles = 0;
     for (int e0 = 0; e0 < a.E; e0 += 64) {
         int begin, end;
         expert_rows(a, e0, lane, carry, begin, end);
-        const int upto = tiles + wave_scan_sum((end - begin + BM - 1) / BM);
+        const int upto = tiles + wave_scan_sum((end - begin + height - 1) / height);
         if (e0 + lane <= a.E) row_begin[e0 + lane] = begin;
         if (e0 + lane + 1 == a.E) row_begin[a.E] = end;
         tiles_upto[e0 + lane] = upto;
@@ -111,10 +111,36 @@ __device__ __forceinline__ int expert_tables(const GroupedArgs& a, int* row_begi
     return tiles;
 }
 
-// Tile number s: rows [m0, min(m0 + BM, end)) of expert e.  Eight row tiles of an expert run through its columns together (tile_from_seq's order).
-struct ExpertTile { int e, m0, end, col_tile; };
+constexpr int GROUPED_COST[4] = {59, 76, 92, 100};
+// The height, of the quarters of BM rows, at which the busiest workgroup has the least to do: the rows of the experts, which are known here only,
+// fill a number of tiles, and the workgroups take them in turn.  GROUPED_COST[q]: what a tile of q + 1 quarters costs (its weights come in whole;
+// 1024 rows to each of eight experts x 4096 x 4096 in tiles of 64, 128, 192, 256 rows: INT8 250, 166, 135, 118 us, BF16 535, 305, 255, 219).
 template <int BM>
-__device__ __forceinline__ ExpertTile expert_tile(const GroupedArgs& a, const int* row_begin, const int* tiles_upto, int s, int lane) {
+__device__ __forceinline__ int best_height(const GroupedArgs& a, int workgroups, int lane) {
+    int carry = 0, tiles[4] = {0, 0, 0, 0};
+    for (int e0 = 0; e0 < a.E; e0 += 64) {
+        int begin, end;
+        expert_rows(a, e0, lane, carry, begin, end);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            constexpr int H = BM / 4;
+            tiles[q] += __builtin_amdgcn_readlane(wave_scan_sum((end - begin + (q + 1) * H - 1) / ((q + 1) * H)), 63);
+        }
+        carry = __builtin_amdgcn_readlane(end, 63);
+    }
+    int best = 3;
+    int64_t least = INT64_MAX;
+#pragma unroll
+    for (int q = 3; q >= 0; --q) {
+        const int64_t cost = ((int64_t)tiles[q] * a.g.ntn + workgroups - 1) / workgroups * GROUPED_COST[q];
+        if (cost < least) { least = cost; best = q; }
+    }
+    return (best + 1) * (BM / 4);
+}
+
+// Tile number s: rows [m0, end) of expert e.  Eight row tiles of an expert run through its columns together (tile_from_seq's order).
+struct ExpertTile { int e, m0, end, col_tile; };
+__device__ __forceinline__ ExpertTile expert_tile(const GroupedArgs& a, int height, const int* row_begin, const int* tiles_upto, int s, int lane) {
     const int ntn = a.g.ntn, at = s / ntn;
     int e0 = 0;
     unsigned long long beyond = __ballot(tiles_upto[lane] > at);
@@ -125,8 +151,8 @@ __device__ __forceinline__ ExpertTile expert_tile(const GroupedArgs& a, const in
     const int grp = in / (GROUP_M * ntn), rem = in - grp * (GROUP_M * ntn), rows = min(mt - grp * GROUP_M, GROUP_M);
     ExpertTile t;
     t.e = e;
-    t.m0 = begin + (grp * GROUP_M + rem % rows) * BM;
-    t.end = __builtin_amdgcn_readfirstlane(row_begin[e + 1]);
+    t.m0 = begin + (grp * GROUP_M + rem % rows) * height;
+    t.end = min(__builtin_amdgcn_readfirstlane(row_begin[e + 1]), t.m0 + height);
     t.col_tile = rem / rows;
     return t;
 }
@@ -163,9 +189,14 @@ inline int grouped_form(const GroupedArgs& a) {
     }
     if (n <= 48 && active * cols(64) <= 256) return GROUPED_RING + RING_64x64_K2;
     if (n <= 20 || (n <= 48 && active * cols(128) < 512) || !pers) return GROUPED_RING + (n <= 48 ? RING_64x64 : RING_128x64);
-    const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
-    if (n <= 160 && t128 < 512) return GROUPED_RING + RING_128x64;
-    return 9 * ((t128 + 255) / 256) <= 25 * ((t256 + 255) / 256) ? GROUPED_128 : GROUPED_256;
+    if (n <= 160 && tiles(128, 128) < 512) return GROUPED_RING + RING_128x64;
+    // what the busiest CU has to do, in hundredths of a 256 x 256 tile, as best_height() will see it; a 128 x 128 tile costs 0.36 of one
+    int64_t most = INT64_MAX;
+    for (int q = 0; q < 4; ++q) {
+        const int64_t cost = (tiles(64 * (q + 1), 256) + 255) / 256 * GROUPED_COST[q];
+        if (cost < most) most = cost;
+    }
+    return (tiles(128, 128) + 255) / 256 * 36 <= most ? GROUPED_128 : GROUPED_256;
 }
 
 }  // namespace hero_gemm

@@ -78,8 +78,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     int* const row_begin = reinterpret_cast<int*>(smem + TABLE_OFF);     // GROUPED: expert e's rows are row_begin[e] .. row_begin[e + 1] - 1,
     int* const tiles_upto = row_begin + MAX_EXPERTS + 1;                 // the row tiles of experts 0 .. e are tiles_upto[e] in number
     int* const row_number = reinterpret_cast<int*>(smem + INDEX_OFF);    // GATHER: [parity of the tile][row]
+    int height = BM;
     if constexpr (GROUPED) {
-        ntiles = expert_tables<BM>(args, row_begin, tiles_upto, lane) * g.ntn;      // (every wave writes the same)
+        height = args.height ? args.height : BM == 256 ? best_height<BM>(args, (int)gridDim.x, lane) : BM;
+        ntiles = expert_tables(args, height, row_begin, tiles_upto, lane) * g.ntn;  // (every wave writes the same)
         per_xcd = (ntiles + NUM_XCD - 1) / NUM_XCD;
         __syncthreads();
     }
@@ -91,7 +93,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     auto tile_at = [&](int s) {
         Tile t;
         if constexpr (GROUPED) {
-            const ExpertTile x = expert_tile<BM>(args, row_begin, tiles_upto, s, lane);
+            const ExpertTile x = expert_tile(args, height, row_begin, tiles_upto, s, lane);
             t.e = x.e; t.m0 = x.m0; t.end = x.end; t.n0 = x.col_tile * BN;
         } else {
             tile_from_seq<BM, BN>(g, PART ? s % ntiles : s, t.m0, t.n0);
@@ -240,11 +242,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     constexpr int TI = BM / WM / 16, TJ = 2 * TN;
     static_assert(WIDE || TJ == 4, "16 x 16 tiles: 64 columns per wave");
     const int r16 = lane & 15, ch16 = ((lane >> 4) ^ swz4(r16 >> 2)) << 4;
-    const int foa = (wm * TI * 16 + r16) * 64 + ch16, fob = A_RING + (wn * 64 + 16 * (r16 >> 2) + (r16 & 3)) * 64 + ch16;
+    // GROUPED: the waves of a column share a tile's rows fragment by fragment, so that a tile that is not full is as much work for each of them
+    constexpr int FRAG = GROUPED ? WM * 1024 : 1024;                // bytes between a wave's fragments of A
+    const int foa = (wm * (GROUPED ? 16 : TI * 16) + r16) * 64 + ch16, fob = A_RING + (wn * 64 + 16 * (r16 >> 2) + (r16 & 3)) * 64 + ch16;
     int fo[2][NFR];
 #pragma unroll
     for (int t = 0; t < NFR; ++t) {
-        const int rr = (t < TN ? wn * TN * 32 + t * 32 : wm * TM * 32 + (t - TN) * 32) + ml;
+        const int rr = (t < TN ? wn * TN * 32 + t * 32 : GROUPED ? ((t - TN) * WM + wm) * 32 : wm * TM * 32 + (t - TN) * 32) + ml;
         const int base = (t < TN ? A_RING : 0) + rr * 64;
         fo[0][t] = base + (((0 + hh) ^ ((rr >> 2) & 3)) << 4);
         fo[1][t] = base + (((2 + hh) ^ ((rr >> 2) & 3)) << 4);
@@ -302,15 +306,17 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
 #pragma unroll
             for (int t = 0; t < TJ; ++t) fb[t] = *reinterpret_cast<const v4i*>(smem + rdb + fob + t * 256);
 #pragma unroll
-            for (int t = 0; t < TI; ++t) fa[t] = *reinterpret_cast<const v4i*>(smem + rda + foa + t * 1024);
+            for (int t = 0; t < TI; ++t) fa[t] = *reinterpret_cast<const v4i*>(smem + rda + foa + t * FRAG);
         }
 
         // One slab per iteration with the barrier in the middle (see int8_gemm_dma_kernel).  Behind the barrier of iteration i every
         // wave has read the last fragment of slab i, so both its slots are free: a ring of five slots has
         // one to spare and takes the pair (i + 4, i + 5) in even iterations, rings of four and six wait for the odd one
         // and take (i + 3, i + 4), (i + 5, i + 6).  The pairs may already belong to the next tile.
-        auto iteration = [&](auto ODD) {
+        // HEIGHT: how many of a wave's fragments hold rows (all of them, but in the last tile of an expert).
+        auto iteration = [&](auto ODD, auto HEIGHT) {
             constexpr bool odd = decltype(ODD)::value;
+            constexpr int TE = decltype(HEIGHT)::value, NME = TE * TN;      // (WIDE: of 32 rows)
             constexpr bool put_a = odd == (NSA % 2 == 0), put_b = odd == (NSB % 2 == 0);
             constexpr int NU = (put_a ? A_UNITS : 0) + (put_b ? B_UNITS : 0);      // units to issue: A's, then B's
             const int nda = rda + A_BYTES == A_RING ? 0 : rda + A_BYTES, ndb = ONE ? nda : (rdb + B_BYTES == B_RING ? 0 : rdb + B_BYTES);
@@ -328,27 +334,27 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
                 // FP8: one 32x32x64 matrix instruction per accumulator and slab (both k halves of a fragment
                 // side by side: any K grouping shared by the two operands is the same contraction).  A
                 // fragment is reloaded from the next slab right after its last use; the barrier that
-                // publishes that slab sits after the first TM instructions.
+                // publishes that slab sits after the first TE instructions.
 #pragma unroll
-                for (int n = 0; n < NM; ++n) {
-                    const int jj = n / TM, ii = n % TM;
+                for (int n = 0; n < NME; ++n) {
+                    const int jj = n / TE, ii = n % TE;
                     acc[ii][jj] = mfma_wide_f8(f0[jj], f1[jj], f0[TN + ii], f1[TN + ii], acc[ii][jj]);
-                    if (n == TM - 1) {
+                    if (n == TE - 1) {
                         wait_next_slab();
                         __syncthreads();
                     }
-                    if (n >= TM - 1) {
+                    if (n >= TE - 1) {
 #pragma unroll
-                        for (int t = 0; t < NFR; ++t) {
-                            const int last = t < TN ? t * TM + TM - 1 : (TN - 1) * TM + (t - TN);
-                            if ((last < TM - 1 ? TM - 1 : last) == n) {
+                        for (int t = 0; t < TN + TE; ++t) {
+                            const int last = t < TN ? t * TE + TE - 1 : (TN - 1) * TE + (t - TN);
+                            if ((last < TE - 1 ? TE - 1 : last) == n) {
                                 f0[t] = *reinterpret_cast<const v4i*>(smem + (t < TN ? ndb : nda) + fo[0][t]);
                                 f1[t] = *reinterpret_cast<const v4i*>(smem + (t < TN ? ndb : nda) + fo[1][t]);
                             }
                         }
-                        constexpr int SLOTS = NM - TM + 1, PPS = (NU + SLOTS - 1) / SLOTS;      // units per instruction slot
+                        constexpr int SLOTS = NME - TE + 1, PPS = (NU + SLOTS - 1) / SLOTS;      // units per instruction slot
 #pragma unroll
-                        for (int u = (n - (TM - 1)) * PPS; u < (n - (TM - 1) + 1) * PPS; ++u)
+                        for (int u = (n - (TE - 1)) * PPS; u < (n - (TE - 1) + 1) * PPS; ++u)
                             if (u < NU) issue_unit(u);
                     }
                     __builtin_amdgcn_sched_barrier(0);
@@ -363,11 +369,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
                 // 82.8 / 81.8, BF16 109.6 / 108.9;  BERT-large layer 32 x 512 270.9 / 269.0 (282.4 / 280.1 on another card), in M1 357.0 / 356.3, GPT prefill 0 to 1 %
                 // by the card.  (The columns there and back as well, over the two iterations of a pair: 631 / 623 us for the first of these, no gain.)
                 auto there_and_back = [](int jj, int r, int rows) { return jj & 1 ? rows - 1 - r : r; };
-                constexpr int HI = TI / 2, HS = TI - HI, NH = HS * TJ;
+                constexpr int HI = TE / 2, HS = TE - HI, NH = HS * TJ;
                 static_assert(NU <= NH, "a slot of the second half for every unit");
 #pragma unroll
                 for (int n = 0; n < HI * TJ; ++n) {
-                    const int jj = n / HI, ii = there_and_back(jj, n % HI, HI);
+                    const int jj = n / (HI ? HI : 1), ii = there_and_back(jj, n % (HI ? HI : 1), HI);
                     acc[ii][jj] = mfma16_step<ADT>(fb[jj], fa[ii], acc[ii][jj]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -378,9 +384,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
                 for (int n = 0; n < NH; ++n) {
                     const int jj = n / HS, ii = HI + there_and_back(jj, n % HS, HS);
                     acc[ii][jj] = mfma16_step<ADT>(fb[jj], fa[ii], acc[ii][jj]);
-                    if (n < HI) fa[n] = *reinterpret_cast<const v4i*>(smem + nda + foa + n * 1024);
+                    if (n < HI) fa[n] = *reinterpret_cast<const v4i*>(smem + nda + foa + n * FRAG);
                     if (n % HS == HS - 1) fb[jj] = *reinterpret_cast<const v4i*>(smem + ndb + fob + jj * 256);
-                    if (n >= NH - HS) fa[ii] = *reinterpret_cast<const v4i*>(smem + nda + foa + ii * 1024);
+                    if (n >= NH - HS) fa[ii] = *reinterpret_cast<const v4i*>(smem + nda + foa + ii * FRAG);
                     if constexpr (NU > 0) {                            // evenly over the half
                         constexpr int EV = NH / NU;
                         if (n % EV == 0 && n / EV < NU) issue_unit(n / EV);
@@ -397,15 +403,28 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         constexpr int D = STEADY ? NSA / 2 : 0;
         static_assert(!STEADY || (NSB / 2 == D && !ONE && !WIDE && EPI != HERO_EPI_GELU_REQUANT), "both streams move on together");
         const int KS = KT - 2 * D;
-        for (int kt = 0; kt < KS; kt += 2) {
-            iteration(std::false_type{});
-            iteration(std::true_type{});
-            // S_a -> 1 / S_a once per tile (IEEE division): the vectors landed before the first barrier, KT >= 4 leaves another
-            if (!WIDE && EPI == HERO_EPI_GELU_REQUANT && kt == 0 && tid < BN) {
-                float* const s = sv0 + par * SVF + 2 * BN + tid;
-                *s = __fdiv_rn(1.0f, *s);
+        using Full = std::integral_constant<int, CI>;
+        auto slabs = [&](auto HEIGHT) {
+            for (int kt = 0; kt < KS; kt += 2) {
+                iteration(std::false_type{}, HEIGHT);
+                iteration(std::true_type{}, HEIGHT);
+                // S_a -> 1 / S_a once per tile (IEEE division): the vectors landed before the first barrier, KT >= 4 leaves another
+                if (!WIDE && EPI == HERO_EPI_GELU_REQUANT && kt == 0 && tid < BN) {
+                    float* const s = sv0 + par * SVF + 2 * BN + tid;
+                    *s = __fdiv_rn(1.0f, *s);
+                }
             }
-        }
+        };
+        if constexpr (GROUPED) {
+            // (in quarters of a wave's fragments; a loop for each, chosen once per tile)
+            constexpr int Q = CI >= 4 ? CI / 4 : 1, QUARTERS = CI / Q, UNIT_ROWS = WM * Q * (WIDE ? 32 : 16);
+            constexpr int THREE = (QUARTERS > 3) ? 3 * Q : CI, TWO = (QUARTERS > 2) ? 2 * Q : CI;
+            const int quarters = (tile.end - m0 + UNIT_ROWS - 1) / UNIT_ROWS;
+            if (quarters >= QUARTERS) slabs(Full{});
+            else if (QUARTERS > 3 && quarters == 3) slabs(std::integral_constant<int, THREE>{});
+            else if (QUARTERS > 2 && quarters == 2) slabs(std::integral_constant<int, TWO>{});
+            else slabs(std::integral_constant<int, Q>{});
+        } else slabs(Full{});
         if constexpr (STEADY) {
             const bool last = seq + nslot >= seq_end;
             const int back = last ? 2 * BK : 0;
@@ -417,8 +436,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
             }
             static_for<D>([&](auto) {
                 ia -= back; ib -= back;
-                iteration(std::false_type{});
-                iteration(std::true_type{});
+                iteration(std::false_type{}, Full{});
+                iteration(std::true_type{}, Full{});
             });
         }
         // Prefetch for the caller's next kernel: this tile's share of the lines, one dword of each, through the same
@@ -446,13 +465,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         float rsr[CI];
 #pragma unroll
         for (int i = 0; i < CI; ++i)
-            rsr[i] = (EPI != HERO_EPI_RAW_I32 && has_rs) ? sv[3 * BN + wm * (BM / WM) + i * (WIDE ? 32 : 16) + (HP || STEADY ? el & 15 : WIDE ? ml : r16)] : 1.0f;
+            rsr[i] = (EPI != HERO_EPI_RAW_I32 && has_rs) ? sv[3 * BN + (GROUPED ? (i * WM + wm) * (WIDE ? 32 : 16) : wm * (BM / WM) + i * (WIDE ? 32 : 16)) + (HP || STEADY ? el & 15 : WIDE ? ml : r16)] : 1.0f;
         if constexpr (GROUPED) {
             GemmArgs ge = g;
             ge.M = tile.end;                                       // (the rows behind are another expert's)
-            if constexpr (WIDE) epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, true, UNIT>(ge, acc, sv, rsr, m0, n0, tid);
-            else if constexpr (HP) epilogue_rows16_hp<BM, BN, WM, WN, EPI, CDT, RDT, UNIT>(ge, acc, sv, rsr, m0, n0, wave, el);
-            else epilogue_rows16<BM, BN, WM, WN, EPI, CDT, UNIT>(ge, acc, sv, rsr, m0, n0, tid);
+            if constexpr (WIDE) epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, true, UNIT, true>(ge, acc, sv, rsr, m0, n0, tid);
+            else if constexpr (HP) epilogue_rows16_hp<BM, BN, WM, WN, EPI, CDT, RDT, UNIT, true>(ge, acc, sv, rsr, m0, n0, wave, el);
+            else epilogue_rows16<BM, BN, WM, WN, EPI, CDT, UNIT, true>(ge, acc, sv, rsr, m0, n0, tid);
         } else if constexpr (WIDE) epilogue_direct<BM, BN, WM, WN, EPI, CDT, RDT, true, UNIT>(g, acc, sv, rsr, m0, n0, tid);
         else if constexpr (HP) epilogue_rows16_hp<BM, BN, WM, WN, EPI, CDT, RDT, UNIT>(g, acc, sv, rsr, m0, n0, wave, el);
         else if constexpr (PART) {
@@ -548,12 +567,14 @@ hero_status launch_persistent_part(const GemmArgs& g, int rows, hipStream_t st) 
 
 // Grouped products: 256 x 256, or 128 x 128 with two workgroups per CU.  K >= 512 bytes, a multiple of 128.
 template <int ADT, int EPI, int CDT>
-hero_status launch_grouped_tile(const GroupedArgs& ga, int rows, hipStream_t st) {
+hero_status launch_grouped_tile(const GroupedArgs& ga, int form, hipStream_t st) {
+    const int rows = form >= GROUPED_256 ? 256 : 128;
     auto go = [&](auto R, auto GATHER) {
         constexpr int BM = decltype(R)::value, BN = BM, W = BM == 256 ? 4 : 2, NA = 4, NB = BM == 256 ? 5 : 4, PER_CU = BM == 256 ? 1 : 2;
         GroupedArgs a = ga;
         a.g.ntn = (a.g.N + BN - 1) / BN;
-        const int64_t tiles = most_row_tiles(a.g.M, a.E, BM) * a.g.ntn, per = (tiles + NUM_XCD - 1) / NUM_XCD;
+        a.height = (form - BM) * (BM / 4);                             // (GROUPED_256 + q, GROUPED_128 + q: q quarters)
+        const int64_t tiles = most_row_tiles(a.g.M, a.E, BM / 4) * a.g.ntn, per = (tiles + NUM_XCD - 1) / NUM_XCD;
         if (tiles > 0x7fffff00LL) return HERO_ERR_SHAPE;
         const int nslot = per < 32 * PER_CU ? (int)per : 32 * PER_CU;
         hipLaunchKernelGGL((int8_gemm_persistent_kernel<BM, BN, 2, W, NA, NB, EPI, CDT, -1, ADT, false, false, true, decltype(GATHER)::value>),

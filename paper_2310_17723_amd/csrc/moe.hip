@@ -2,76 +2,121 @@
 // hero_moe_route, hero_moe_combine.
 #include "hero_common.h"
 #include <float.h>
+#include <type_traits>
 
 namespace {
 
 constexpr int MAX_E = 512, MAX_K = 16;
-constexpr int TOKENS = 64;                  // of a workgroup: at most 1024 choices, one for each of its threads
-constexpr int THREADS = 1024, WAVES = THREADS / 64;
+// Tokens of a workgroup, sixteen threads to each: for few tokens one workgroup of up to 64 of them, for many workgroups of 16
+constexpr int ONE_TOKENS = 64, TOKENS = 16, MAX_WAVES = ONE_TOKENS / 4;
 
 struct RouteArgs {
     const void* logits; int64_t ldl;
-    int T, E, k, renorm, nb;                // nb workgroups of TOKENS tokens
+    int T, E, k, renorm, nb;                // nb workgroups
     int32_t* expert; float* weight; int32_t* slot; int32_t* row_token; int32_t* offsets;
-    int32_t* counts;                        // [E][nb]: choices of each workgroup; behind the scan those of the workgroups before it
+    int32_t* counts;                        // [nb][E]: choices of each workgroup; behind the scan those of the workgroups before it
     int32_t* totals;                        // [E]
 };
 
-template <int DT>
-__device__ __forceinline__ float logit_at(const void* p, int64_t i) {
-    if constexpr (DT == HERO_F32) return ((const float*)p)[i];
-    else return hp_to_f32<DT>(((const uint16_t*)p)[i]);
+// reductions over rows of 16 lanes; every lane of a row gets the result
+template <int CTRL> __device__ __forceinline__ int row_swap(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
+template <typename T, typename F>
+__device__ __forceinline__ T row_reduce(T x, F f) {
+    auto step = [&](auto C) { x = f(x, __builtin_bit_cast(T, row_swap<decltype(C)::value>(__builtin_bit_cast(int, x)))); };
+    step(std::integral_constant<int, 0xB1>{});                    // quad_perm [1,0,3,2]
+    step(std::integral_constant<int, 0x4E>{});                    // quad_perm [2,3,0,1]
+    step(std::integral_constant<int, 0x141>{});                   // row_half_mirror
+    step(std::integral_constant<int, 0x140>{});                   // row_mirror
+    return x;
 }
 
-// A wave chooses the experts of one token: lane l holds the logits of experts l V .. l V + V - 1, so that the first lane (and of its
-// experts the first) of those that hold the maximum is the lowest index.  k rounds of a maximum over the wave and a ballot.
+// Sixteen lanes choose the experts of one token, a wave those of four: lane l holds the logits of experts 16 v + l.  top_k rounds of a maximum; ties
+// go to the lowest index.  Bound by the instructions of the rounds: a logit of 16 bits shares a word with its index, so that the maximum is
+// one of words, all different, 3 V instructions a round for V logits to a lane; 32 bits take 5 V (value, then index).  us, a wave to a token ->
+// this: 16384 tokens x 256 bf16, 8 chosen 17.8 -> 8.2, 5001 x 160 f32, 6 chosen 15.0 -> 5.5.
 template <int DT, int V>
-__device__ __forceinline__ void choose(const RouteArgs& a, int t, int lane, int32_t* chosen) {
-    float l[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int e = lane * V + v;
-        const float x = logit_at<DT>(a.logits, (int64_t)t * a.ldl + min(e, a.E - 1));
-        l[v] = e < a.E && x == x ? fminf(x, FLT_MAX) : -INFINITY;
-    }
-    float top = 0.0f, mine = -INFINITY, all = 0.0f;               // lane j keeps the logit of choice j
+__device__ __forceinline__ void choose(const RouteArgs& a, int t, int t_end, int lane, int32_t* chosen) {
+    const int l16 = lane & 15;
+    const bool real = t < t_end;
+    const int64_t row = (int64_t)min(t, t_end - 1) * a.ldl + l16;
+    auto max_of = [](auto x, auto y) { return x > y ? x : y; };
+    auto sum_of = [](float x, float y) { return x + y; };
+    float top = -INFINITY, all = 0.0f, mine = -INFINITY;          // lane j of the row keeps choice j
     int who = -1;
-    for (int j = 0; j < a.k; ++j) {
-        float best = l[0];
+    if constexpr (DT != HERO_F32) {
+        // w: the type's bits, turned so that they order as unsigned numbers (-0 as +0), above the index from above; 0: no expert (-infinity, NaN)
+        constexpr uint32_t INF = DT == HERO_BF16 ? 0x7f80u : 0x7c00u;
+        auto value = [](uint32_t b) { return fminf(hp_to_f32<DT>(b), FLT_MAX); };
+        auto bits = [](uint32_t w) { const uint32_t b = w >> 16; return b & 0x8000u ? b & 0x7fffu : 0xffffu ^ b; };
+        uint32_t w[V];
 #pragma unroll
-        for (int v = 1; v < V; ++v) best = fmaxf(best, l[v]);
-        const float m = wave_reduce<true>(best);
-        if (j == 0) {
-            top = m > -INFINITY ? m : 0.0f;
-            if (!a.renorm) {
+        for (int v = 0; v < V; ++v) w[v] = v * 16 + l16 < a.E ? ((const uint16_t*)a.logits)[row + v * 16] : INF | 0x8000u;
 #pragma unroll
-                for (int v = 0; v < V; ++v) all += expf(l[v] - top);
-            }
+        for (int v = 0; v < V; ++v) {
+            uint32_t b = w[v] == 0x8000u ? 0u : w[v];
+            const bool none = (b & 0x7fffu) > INF || b == (INF | 0x8000u);
+            b = b & 0x8000u ? 0xffffu ^ b : b | 0x8000u;
+            w[v] = none ? 0u : (b << 16) | (0xffffu - (uint32_t)(v * 16 + l16));
         }
-        if (!(m > -INFINITY)) break;                              // (uniform)
-        const int first = __ffsll((unsigned long long)__ballot(best == m)) - 1;
-        int at = V - 1;
+        uint32_t m = 0;
+        for (int j = 0; j < a.k; ++j) {
+            uint32_t next = w[0];
 #pragma unroll
-        for (int v = V - 2; v >= 0; --v) if (l[v] == m) at = v;
-        at = __builtin_amdgcn_readlane(at, first);
-        if (lane == j) { mine = m; who = first * V + at; }
+            for (int v = 1; v < V; ++v) next = max(next, w[v]);
+            m = row_reduce(next, max_of);
+            if (j == 0) {
+                top = m ? value(bits(m)) : 0.0f;
+                if (!a.renorm) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) if (lane == first && v == at) l[v] = -INFINITY;
+                    for (int v = 0; v < V; ++v) all += w[v] ? expf(value(bits(w[v])) - top) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) w[v] = w[v] == m ? 0u : w[v];
+            if (l16 == j && m) { who = 0xffff - (int)(m & 0xffffu); mine = value(bits(m)); }
+        }
+    } else {
+        float l[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) l[v] = v * 16 + l16 < a.E ? ((const float*)a.logits)[row + v * 16] : -INFINITY;
+#pragma unroll
+        for (int v = 0; v < V; ++v) l[v] = l[v] == l[v] ? fminf(l[v], FLT_MAX) : -INFINITY;
+        for (int j = 0; j < a.k; ++j) {
+            float m = l[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) m = fmaxf(m, l[v]);
+            m = row_reduce(m, [](float x, float y) { return fmaxf(x, y); });
+            if (j == 0) {
+                top = m > -INFINITY ? m : 0.0f;
+                if (!a.renorm) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) all += expf(l[v] - top);
+                }
+            }
+            int at = V;
+#pragma unroll
+            for (int v = V - 1; v >= 0; --v) at = l[v] == m ? v : at;
+            const int index = at * 16 + l16, first = row_reduce(index, [](int x, int y) { return min(x, y); });
+            at = index == first ? at : V;
+#pragma unroll
+            for (int v = 0; v < V; ++v) l[v] = v == at ? -INFINITY : l[v];
+            if (l16 == j && m > -INFINITY) { who = first; mine = m; }
+        }
     }
     const float p = who >= 0 ? expf(mine - top) : 0.0f;
-    const float total = wave_reduce<false>(a.renorm ? p : all);
-    if (lane < a.k) {
-        a.expert[(int64_t)t * a.k + lane] = who;
-        a.weight[(int64_t)t * a.k + lane] = who >= 0 ? __fdiv_rn(p, total) : 0.0f;
-        if (chosen) chosen[lane] = who;
+    const float total = row_reduce(a.renorm ? p : all, sum_of);
+    if (real && l16 < a.k) {
+        a.expert[(int64_t)t * a.k + l16] = who;
+        a.weight[(int64_t)t * a.k + l16] = who >= 0 ? __fdiv_rn(p, total) : 0.0f;
+        chosen[l16] = who;
     }
 }
 
 // Choice c of this workgroup, one to a thread: how many choices of the same expert come before it in its wave, and in the workgroup's
-// earlier waves (`before` [WAVES][E]).  Equal experts of a wave are found bit by bit of their number.
+// earlier waves (`before` [waves][E]).  Equal experts of a wave are found bit by bit of their number.
 __device__ __forceinline__ int rank_in_group(int e, int E, int* before, int* group_total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < WAVES * E; i += THREADS) before[i] = 0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, threads = blockDim.x, waves = threads >> 6;
+    for (int i = threadIdx.x; i < waves * E; i += threads) before[i] = 0;
     __syncthreads();
     unsigned long long same = __ballot(e >= 0);
 #pragma unroll
@@ -82,9 +127,9 @@ __device__ __forceinline__ int rank_in_group(int e, int E, int* before, int* gro
     const int rank = __popcll(same & ((1ull << lane) - 1));
     if (e >= 0 && rank == 0) before[wave * E + e] = __popcll(same);
     __syncthreads();
-    for (int i = threadIdx.x; i < E; i += THREADS) {
+    for (int i = threadIdx.x; i < E; i += threads) {
         int sum = 0;
-        for (int w = 0; w < WAVES; ++w) { const int n = before[w * E + i]; before[w * E + i] = sum; sum += n; }
+        for (int w = 0; w < waves; ++w) { const int n = before[w * E + i]; before[w * E + i] = sum; sum += n; }
         if (group_total) group_total[i] = sum;
     }
     __syncthreads();
@@ -109,19 +154,18 @@ __device__ __forceinline__ void starts(const int* total, int E, int* start) {
     __syncthreads();
 }
 
-// Choices of TOKENS tokens, a wave for each in turn.  ONE: the only workgroup of the call, which orders the rows as well; else it leaves
-// behind how many of its choices fall to each expert.
+// ONE: the only workgroup of the call (of as many waves as it needs), which orders the rows as well; else a workgroup leaves behind how many of its
+// choices fall to each expert.
 template <int DT, int V, bool ONE>
-__global__ __launch_bounds__(THREADS) void route_choose_kernel(RouteArgs a) {
-    __shared__ int32_t chosen[TOKENS * MAX_K];
-    __shared__ int before[ONE ? WAVES * MAX_E : MAX_E], total[ONE ? MAX_E : 1], start[ONE ? MAX_E + 1 : 1];
+__global__ __launch_bounds__(ONE ? ONE_TOKENS * 16 : TOKENS * 16) void route_choose_kernel(RouteArgs a) {
+    constexpr int NTOK = ONE ? ONE_TOKENS : TOKENS;
+    __shared__ int32_t chosen[NTOK * MAX_K];
+    __shared__ int before[ONE ? MAX_WAVES * MAX_E : MAX_E], total[ONE ? MAX_E : 1], start[ONE ? MAX_E + 1 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int t0 = blockIdx.x * TOKENS, nt = min(TOKENS, a.T - t0);
-    if (!ONE) {
-        for (int i = threadIdx.x; i < a.E; i += THREADS) before[i] = 0;
-        __syncthreads();
-    }
-    for (int t = wave; t < nt; t += WAVES) choose<DT, V>(a, t0 + t, lane, chosen + t * a.k);
+    const int t0 = blockIdx.x * NTOK, nt = min(NTOK, a.T - t0), t = wave * 4 + (lane >> 4);
+    if (!ONE)
+        for (int i = threadIdx.x; i < a.E; i += TOKENS * 16) before[i] = 0;
+    if (wave * 4 < nt) choose<DT, V>(a, t0 + t, t0 + nt, lane, chosen + t * a.k);
     __syncthreads();
     const int c = threadIdx.x, e = c < nt * a.k ? chosen[c] : -1;
     if constexpr (ONE) {
@@ -130,67 +174,84 @@ __global__ __launch_bounds__(THREADS) void route_choose_kernel(RouteArgs a) {
         if (c < nt * a.k) a.slot[c] = e >= 0 ? start[e] + r : -1;
         if (e >= 0) a.row_token[start[e] + r] = c / a.k;
         if (c < nt * a.k && c >= start[a.E]) a.row_token[c] = -1;
-        for (int i = threadIdx.x; i <= a.E; i += THREADS) a.offsets[i] = start[i];
+        for (int i = threadIdx.x; i <= a.E; i += blockDim.x) a.offsets[i] = start[i];
     } else {
         if (e >= 0) atomicAdd(&before[e], 1);                       // (counts: their order does not show)
         __syncthreads();
-        for (int i = threadIdx.x; i < a.E; i += THREADS) a.counts[(int64_t)i * a.nb + blockIdx.x] = before[i];
+        for (int i = threadIdx.x; i < a.E; i += TOKENS * 16) a.counts[(int64_t)blockIdx.x * a.E + i] = before[i];
     }
 }
 
-// counts[e][b] -> choices of e in the workgroups before b; totals[e].  A workgroup per expert.
-__global__ __launch_bounds__(256) void route_scan_kernel(RouteArgs a) {
-    __shared__ int part[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int32_t* const row = a.counts + (int64_t)blockIdx.x * a.nb;
-    int carry = 0;
-    for (int b0 = 0; b0 < a.nb; b0 += 256) {
-        const int b = b0 + threadIdx.x, n = b < a.nb ? row[b] : 0;
+// counts[b][e] -> choices of e in the workgroups before b; totals[e].  A workgroup for 16 experts: 64 threads to each, a stretch of the workgroups to
+// every one of them.
+__global__ __launch_bounds__(1024) void route_scan_kernel(RouteArgs a) {
+    constexpr int ROWS = 16;                                            // of a stretch
+    __shared__ int part[64][17], whole[16];
+    const int col = threadIdx.x & 15, seg = threadIdx.x >> 4, e = blockIdx.x * 16 + col;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int carry = 0;                                                      // (of this thread's expert)
+    for (int b0 = seg * ROWS; b0 - seg * ROWS < a.nb; b0 += 64 * ROWS) {
+        int x[ROWS], sum = 0;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) x[i] = e < a.E && b0 + i < a.nb ? a.counts[(int64_t)(b0 + i) * a.E + e] : 0;
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) { const int n = x[i]; x[i] = sum; sum += n; }
+        part[seg][col] = sum;
+        __syncthreads();
+        const int n = part[lane][wave];                                 // wave w scans the 64 stretches of expert w
         int upto = n;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(upto, o); if (lane >= o) upto += x; }
+        for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(upto, o); if (lane >= o) upto += y; }
+        part[lane][wave] = upto - n;
+        if (lane == 63) whole[wave] = upto;
         __syncthreads();
-        if (lane == 63) part[wave] = upto;
+        const int at = carry + part[seg][col];
+        carry += whole[col];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            if (e < a.E && b0 + i < a.nb) a.counts[(int64_t)(b0 + i) * a.E + e] = at + x[i];
         __syncthreads();
-        int base = carry;
-        for (int w = 0; w < wave; ++w) base += part[w];
-        if (b < a.nb) row[b] = base + upto - n;
-        carry += part[0] + part[1] + part[2] + part[3];
     }
-    if (threadIdx.x == 0) a.totals[blockIdx.x] = carry;
+    if (seg == 0 && e < a.E) a.totals[e] = carry;
 }
 
-__global__ __launch_bounds__(THREADS) void route_place_kernel(RouteArgs a) {
-    __shared__ int before[WAVES * MAX_E], start[MAX_E + 1];
+__global__ __launch_bounds__(TOKENS * 16) void route_place_kernel(RouteArgs a) {
+    __shared__ int before[TOKENS / 4 * MAX_E], start[MAX_E + 1];
     const int t0 = blockIdx.x * TOKENS, n = min(TOKENS, a.T - t0) * a.k, c = threadIdx.x;
     const int64_t i = (int64_t)t0 * a.k + c;
     const int e = c < n ? a.expert[i] : -1;
+    const int earlier = e >= 0 ? a.counts[(int64_t)blockIdx.x * a.E + e] : 0;
     const int r = rank_in_group(e, a.E, before, nullptr);
     starts(a.totals, a.E, start);
     if (c < n) {
-        const int s = e >= 0 ? start[e] + a.counts[(int64_t)e * a.nb + blockIdx.x] + r : -1;
+        const int s = e >= 0 ? start[e] + earlier + r : -1;
         a.slot[i] = s;
         if (e >= 0) a.row_token[s] = t0 + c / a.k;
         if (i >= start[a.E]) a.row_token[i] = -1;
     }
     if (blockIdx.x == 0)
-        for (int j = threadIdx.x; j <= a.E; j += THREADS) a.offsets[j] = start[j];
+        for (int j = threadIdx.x; j <= a.E; j += TOKENS * 16) a.offsets[j] = start[j];
 }
 
 template <int DT, int V>
 hero_status launch_route(const RouteArgs& a, hipStream_t st) {
-    if (a.nb <= 1) {
-        hipLaunchKernelGGL((route_choose_kernel<DT, V, true>), dim3(1), dim3(THREADS), 0, st, a);
+    if (a.T <= ONE_TOKENS) {
+        const int waves = (a.T + 3) / 4;
+        hipLaunchKernelGGL((route_choose_kernel<DT, V, true>), dim3(1), dim3(64 * (waves < 1 ? 1 : waves)), 0, st, a);
         return hero_launch_status();
     }
-    hipLaunchKernelGGL((route_choose_kernel<DT, V, false>), dim3((unsigned)a.nb), dim3(THREADS), 0, st, a);
-    hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)a.E), dim3(256), 0, st, a);
-    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.nb), dim3(THREADS), 0, st, a);
+    hipLaunchKernelGGL((route_choose_kernel<DT, V, false>), dim3((unsigned)a.nb), dim3(TOKENS * 16), 0, st, a);
+    hipLaunchKernelGGL(route_scan_kernel, dim3((unsigned)(a.E + 15) / 16), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(route_place_kernel, dim3((unsigned)a.nb), dim3(TOKENS * 16), 0, st, a);
     return hero_launch_status();
 }
 template <int DT>
 hero_status launch_route(const RouteArgs& a, hipStream_t st) {
-    return a.E <= 64 ? launch_route<DT, 1>(a, st) : a.E <= 128 ? launch_route<DT, 2>(a, st) : a.E <= 256 ? launch_route<DT, 4>(a, st) : launch_route<DT, 8>(a, st);
+    const int v = (a.E + 15) / 16;
+#define HERO_ROUTE(V) if (v <= V) return launch_route<DT, V>(a, st)
+    HERO_ROUTE(1); HERO_ROUTE(2); HERO_ROUTE(4); HERO_ROUTE(8); HERO_ROUTE(12); HERO_ROUTE(16); HERO_ROUTE(24);
+#undef HERO_ROUTE
+    return launch_route<DT, 32>(a, st);
 }
 
 struct CombineArgs {
@@ -236,7 +297,7 @@ inline bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 }  // namespace
 
 extern "C" size_t hero_moe_route_workspace_bytes(int64_t T, int64_t E, int64_t top_k) {
-    if (T <= TOKENS || E < 1 || E > MAX_E || top_k < 1 || top_k > MAX_K || T > 0x7fffffffLL / top_k) return 0;
+    if (T <= ONE_TOKENS || E < 1 || E > MAX_E || top_k < 1 || top_k > MAX_K || T > 0x7fffffffLL / top_k) return 0;
     const size_t nb = (size_t)((T + TOKENS - 1) / TOKENS);
     return ((nb + 1) * (size_t)E * 4 + 255) / 256 * 256;
 }
@@ -259,7 +320,7 @@ extern "C" hero_status hero_moe_route(const void* logits, hero_dtype dt, int64_t
     a.nb = (int)((T + TOKENS - 1) / TOKENS);
     a.expert = expert; a.weight = weight; a.slot = slot; a.row_token = row_token; a.offsets = offsets;
     a.counts = (int32_t*)workspace; a.totals = a.counts ? a.counts + (int64_t)a.nb * E : nullptr;
-    if ((int64_t)a.nb * THREADS > 0xffffffffLL) return HERO_ERR_SHAPE;
+    if ((int64_t)a.nb * TOKENS * 16 > 0xffffffffLL) return HERO_ERR_SHAPE;
     hipStream_t st = (hipStream_t)stream;
     return dt == HERO_F32 ? launch_route<HERO_F32>(a, st) : dt == HERO_BF16 ? launch_route<HERO_BF16>(a, st) : launch_route<HERO_F16>(a, st);
 }
