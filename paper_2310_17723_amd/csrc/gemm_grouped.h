@@ -13,7 +13,6 @@ struct GroupedArgs {
     int E, MA;                                  // experts, rows of A
     int64_t expert_stride;                      // bytes between the weights of two experts
     int epi, c_dt;                              // (for the kernel that asks at run time)
-    int height;                                 // persistent kernel: rows of a tile, 0: each workgroup works it out from the experts' rows
 };
 
 // what a kernel takes that has a grouped form
@@ -111,10 +110,13 @@ __device__ __forceinline__ int expert_tables(const GroupedArgs& a, int height, i
     return tiles;
 }
 
+// What a tile of one to four quarters of the rows of 256 costs: its weights come in whole.  us, 1024 rows to each of eight experts x 4096 x 4096 in tiles of
+// 64, 128, 192, 256 rows: INT8 250, 166, 135, 118, BF16 535, 305, 255, 219.
 constexpr int GROUPED_COST[4] = {59, 76, 92, 100};
-// The height, of the quarters of BM rows, at which the busiest workgroup has the least to do: the rows of the experts, which are known here only,
-// fill a number of tiles, and the workgroups take them in turn.  GROUPED_COST[q]: what a tile of q + 1 quarters costs (its weights come in whole;
-// 1024 rows to each of eight experts x 4096 x 4096 in tiles of 64, 128, 192, 256 rows: INT8 250, 166, 135, 118 us, BF16 535, 305, 255, 219).
+// The height at which the busiest workgroup has the least to do: the rows of the experts, which are known here only, make a number of tiles that the
+// workgroups take in turn.  us, 256 rows always / this: INT8 3200 rows of 8 experts x 4096 x 4096 101 / 83, 6400 rows of 16 x 1024 x 4096 51 / 45.  (The last
+// tiles of a workgroup cut into pieces instead, so that all of them end together: no gain, and 8192 rows of 8 experts x 4096 x 16384 517 -> 544: what idles
+// at the end leaves the others its power.)
 template <int BM>
 __device__ __forceinline__ int best_height(const GroupedArgs& a, int workgroups, int lane) {
     int carry = 0, tiles[4] = {0, 0, 0, 0};
@@ -149,11 +151,11 @@ __device__ __forceinline__ ExpertTile expert_tile(const GroupedArgs& a, int heig
     const int first = __builtin_amdgcn_readfirstlane(e ? tiles_upto[e - 1] : 0), mt = __builtin_amdgcn_readfirstlane(tiles_upto[e]) - first;
     const int begin = __builtin_amdgcn_readfirstlane(row_begin[e]), in = s - first * ntn;
     const int grp = in / (GROUP_M * ntn), rem = in - grp * (GROUP_M * ntn), rows = min(mt - grp * GROUP_M, GROUP_M);
-    ExpertTile t;
-    t.e = e;
-    t.m0 = begin + (grp * GROUP_M + rem % rows) * height;
-    t.end = min(__builtin_amdgcn_readfirstlane(row_begin[e + 1]), t.m0 + height);
-    t.col_tile = rem / rows;
+    ExpertTile t;                               // (uniform, and said to be: the addresses of the direct loads are scalars)
+    t.e = __builtin_amdgcn_readfirstlane(e);
+    t.m0 = __builtin_amdgcn_readfirstlane(begin + (grp * GROUP_M + rem % rows) * height);
+    t.end = __builtin_amdgcn_readfirstlane(min(row_begin[e + 1], t.m0 + height));
+    t.col_tile = __builtin_amdgcn_readfirstlane(rem / rows);
     return t;
 }
 

@@ -78,7 +78,7 @@ hero_status run(const Request& q, hero_dtype dt, int tile, void* stream) {
     g.C = q.C; g.ldc = q.ldc; g.M = (int)q.R; g.N = (int)q.N; g.K = (int)(q.K * es);
     g.ntm = g.ntn = g.per_xcd = 0; g.ksplit = 1; g.kslabs = 0;
     a.offsets = q.offsets; a.row_index = q.row_index; a.E = (int)q.E; a.MA = (int)q.MA;
-    a.expert_stride = q.expert_stride * es; a.epi = q.epi; a.c_dt = q.c_dt; a.height = 0;
+    a.expert_stride = q.expert_stride * es; a.epi = q.epi; a.c_dt = q.c_dt;
     hipStream_t st = (hipStream_t)stream;
     if (tile == 0) tile = grouped_form(a);
     if (tile == GROUPED_ANY) return launch_grouped_rows(a, dt, st);
@@ -124,7 +124,7 @@ extern "C" hero_status hero_gemm_grouped_tile(hero_dtype dt, const void* A, int6
                                               hero_epilogue epi, const float* out_col_scale, void* C, hero_dtype c_dt, int64_t ldc,
                                               const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K, void* stream, int tile) {
     if (dt != HERO_I8 && dt != HERO_F8E4M3 && dt != HERO_BF16 && dt != HERO_F16) return HERO_ERR_UNSUPPORTED;
-    if (tile < 0 || (tile > GROUPED_ANY && tile < GROUPED_RING) || (tile >= GROUPED_RING + RING_128x256 && (tile & ~7) != GROUPED_128 && (tile & ~7) != GROUPED_256) || (tile >= GROUPED_128 && (tile & 7) > 4)) return HERO_ERR_UNSUPPORTED;
+    if (tile < 0 || (tile > GROUPED_ANY && tile < GROUPED_RING) || (tile >= GROUPED_RING + RING_128x256 && tile != GROUPED_128 && tile != GROUPED_256)) return HERO_ERR_UNSUPPORTED;
 
     const Request q{A, lda, MA, a_row_scale, row_index, Bt, ldb, expert_stride, b_col_scale, bias, epi, out_col_scale, C, c_dt, ldc, offsets, E, R, N, K};
     return run(q, dt, tile, stream);

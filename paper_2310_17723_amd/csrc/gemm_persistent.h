@@ -80,7 +80,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     int* const row_number = reinterpret_cast<int*>(smem + INDEX_OFF);    // GATHER: [parity of the tile][row]
     int height = BM;
     if constexpr (GROUPED) {
-        height = args.height ? args.height : BM == 256 ? best_height<BM>(args, (int)gridDim.x, lane) : BM;
+        // (128 x 128 tiles keep their height: two workgroups share a CU, and smaller ones gain nothing.  us, INT8 384 and 768 rows of 8 experts x 4096 x 4096
+        // 37.7, 36.4, with heights 41.2, 44.2)
+        if (BM == 256) height = best_height<BM>(args, (int)gridDim.x, lane);
         ntiles = expert_tables(args, height, row_begin, tiles_upto, lane) * g.ntn;  // (every wave writes the same)
         per_xcd = (ntiles + NUM_XCD - 1) / NUM_XCD;
         __syncthreads();
@@ -124,7 +126,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     int aseq = seq, akt = 0, aKT, bseq = seq, bkt = 0, bKT, bpar = 0;
     const int8_t* ia; const int8_t* ib;                          // wave-uniform: tile base + slab offset
     uint32_t oa[A_UNITS], ob[B_UNITS];
-    Tile tb{0, 0, 0, 0};                                         // B's tile
+    Tile tb{0, 0, 0, 0}, tn{0, 0, 0, 0};                         // B's tile; GATHER: the one behind it
+    const int first_seq = seq;
     int apar = 0;                                                // GATHER: parity of A's tile
     // GROUPED: every XCD starts an eighth of K further on and turns round at its end (at slab `turn` of a tile)
     const int begin_k = GROUPED ? xcd * (g.K / (2 * BK)) / NUM_XCD * (2 * BK) : 0, turn = GROUPED ? (g.K - begin_k) / BK : 0;
@@ -147,13 +150,16 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     };
     auto set_tile_a = [&](int s) {
         if constexpr (!ONE) {
-            const Tile t = tile_at(s);
+            // GROUPED: B's stream has moved on to this tile just before
+            const Tile t = GROUPED ? tb : tile_at(s);
             aKT = range_slabs(s);
             set_rows(t, s, apar);
         }
     };
     auto set_tile_b = [&](int s) {
-        tb = tile_at(s);
+        // (GATHER: looked up a tile ahead, for its row numbers.  A look-up is a few hundred clocks of every wave.)
+        tb = GATHER && s != first_seq ? tn : tile_at(s);
+        if (GATHER && s + nslot < seq_end) tn = tile_at(s + nslot);
         if constexpr (ONE) set_rows(tb, s, bpar);
         bKT = range_slabs(s);
         ib = g.Bt + (int64_t)tb.n0 * g.ldb + range_start(s);
@@ -184,8 +190,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         }
         if constexpr (GATHER) {                                  // the next tile's row numbers, a wave for every 64
             if (which == 0 && ch < BM && bseq + nslot < seq_end) {
-                const Tile t = tile_at(bseq + nslot);
-                dma4s((uint32_t)min(ch + lane, t.end - 1 - t.m0) * 4u, reinterpret_cast<const float*>(args.row_index + t.m0),
+                dma4s((uint32_t)min(ch + lane, tn.end - 1 - tn.m0) * 4u, reinterpret_cast<const float*>(args.row_index + tn.m0),
                       __builtin_amdgcn_readfirstlane(lds_offset(row_number + (par ^ 1) * BM + ch)));
             }
         }
@@ -261,8 +266,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         if (tid < BM) row_number[tid] = args.row_index[t.m0 + min(tid, t.end - 1 - t.m0)];
         __syncthreads();
     }
-    set_tile_a(seq);
-    set_tile_b(seq);
+    if constexpr (GROUPED) { set_tile_b(seq); set_tile_a(seq); }
+    else { set_tile_a(seq); set_tile_b(seq); }
 #pragma unroll
     for (int t = -5; t < 0; ++t) {
         const int pb = t + NSB - 1, pa = t + NSA - 1;              // twice the pair whose turn it is
@@ -284,7 +289,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
 
     int rda = 0, rdb = 0, par = 0;                                  // LDS offsets of the current slab
     for (;;) {
-        const Tile tile = tile_at(seq);
+        // GROUPED: B's stream is on this tile (it runs at most five slabs ahead, and a tile has eight)
+        const Tile tile = GROUPED ? tb : tile_at(seq);
         const int m0 = tile.m0, n0 = tile.n0;
         const int KT = range_slabs(seq);
         constexpr int CI = WIDE ? TM : TI, CJ = WIDE ? TN : TJ, CR = WIDE ? 16 : 4;
@@ -567,13 +573,11 @@ hero_status launch_persistent_part(const GemmArgs& g, int rows, hipStream_t st) 
 
 // Grouped products: 256 x 256, or 128 x 128 with two workgroups per CU.  K >= 512 bytes, a multiple of 128.
 template <int ADT, int EPI, int CDT>
-hero_status launch_grouped_tile(const GroupedArgs& ga, int form, hipStream_t st) {
-    const int rows = form >= GROUPED_256 ? 256 : 128;
+hero_status launch_grouped_tile(const GroupedArgs& ga, int rows, hipStream_t st) {
     auto go = [&](auto R, auto GATHER) {
         constexpr int BM = decltype(R)::value, BN = BM, W = BM == 256 ? 4 : 2, NA = 4, NB = BM == 256 ? 5 : 4, PER_CU = BM == 256 ? 1 : 2;
         GroupedArgs a = ga;
         a.g.ntn = (a.g.N + BN - 1) / BN;
-        a.height = (form - BM) * (BM / 4);                             // (GROUPED_256 + q, GROUPED_128 + q: q quarters)
         const int64_t tiles = most_row_tiles(a.g.M, a.E, BM / 4) * a.g.ntn, per = (tiles + NUM_XCD - 1) / NUM_XCD;
         if (tiles > 0x7fffff00LL) return HERO_ERR_SHAPE;
         const int nslot = per < 32 * PER_CU ? (int)per : 32 * PER_CU;
