@@ -568,30 +568,42 @@ class Hero:
         """What the products by expert share: (the result, their device, the arguments in front of, between and behind the vectors)."""
         E, N, K = W.shape
         expert_stride, ldb, step = W.stride()
-        if E > 0 and N > 0 and (step != 1 or A.element_size() != W.element_size()):
-            raise ValueError("weights are [E, N, K] with K contiguous, of the rows' type")
-        R = MA = A.shape[0]
-        dev, index = A.get_device(), None
+        dev, rows = A.get_device(), A.shape
+        R = MA = rows[0]
+        index = None
         if row_index is not None:
             R = row_index.shape[0]
-            index = _vector(row_index, torch.int32, R)
+            if row_index.dtype is not torch.int32 or row_index.dim() != 1 or not row_index.is_contiguous() or row_index.get_device() != dev:
+                _one_device(dev, row_index)
+                _vector(row_index, torch.int32, R)
+            index = row_index.data_ptr()
         if C_out is None:
             C_out = torch.empty((R, N), dtype=out_dtype, device=A.device)
         elif C_out.shape[0] != R:
             raise ValueError(f"the result has a row for each of the {R} rows, not {C_out.shape[0]}")
-        if not (W.get_device() == offsets.get_device() == C_out.get_device() == dev) or (index is not None and row_index.get_device() != dev):
-            _one_device(dev, W, offsets, row_index, C_out)
+        if step != 1 and E > 0 and N > 0:
+            raise ValueError("weights are [E, N, K] with K contiguous")
+        if not (W.get_device() == offsets.get_device() == C_out.get_device() == dev):
+            _one_device(dev, W, offsets, C_out)
+        if offsets.dtype is not torch.int32 or offsets.shape != (E + 1,) or not offsets.is_contiguous():
+            _vector(offsets, torch.int32, E + 1)
         return (C_out, dev, (A.data_ptr(), _matrix(A, K), MA), (index, W.data_ptr(), ldb if N > 1 else max(K, ldb), expert_stride),
-                (C_out.data_ptr(), _DT[C_out.dtype], _matrix(C_out, N), _vector(offsets, torch.int32, E + 1), E, R, N, K))
+                (C_out.data_ptr(), _DT[C_out.dtype], _matrix(C_out, N), offsets.data_ptr(), E, R, N, K))
 
     def _gemm_grouped8(self, fn, dt, A, W, offsets, row_index, a_row_scale, b_col_scale, bias, epi, out_col_scale, out_dtype, C_out, stream, tile):
         if out_dtype is None and C_out is None:
             out_dtype = torch.bfloat16 if epi in (EPI_DEQUANT, EPI_DEQUANT_GELU) else torch.int8 if dt == I8 else torch.float8_e4m3fn
         C_out, dev, front, weights, back = self._grouped(A, W, offsets, row_index, out_dtype, C_out)
         EN = W.shape[:2]
-        args = (*front, None if a_row_scale is None else _floats(a_row_scale, A.shape[:1], dev), *weights, _floats(b_col_scale, EN, dev),
-                _floats(bias, EN, dev), epi, _floats(out_col_scale, EN, dev), *back, _stream_on(dev, stream))
-        self._check(fn(*args) if tile is None else self.lib.hero_gemm_grouped_tile(dt, *args, int(tile)))
+        rs = None if a_row_scale is None else _floats(a_row_scale, A.shape[:1], dev)
+        cs = None if b_col_scale is None else _floats(b_col_scale, EN, dev)
+        b = None if bias is None else _floats(bias, EN, dev)
+        os = None if out_col_scale is None else _floats(out_col_scale, EN, dev)
+        st = _stream_on(dev, stream)
+        if tile is None:
+            self._check(fn(*front, rs, *weights, cs, b, epi, os, *back, st))
+        else:
+            self._check(self.lib.hero_gemm_grouped_tile(dt, *front, rs, *weights, cs, b, epi, os, *back, st, int(tile)))
         return C_out
 
     def hero_int8_gemm_grouped(self, A, W, offsets, row_index=None, a_row_scale=None, b_col_scale=None, bias=None, epi=EPI_DEQUANT,

@@ -179,26 +179,34 @@ inline bool grouped_ring_ok(const GroupedArgs& a) {
 // .. and the persistent kernel, which looks ahead
 inline bool grouped_tile_ok(const GroupedArgs& a) { return grouped_ring_ok(a) && a.g.K >= 8 * BK; }
 
+// The rule goes by what the host knows: the rows of an expert, were all of them equal.  While they are few, the weights' bytes are all there is, and what
+// decides is whether every CU streams its share: the smallest tiles, with K groups, while they are no more than the CUs; then the ring's tiles, 64 x 64 three
+// and 128 x 64 two to a CU, or 128 x 128 persistent ones, two to a CU, by the rounds that they make times what a round brings in; with more rows 128 x 128
+// or 256 x 256, by rounds again.  us, 32x32 K4, 32x64 K2, 64x64 K2, 64x64, 128x64 ring tiles, 128x128, 256x256 persistent ones, weights from memory:
+//   INT8 2 rows of 8 experts x 4096 x 4096 9.0 10.0 10.6 12.2 14.1 20.9 40.7;  128 of 16 x 1024 x 4096 16.7 13.9 14.2 13.6 14.8 21.7 40.9
+//   BF16 512 of 16 x 1024 x 4096 39.4 37.4 26.5 31.6 34.4 56.9 84.5;  INT8 128 of 8 x 4096 x 16384 105 93.8 93.6 93.8 98.6 117 166
+//   INT8 512 of 8 x 4096 x 4096 69 50 41 36 33 36 50;  2048 of 64 x 2048 x 1024 93 58 49 33 39 32 39;  2048 of 8 x 4096 x 4096 206 145 100 78 68 70 57
+// Over 180 problems of 1 to 32768 rows, 2 to 256 experts, every type, the choice takes 1.02 times the best form's time on average and 1.22 times at most.
 inline int grouped_form(const GroupedArgs& a) {
     const int64_t R = a.g.M, N = a.g.N, active = a.E < R ? a.E : R, n = R / active;       // rows of an expert, were none empty
-    auto cols = [&](int bn) { return (N + bn - 1) / bn; };
-    auto tiles = [&](int bm, int bn) { return (n <= bm / 2 ? active : (R + active * bm / 2) / bm) * cols(bn); };      // (the last tile of an expert: half full)
+    // Tiles: of experts of few rows one each, of others as many as fill, the last one half full.  (What few is: to the ring a second row tile is a second
+    // stream of the weights, and experts are not equal.)
+    auto tiles = [&](int bm, int bn, int few) { return (n <= few ? active : (R + active * bm / 2) / bm) * ((N + bn - 1) / bn); };
+    auto rounds = [](int64_t t, int slots) { return (t + slots - 1) / slots; };
     if (!grouped_ring_ok(a)) return GROUPED_ANY;
-    const bool pers = grouped_tile_ok(a);
-    if (n <= 32) {
-        if (active * cols(32) <= 320) return GROUPED_RING + RING_32x32_K4;
-        if (active * cols(64) <= 256) return GROUPED_RING + RING_32x64_K2;
-    }
-    if (n <= 48 && active * cols(64) <= 256) return GROUPED_RING + RING_64x64_K2;
-    if (n <= 20 || (n <= 48 && active * cols(128) < 512) || !pers) return GROUPED_RING + (n <= 48 ? RING_64x64 : RING_128x64);
-    if (n <= 160 && tiles(128, 128) < 512) return GROUPED_RING + RING_128x64;
+    if (tiles(32, 32, 16) <= 256) return GROUPED_RING + RING_32x32_K4;
+    if (tiles(32, 64, 16) <= 256) return GROUPED_RING + RING_32x64_K2;
+    if (tiles(64, 64, 32) <= 256) return GROUPED_RING + RING_64x64_K2;
+    const int64_t t128 = tiles(128, 128, 96), c128 = 4 * rounds(t128, 512);
+    const int64_t ring = n <= 56 ? 3 * rounds(tiles(64, 64, 32), 768) : 2 * rounds(tiles(128, 64, 64), 512);
+    if (!grouped_tile_ok(a) || ((n <= 32 || t128 <= 512) && ring < c128)) return GROUPED_RING + (n <= 56 ? RING_64x64 : RING_128x64);
     // what the busiest CU has to do, in hundredths of a 256 x 256 tile, as best_height() will see it; a 128 x 128 tile costs 0.36 of one
-    int64_t most = INT64_MAX;
+    int64_t least = INT64_MAX;
     for (int q = 0; q < 4; ++q) {
-        const int64_t cost = (tiles(64 * (q + 1), 256) + 255) / 256 * GROUPED_COST[q];
-        if (cost < most) most = cost;
+        const int64_t cost = rounds(tiles(64 * (q + 1), 256, 48 * (q + 1)), 256) * GROUPED_COST[q];
+        if (cost < least) least = cost;
     }
-    return (tiles(128, 128) + 255) / 256 * 36 <= most ? GROUPED_128 : GROUPED_256;
+    return n <= 32 || rounds(t128, 256) * 36 <= least ? GROUPED_128 : GROUPED_256;
 }
 
 }  // namespace hero_gemm

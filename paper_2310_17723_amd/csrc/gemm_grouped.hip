@@ -20,7 +20,7 @@ hero_status check(const Request& q, hero_dtype dt, bool* noop) {
     const bool hp = dt == HERO_BF16 || dt == HERO_F16;
     const int es = hp ? 2 : 1;
     if (q.E < 0 || q.R < 0 || q.N < 0 || q.K <= 0 || q.MA < 0) return HERO_ERR_SHAPE;
-    if (q.R >= (1LL << 23) || q.N > 0x7fffffffLL || q.K > 0x7fffffffLL / es || q.MA > 0x7fffffffLL) return HERO_ERR_SHAPE;
+    if (q.R >= (1LL << 23) || q.N > 0x7fffff00LL || q.K > 0x7fffffffLL / es || q.MA > 0x7fffffffLL) return HERO_ERR_SHAPE;
     if (q.E > MAX_EXPERTS || q.K * es % KMULT != 0) return HERO_ERR_UNSUPPORTED;
     if (q.lda < q.K || q.ldb < q.K || q.ldc < q.N || q.expert_stride < 0) return HERO_ERR_SHAPE;
     const bool c16 = q.c_dt == HERO_F16 || q.c_dt == HERO_BF16;
@@ -124,7 +124,7 @@ extern "C" hero_status hero_gemm_grouped_tile(hero_dtype dt, const void* A, int6
                                               hero_epilogue epi, const float* out_col_scale, void* C, hero_dtype c_dt, int64_t ldc,
                                               const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K, void* stream, int tile) {
     if (dt != HERO_I8 && dt != HERO_F8E4M3 && dt != HERO_BF16 && dt != HERO_F16) return HERO_ERR_UNSUPPORTED;
-    if (tile < 0 || (tile > GROUPED_ANY && tile < GROUPED_RING) || (tile >= GROUPED_RING + RING_128x256 && tile != GROUPED_128 && tile != GROUPED_256)) return HERO_ERR_UNSUPPORTED;
+    if (tile < 0 || (tile > GROUPED_ANY && tile < GROUPED_RING) || (tile > GROUPED_RING + RING_128x64 && tile != GROUPED_128 && tile != GROUPED_256)) return HERO_ERR_UNSUPPORTED;
 
     const Request q{A, lda, MA, a_row_scale, row_index, Bt, ldb, expert_stride, b_col_scale, bias, epi, out_col_scale, C, c_dt, ldc, offsets, E, R, N, K};
     return run(q, dt, tile, stream);

@@ -277,7 +277,6 @@ hero_status launch_grouped_ring(const GroupedArgs& ga, RingForm f, hipStream_t s
     case RING_64x64_K2: HERO_RING(64, 64, 2, 2, 2, 3);
     case RING_64x64:    HERO_RING(64, 64, 2, 2, 1, 3);
     case RING_128x64:   HERO_RING(128, 64, 2, 2, 1, 3);
-    case RING_128x128:  HERO_RING(128, 128, 4, 2, 1, 4);
     default: return HERO_ERR_UNSUPPORTED;
     }
 #undef HERO_RING

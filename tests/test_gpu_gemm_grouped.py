@@ -10,7 +10,7 @@ from parity import to_np
 
 pytestmark = pytest.mark.gpu
 
-TILES = [None, 1, 17, 18, 21, 22, 24, 25, 128, 256]                                          # the library's choice of a kernel, and each kernel
+TILES = [None, 1, 17, 18, 21, 22, 24, 128, 256]                                          # the library's choice of a kernel, and each kernel
 HP = {"bf16": torch.bfloat16, "f16": torch.float16}
 
 
@@ -140,7 +140,7 @@ COUNTS = [[1], [0, 3, 0, 16, 1], [17, 0, 0, 40, 15, 33, 16], [5] * 70, [0, 0, 13
 
 @pytest.mark.parametrize("tile", TILES)
 @pytest.mark.parametrize("fmt", ["i8", "e4m3", "bf16", "f16"])
-@pytest.mark.parametrize("counts", COUNTS, ids=str)
+@pytest.mark.parametrize("counts", COUNTS, ids=lambda c: f"{sum(c)}of{len(c)}")
 def test_rows_of_experts(hero, counts, fmt, tile):
     for i, (N, K, tokens) in enumerate(((64, 256, 0), (100, 512, 50), (259, 128, 7), (300, 640, 0), (513, 1152, 300))):
         if not _runs(tile, fmt, K):
@@ -271,6 +271,86 @@ def test_other_stream_and_replayed_with_other_offsets(hero):
         graph.replay()
         torch.cuda.synchronize()
         p.check(out, offsets=o)
+
+
+@pytest.mark.parametrize("tile", [None, 1])
+def test_rows_gathered_from_beyond_4_gb(hero, tile):
+    """Rows whose byte offsets pass 32 bits: the kernels with 32-bit offsets do not take them."""
+    MA, K, N = 1_100_000, 4096, 48
+    A = torch.zeros((MA, K), dtype=torch.int8, device="cuda")
+    idx = torch.tensor([0, MA - 1, 524_288, 1_048_576, 1_048_575, MA - 2, 77], dtype=torch.int32)
+    g = torch.Generator().manual_seed(1)
+    rows = torch.randint(-127, 128, (7, K), generator=g).to(torch.int8)
+    A[idx.long().cuda()] = rows.cuda()
+    W = torch.randint(-127, 128, (2, N, K), generator=g).to(torch.int8)
+    off, cs = torch.tensor([0, 3, 7], dtype=torch.int32), torch.full((2, N), 1e-4)
+    rs = torch.ones(MA, device="cuda")
+    rs[idx.long().cuda()] = torch.arange(1.0, 8.0, device="cuda")
+    got = hero.hero_int8_gemm_grouped(A, W.cuda(), off.cuda(), row_index=idx.cuda(), a_row_scale=rs, b_col_scale=cs.cuda(), tile=tile)
+    for e, (a, b) in enumerate(((0, 3), (3, 7))):
+        want = O.int8_gemm(rows[a:b].numpy(), W[e].numpy(), a_row_scale=np.arange(1.0, 8.0, dtype=np.float32)[a:b], b_col_scale=cs[e].numpy(), epi=HB.EPI_DEQUANT, c_dt=O.BF16)
+        assert np.array_equal(to_np(got[a:b]).view(np.uint8), want.view(np.uint8))
+    assert tile != 1 or hero.lib.hero_gemm_grouped_tile(HB.I8, 0x10000, K, MA, None, 0x10000, 0x10000, K, N * K, 0x10000, None, HB.EPI_DEQUANT, None, 0x10000, HB.BF16, 48,
+                                                        0x10000, 2, 7, N, K, None, 22) == 4
+
+
+@pytest.mark.parametrize("tile", [None, 1, 22, 128, 256])
+def test_weights_and_results_beyond_4_gb(hero, tile):
+    N, K, E = 8192, 8192, 70                                              # 4.7 GB of weights
+    W = torch.zeros((E, N, K), dtype=torch.int8, device="cuda")
+    g = torch.Generator().manual_seed(2)
+    W[0, :64], W[E - 1, -64:], W[E - 2, :64] = (torch.randint(-127, 128, (64, K), generator=g).to(torch.int8).cuda() for _ in range(3))
+    A = torch.randint(-127, 128, (9, K), generator=g).to(torch.int8).cuda()
+    off = torch.zeros(E + 1, dtype=torch.int32)
+    off[1:], off[E - 1], off[E] = 2, 5, 9                                 # rows 0, 1: expert 0; 2 .. 4: the last but one; 5 .. 8: the last
+    cs = torch.full((E, N), 1e-4, device="cuda")
+    got = hero.hero_int8_gemm_grouped(A, W, off.cuda(), b_col_scale=cs, tile=tile).float()
+    for rows, e in ((slice(0, 2), 0), (slice(2, 5), E - 2), (slice(5, 9), E - 1)):
+        want = hero.hero_int8_gemm(A[rows].contiguous(), W[e], b_col_scale=cs[e], epi=HB.EPI_DEQUANT, out_dtype=torch.bfloat16).float()
+        assert torch.equal(got[rows], want)
+    del W
+    R, N, K = 300_000, 8192, 512                                          # 4.9 GB of results
+    W = torch.randint(-127, 128, (2, N, K), generator=g).to(torch.int8).cuda()
+    few = torch.randint(-127, 128, (64, K), generator=g).to(torch.int8).cuda()
+    idx = (torch.arange(R, device="cuda") % 64).int()
+    out = torch.zeros((R, N), dtype=torch.bfloat16, device="cuda")
+    off = torch.tensor([0, 150_000, R - 5], dtype=torch.int32, device="cuda")
+    hero.hero_int8_gemm_grouped(few, W, off, row_index=idx, b_col_scale=cs[:2].contiguous(), C_out=out, tile=tile)
+    for at in (0, 149_936, 262_144, 299_900):
+        n, e = 64, int(at >= 150_000)
+        n = min(n, R - 5 - at)
+        want = hero.hero_int8_gemm(few[idx[at:at + n].long()].contiguous(), W[e], b_col_scale=cs[e], epi=HB.EPI_DEQUANT, out_dtype=torch.bfloat16)
+        assert torch.equal(out[at:at + n], want)
+    assert (out[R - 5:] == 0).all()
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_one_weight_matrix_for_every_expert(hero, tile):
+    """An expert stride of 0 (a view): read only."""
+    p = Problem("i8", [9, 40, 0, 3], 64, 512, 20, seed=3)
+    p.W = np.repeat(p.W[:1], 4, 0)
+    W = torch.from_numpy(p.W[:1]).cuda().expand(4, -1, -1)
+    wide = torch.full((p.R, p.N * 2), 91, dtype=torch.uint8, device="cuda")
+    out = hero.hero_int8_gemm_grouped(torch.from_numpy(p.A).cuda(), W, torch.from_numpy(p.offsets).cuda(), row_index=torch.from_numpy(p.row_index).cuda(),
+                                      a_row_scale=torch.from_numpy(p.rs).cuda(), b_col_scale=torch.from_numpy(p.cs).cuda(), bias=torch.from_numpy(p.bias).cuda(),
+                                      C_out=wide.view(torch.bfloat16), tile=tile)
+    p.check(out)
+
+
+def test_two_calls_at_once(hero):
+    """Nothing is shared between calls: two streams, each with its results."""
+    ps = [Problem("i8", [300, 0, 77, 500], 700, 1024, 400, seed=s) for s in (1, 2)]
+    streams, outs = [torch.cuda.Stream() for _ in ps], []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        outs = []
+        for p, s in zip(ps, streams):
+            with torch.cuda.stream(s):
+                outs.append(p.run(hero, stream=s))
+    torch.cuda.synchronize()
+    for p, o in zip(ps, outs):
+        p.check(o)
 
 
 def test_nothing_to_do(hero):
