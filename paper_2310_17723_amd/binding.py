@@ -546,7 +546,9 @@ class Hero:
             out = self.moe_routing(T, E, top_k, logits.device)
         if workspace is None:
             need = self.hero_moe_route_workspace_bytes(T, E, top_k)
-            workspace = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+            if need:                                             # (the stream's memory: it is given back before the kernels are done with it)
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
         expert, weight, slot, token, offsets = out
         dev = logits.get_device()
         if not (expert.get_device() == weight.get_device() == slot.get_device() == token.get_device() == offsets.get_device() == dev) or (

@@ -137,6 +137,24 @@ def test_the_same_call_again_on_another_stream_and_replayed(hero, T):
         _check(hero, x, 4, got=out)
 
 
+def test_a_workspace_of_its_own_is_not_given_away_while_the_call_runs(hero):
+    """The call makes its workspace and lets go of it before the stream has come to the kernels: what the current stream is then given is other memory."""
+    T = 20000
+    x = _logits(T, 64, "bf16", 3)
+    d, out, side = x.cuda(), hero.moe_routing(T, 64, 4), torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy = busy @ busy
+    hero.hero_moe_route(d, 4, out=out, stream=side)
+    need = hero.hero_moe_route_workspace_bytes(T, 64, 4)
+    other = [torch.full((need,), 0x7f, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    _check(hero, x, 4, got=out)
+    assert all((o == 0x7f).all() for o in other)
+
+
 # ---------------------------------------------------------------------------------------- the weighted sum
 def _combine_case(T, k, D, dt, seed, rows=None):
     g = torch.Generator().manual_seed(seed)
