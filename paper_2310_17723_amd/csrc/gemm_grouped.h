@@ -186,7 +186,7 @@ inline bool grouped_tile_ok(const GroupedArgs& a) { return grouped_ring_ok(a) &&
 //   INT8 2 rows of 8 experts x 4096 x 4096 9.0 10.0 10.6 12.2 14.1 20.9 40.7;  128 of 16 x 1024 x 4096 16.7 13.9 14.2 13.6 14.8 21.7 40.9
 //   BF16 512 of 16 x 1024 x 4096 39.4 37.4 26.5 31.6 34.4 56.9 84.5;  INT8 128 of 8 x 4096 x 16384 105 93.8 93.6 93.8 98.6 117 166
 //   INT8 512 of 8 x 4096 x 4096 69 50 41 36 33 36 50;  2048 of 64 x 2048 x 1024 93 58 49 33 39 32 39;  2048 of 8 x 4096 x 4096 206 145 100 78 68 70 57
-// Over 180 problems of 1 to 32768 rows, 2 to 256 experts, every type, the choice takes 1.02 times the best form's time on average and 1.22 times at most.
+// Over 360 problems of 1 to 32768 rows, 2 to 256 experts, every type, the choice takes 1.02 times the best form's time on average and 1.24 times at most.
 inline int grouped_form(const GroupedArgs& a) {
     const int64_t R = a.g.M, N = a.g.N, active = a.E < R ? a.E : R, n = R / active;       // rows of an expert, were none empty
     // Tiles: of experts of few rows one each, of others as many as fill, the last one half full.  (What few is: to the ring a second row tile is a second
