@@ -110,6 +110,27 @@ def test_many_workgroups(hero):
     assert np.array_equal(got.offsets.cpu().numpy(), np.searchsorted(flat[order], np.arange(E + 1)))
 
 
+@pytest.mark.parametrize("T,E,k,same", [(32768, 32, 2, True), (32768, 29, 3, False), (32769, 3, 1, True), (8192, 128, 4, False), (8177, 68, 5, True), (8193, 128, 4, False),
+                                        (40000, 70, 2, False), (4099, 500, 7, False)])
+def test_many_tokens(hero, T, E, k, same):
+    """Counts added by the workgroups that place the rows, or by a scan, on either side of the choice; every token with the same experts: the largest sums."""
+    l = _logits(T, E, "bf16", T + E)
+    if same:
+        l[:, E // 2] = 1000
+    l[T // 2:T // 2 + 99] = -torch.inf
+    got = hero.hero_moe_route(l.cuda(), k)
+    v, i = l.float().sort(dim=1, descending=True, stable=True)
+    flat = torch.where(v[:, :k] > -torch.inf, i[:, :k], E).reshape(-1).numpy()
+    order = np.argsort(flat, kind="stable")
+    n = int((flat < E).sum())
+    slot = np.empty(T * k, np.int64)
+    slot[order] = np.arange(T * k)
+    assert np.array_equal(got.expert.cpu().numpy().reshape(-1), np.where(flat < E, flat, -1))
+    assert np.array_equal(got.offsets.cpu().numpy(), np.searchsorted(flat[order], np.arange(E + 1)))
+    assert np.array_equal(got.slot.cpu().numpy().reshape(-1), np.where(flat < E, slot, -1))
+    assert np.array_equal(got.row_token.cpu().numpy(), np.where(np.arange(T * k) < n, order // k, -1))
+
+
 def test_no_tokens(hero):
     got = hero.hero_moe_route(torch.empty((0, 6), device="cuda"), 2)
     assert got.offsets.tolist() == [0] * 7 and got.row_token.numel() == 0
