@@ -57,7 +57,7 @@ hero_status hero_kv_attn_tile(const hero_kv_cache* cache, const void* q, const i
 /* hero_int8_gemm_grouped, hero_fp8_gemm_grouped and hero_hp_gemm_grouped (dt HERO_I8, HERO_F8E4M3, HERO_BF16, HERO_F16; the 16-bit types
  * take epi HERO_EPI_DEQUANT or HERO_EPI_DEQUANT_GELU, no scales, and c_dt == dt) with the kernel forced.  tile: 1 = the kernel of every size;
  * 17 / 18 / 21 / 22 / 24 = the ring kernel, 16 + its form as in hero_gemm_kernel (K a multiple of 128 bytes, rows less than 16 MB apart, rows
- * to gather from within 4 GB); 128 / 256 = the persistent kernel with tiles of 128x128 / 256x256 (of these with K of 512 bytes or more); 0 = the library's
+ * to gather from within 4 GB); 128 / 256 / 384 = the persistent kernel with tiles of 128x128 / 256x256 / 256x128 (of these with K of 512 bytes or more); 0 = the library's
  * own choice; else HERO_ERR_UNSUPPORTED. */
 hero_status hero_gemm_grouped_tile(hero_dtype dt, const void* A, int64_t lda, int64_t MA, const float* a_row_scale, const int32_t* row_index,
                                    const void* Bt, int64_t ldb, int64_t expert_stride, const float* b_col_scale, const float* bias,

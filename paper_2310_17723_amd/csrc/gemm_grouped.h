@@ -1,5 +1,6 @@
 // What the kernels of products grouped by expert share: their arguments, and which rows of which expert a tile holds.
 #pragma once
+#include <math.h>
 #include "gemm_common.h"
 
 namespace hero_gemm {
@@ -165,13 +166,13 @@ inline int64_t most_row_tiles(int64_t R, int64_t E, int BM) {
 }
 
 // Which kernel: the numbers of include/hero_debug.h (hero_gemm_grouped_tile)
-enum GroupedForm { GROUPED_ANY = 1, GROUPED_RING = 16 /* + RingForm */, GROUPED_128 = 128, GROUPED_256 = 256 };
+enum GroupedForm { GROUPED_ANY = 1, GROUPED_RING = 16 /* + RingForm */, GROUPED_128 = 128, GROUPED_256 = 256, GROUPED_256x128 = 384 };
 // gemm_grouped_rows.hip: every size
 hero_status launch_grouped_rows(const GroupedArgs& a, hero_dtype adt, hipStream_t st);
 // gemm_ring.h: one tile per workgroup
 template <int ADT, int EPI, int CDT> hero_status launch_grouped_ring(const GroupedArgs& a, RingForm f, hipStream_t st);
-// gemm_persistent.h: tiles of 256 x 256 or 128 x 128 (`rows` 256 or 128)
-template <int ADT, int EPI, int CDT> hero_status launch_grouped_tile(const GroupedArgs& a, int rows, hipStream_t st);
+// gemm_persistent.h: tiles of 256 x 256, 256 x 128 or 128 x 128
+template <int ADT, int EPI, int CDT> hero_status launch_grouped_tile(const GroupedArgs& a, int tile, hipStream_t st);
 // The sizes that the ring kernel takes: whole slabs, and 32-bit offsets per lane (of a tile's rows, or of all rows that may be gathered)
 inline bool grouped_ring_ok(const GroupedArgs& a) {
     return a.g.K % (2 * BK) == 0 && ring_ok(a.g.lda, a.g.ldb) && (!a.row_index || (int64_t)a.MA * a.g.lda <= (1LL << 32));
@@ -179,34 +180,52 @@ inline bool grouped_ring_ok(const GroupedArgs& a) {
 // .. and the persistent kernel, which looks ahead
 inline bool grouped_tile_ok(const GroupedArgs& a) { return grouped_ring_ok(a) && a.g.K >= 8 * BK; }
 
-// The rule goes by what the host knows: the rows of an expert, were all of them equal.  While they are few, the weights' bytes are all there is, and what
-// decides is whether every CU streams its share: the smallest tiles, with K groups, while they are no more than the CUs; then the ring's tiles, 64 x 64 three
-// and 128 x 64 two to a CU, or 128 x 128 persistent ones, two to a CU, by the rounds that they make times what a round brings in; with more rows 128 x 128
-// or 256 x 256, by rounds again.  us, 32x32 K4, 32x64 K2, 64x64 K2, 64x64, 128x64 ring tiles, 128x128, 256x256 persistent ones, weights from memory:
-//   INT8 2 rows of 8 experts x 4096 x 4096 9.0 10.0 10.6 12.2 14.1 20.9 40.7;  128 of 16 x 1024 x 4096 16.7 13.9 14.2 13.6 14.8 21.7 40.9
-//   BF16 512 of 16 x 1024 x 4096 39.4 37.4 26.5 31.6 34.4 56.9 84.5;  INT8 128 of 8 x 4096 x 16384 105 93.8 93.6 93.8 98.6 117 166
-//   INT8 512 of 8 x 4096 x 4096 69 50 41 36 33 36 50;  2048 of 64 x 2048 x 1024 93 58 49 33 39 32 39;  2048 of 8 x 4096 x 4096 206 145 100 78 68 70 57
-// Over 360 problems of 1 to 32768 rows, 2 to 256 experts, every type, the choice takes 1.02 times the best form's time on average and 1.24 times at most.
+// The choice goes by an estimate of each form's time (us) from what the host knows: a round of tiles takes start + slab times the 128-byte slabs of K, a first one
+// that fills the slots to r only alone + (1 - alone) r of that, a last one two fifths more than its share; the weights of the experts that can have a row come at 5.4 TB/s, and
+// the lesser of the two times shows to 15 %.  Fitted, a form at a time, to 420 problems of 1 to 32768 rows, 2 to 256 experts, every type, drawn at random, weights from memory.  Over 80
+// others the choice takes 1.022 times the best form's time (1.26 at most), over 120 of 40 to 700 rows an expert 1.030 (1.55); by the number of tiles to a CU alone 1.029 and 1.052.
+struct FormTime { int form, bm, bn, slots; float start, slab, alone; };
+constexpr FormTime FORM_TIMES[] = {
+    {GROUPED_RING + RING_32x32_K4, 32, 32, 256, 3.16f, 0.111f, 0.86f}, {GROUPED_RING + RING_32x64_K2, 32, 64, 256, 3.27f, 0.187f, 0.87f},
+    {GROUPED_RING + RING_64x64_K2, 64, 64, 256, 3.46f, 0.246f, 0.74f}, {GROUPED_RING + RING_64x64, 64, 64, 768, 3.21f, 0.657f, 0.38f},
+    {GROUPED_RING + RING_128x64, 128, 64, 512, 3.90f, 0.659f, 0.45f},  {GROUPED_128, 128, 128, 512, 3.97f, 1.160f, 0.44f},
+    {GROUPED_256, 256, 256, 256, 10.25f, 1.501f, 0.72f},               {GROUPED_256x128, 256, 128, 256, 5.61f, 0.944f, 1.00f}};
 inline int grouped_form(const GroupedArgs& a) {
-    const int64_t R = a.g.M, N = a.g.N, active = a.E < R ? a.E : R, n = R / active;       // rows of an expert, were none empty
-    // Tiles: of experts of few rows one each, of others as many as fill, the last one half full.  (What few is: to the ring a second row tile is a second
-    // stream of the weights, and experts are not equal.)
-    auto tiles = [&](int bm, int bn, int few) { return (n <= few ? active : (R + active * bm / 2) / bm) * ((N + bn - 1) / bn); };
-    auto rounds = [](int64_t t, int slots) { return (t + slots - 1) / slots; };
     if (!grouped_ring_ok(a)) return GROUPED_ANY;
-    if (tiles(32, 32, 16) <= 256) return GROUPED_RING + RING_32x32_K4;
-    if (tiles(32, 64, 16) <= 256) return GROUPED_RING + RING_32x64_K2;
-    if (tiles(64, 64, 32) <= 256) return GROUPED_RING + RING_64x64_K2;
-    const int64_t t128 = tiles(128, 128, 96), c128 = 4 * rounds(t128, 512);
-    const int64_t ring = n <= 56 ? 3 * rounds(tiles(64, 64, 32), 768) : 2 * rounds(tiles(128, 64, 64), 512);
-    if (!grouped_tile_ok(a) || ((n <= 32 || t128 <= 512) && ring < c128)) return GROUPED_RING + (n <= 56 ? RING_64x64 : RING_128x64);
-    // what the busiest CU has to do, in hundredths of a 256 x 256 tile, as best_height() will see it; a 128 x 128 tile costs 0.36 of one
-    int64_t least = INT64_MAX;
-    for (int q = 0; q < 4; ++q) {
-        const int64_t cost = rounds(tiles(64 * (q + 1), 256, 48 * (q + 1)), 256) * GROUPED_COST[q];
-        if (cost < least) least = cost;
+    const bool tile_ok = grouped_tile_ok(a);
+    const int R = a.g.M, N = a.g.N, active = a.E < R ? a.E : R;
+    // experts are not equal: eight of them have 0.3, 0.5, .. 1.7 times the rows that each would have
+    int of_eight[9] = {};                                           // their row tiles of 32, 64, 128, 192 and 256 rows, by 32 rows
+    for (int i = 3; i <= 17; i += 2) {
+        const int rows = (int)(((int64_t)R * i + 10 * active - 1) / (10 * active)), t64 = (rows + 63) >> 6;
+        of_eight[1] += (rows + 31) >> 5;
+        of_eight[2] += t64;
+        of_eight[4] += (t64 + 1) >> 1;
+        of_eight[6] += (t64 + 2) / 3;
+        of_eight[8] += (t64 + 3) >> 2;
     }
-    return n <= 32 || rounds(t128, 256) * 36 <= least ? GROUPED_128 : GROUPED_256;
+    auto tiles = [&](int bm, int bn) {
+        const float some = (float)of_eight[bm >> 5] * (float)active / 8, most = (float)((R + active * (bm - 1)) / bm), t = some < most ? some : most;
+        return (t > 1 ? t : 1) * (float)((N + bn - 1) / bn);
+    };
+    const float slabs = (float)(a.g.K / (2 * BK)), stream = (float)active * (float)N * (float)a.g.K / 5.4e6f;
+    int best = GROUPED_ANY;
+    float least = INFINITY;
+    for (const FormTime& f : FORM_TIMES) {
+        if (f.form >= GROUPED_128 && !tile_ok) continue;
+        if (f.bm == 256 && R / active <= 32) continue;              // (rows that are too few for their tiles, whatever the estimate)
+        float time = INFINITY;
+        for (int q = f.bm == 256 ? 0 : 3; q < 4; ++q) {             // (best_height())
+            const float r = tiles(f.bm / 4 * (q + 1), f.bn) / (float)f.slots;
+            if (f.form < GROUPED_RING + RING_64x64 && r > 1) continue;      // K groups: one round
+            const float rounds = r <= 1 ? f.alone + (1 - f.alone) * r : r + 0.4f * (ceilf(r) - r);
+            const float t = rounds * (f.start + f.slab * slabs) * (f.bm == 256 ? GROUPED_COST[q] * 0.01f : 1.0f);
+            time = t < time ? t : time;
+        }
+        time = time > stream ? time + 0.15f * stream : stream + 0.15f * time;
+        if (time < least) { least = time; best = f.form; }
+    }
+    return best;
 }
 
 }  // namespace hero_gemm

@@ -124,7 +124,7 @@ extern "C" hero_status hero_gemm_grouped_tile(hero_dtype dt, const void* A, int6
                                               hero_epilogue epi, const float* out_col_scale, void* C, hero_dtype c_dt, int64_t ldc,
                                               const int32_t* offsets, int64_t E, int64_t R, int64_t N, int64_t K, void* stream, int tile) {
     if (dt != HERO_I8 && dt != HERO_F8E4M3 && dt != HERO_BF16 && dt != HERO_F16) return HERO_ERR_UNSUPPORTED;
-    if (tile < 0 || (tile > GROUPED_ANY && tile < GROUPED_RING) || (tile > GROUPED_RING + RING_128x64 && tile != GROUPED_128 && tile != GROUPED_256)) return HERO_ERR_UNSUPPORTED;
+    if (tile < 0 || (tile > GROUPED_ANY && tile < GROUPED_RING) || (tile > GROUPED_RING + RING_128x64 && tile != GROUPED_128 && tile != GROUPED_256 && tile != GROUPED_256x128)) return HERO_ERR_UNSUPPORTED;
 
     const Request q{A, lda, MA, a_row_scale, row_index, Bt, ldb, expert_stride, b_col_scale, bias, epi, out_col_scale, C, c_dt, ldc, offsets, E, R, N, K};
     return run(q, dt, tile, stream);

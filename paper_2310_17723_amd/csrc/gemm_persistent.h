@@ -62,8 +62,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     static_assert(NSA >= 4 && NSA <= 6 && NSB >= 4 && NSB <= 6 && BM % (16 * WM) == 0 && BN % (16 * NWAVE) == 0 && (!WIDE || (NFR <= 2 * NM && BM % (32 * WM) == 0)), "rings / interleave plan");
     static_assert(!PART || (EPI == HERO_EPI_RAW_I32 && !WIDE), "a part writes raw accumulators");
     constexpr int A_RING = NSA * A_BYTES, B_RING = NSB * B_BYTES, RING = A_RING + B_RING;
-    constexpr int SVF = 4 * BN;                                  // floats per vector set: column scale, bias, S_a, row scale
-    static_assert(BM <= BN, "the row-scale vector shares the column vectors' length");
+    constexpr int SVF = 3 * BN + (BM > BN ? BM : BN);            // floats per vector set: column scale, bias, S_a, row scale
+    static_assert(BM <= BN || GROUPED, "the row-scale vector shares the column vectors' length");
     constexpr int PF_OFF = RING + 2 * SVF * 4;                   // 256 bytes per wave where the prefetch requests land (never read)
     constexpr int INDEX_OFF = PF_OFF, TABLE_OFF = INDEX_OFF + (GATHER ? 2 * BM * 4 : 0);    // GROUPED: row numbers of two tiles; the experts' tables
     constexpr int LDS = GROUPED ? TABLE_OFF + (2 * MAX_EXPERTS + 1) * 4 : PF_OFF + NWAVE * 256;
@@ -173,9 +173,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
     // two back until every wave has started the tile in between.
     auto issue_tile_vectors = [&](int par) {
         // wave w fetches 64 entries (chunk w % CH) of vectors w / CH and 2 + w / CH
-        constexpr int CH = BN / 64;
+        constexpr int CH = (BM > BN ? BM : BN) / 64;
         static_assert(NWAVE == 2 * CH, "two vectors per wave");
         const int ch = (wave % CH) * 64, which = wave / CH;
+        const bool cols = BM <= BN || ch < BN;                      // (256 x 128: a wave has no columns left)
         const uint32_t dst = svbase + par * SVF * 4 + ch * 4;
         const int vm = GATHER ? 0 : tb.m0;
         const int64_t vn = GROUPED ? (int64_t)tb.e * g.N + tb.n0 : (int64_t)tb.n0;
@@ -183,10 +184,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         const uint32_t cm = GATHER ? 0u : (uint32_t)min(ch + lane, tb.end - 1 - tb.m0) * 4u;
         if (EPI == HERO_EPI_RAW_I32) return;
         if (which == 0) {
-            if (!UNIT) dma4s(cn, g.b_col_scale + vn, dst);
-            if (EPI == HERO_EPI_GELU_REQUANT) dma4s(cn, g.out_col_scale + vn, dst + 2 * BN * 4);
+            if (!UNIT && cols) dma4s(cn, g.b_col_scale + vn, dst);
+            if (EPI == HERO_EPI_GELU_REQUANT && cols) dma4s(cn, g.out_col_scale + vn, dst + 2 * BN * 4);
         } else {
-            if (has_bias) dma4s(cn, g.bias + vn, dst + BN * 4);
+            if (has_bias && cols) dma4s(cn, g.bias + vn, dst + BN * 4);
             // (a row number is read where it is waited for, or the wait stands in the loop)
             if (has_rs) dma4s(GATHER ? source(row_number[par * BM + min(ch + lane, BM - 1)]) * 4u : cm, g.a_row_scale + vm, dst + 3 * BN * 4);
         }
@@ -608,24 +609,27 @@ hero_status launch_persistent_part(const GemmArgs& g, int rows, hipStream_t st) 
     }
 }
 
-// Grouped products: 256 x 256, or 128 x 128 with two workgroups per CU.  K >= 512 bytes, a multiple of 128.
+// Grouped products: 256 x 256, 128 x 128 with two workgroups per CU, or 256 x 128, whose rings of six slots have two pairs of slabs under way, where an expert has
+// about as many rows as a tile and there is a tile for every CU: what a pair takes there is its weights' latency.  K >= 512 bytes, a multiple of 128.  us, the better
+// of the other two / 256 x 128: 1024 rows of 8 experts x 4096 x 16384 INT8 167 / 133, BF16 341 / 288, x 4096 48.3 / 40.5, 82.7 / 68.6;  4099 uneven ones of 16 x 1024 x 4096 BF16 75 / 68.
 template <int ADT, int EPI, int CDT>
-hero_status launch_grouped_tile(const GroupedArgs& ga, int rows, hipStream_t st) {
+hero_status launch_grouped_tile(const GroupedArgs& ga, int tile, hipStream_t st) {
     auto go = [&](auto R, auto GATHER) {
-        constexpr int BM = decltype(R)::value, BN = BM, W = BM == 256 ? 4 : 2, NA = 4, NB = BM == 256 ? 5 : 4, PER_CU = BM == 256 ? 1 : 2;
+        constexpr int TILE = decltype(R)::value, BM = TILE == GROUPED_128 ? 128 : 256, BN = TILE == GROUPED_256 ? 256 : 128, WM = TILE == GROUPED_256x128 ? 4 : 2, WN = BN / 64;
+        constexpr int NA = TILE == GROUPED_256x128 ? 6 : 4, NB = TILE == GROUPED_256x128 ? 6 : TILE == GROUPED_256 ? 5 : 4, PER_CU = TILE == GROUPED_128 ? 2 : 1;
         GroupedArgs a = ga;
         a.g.ntn = (a.g.N + BN - 1) / BN;
         const int64_t tiles = most_row_tiles(a.g.M, a.E, BM / 4) * a.g.ntn, per = (tiles + NUM_XCD - 1) / NUM_XCD;
         if (tiles > 0x7fffff00LL) return HERO_ERR_SHAPE;
         const int nslot = per < 32 * PER_CU ? (int)per : 32 * PER_CU;
-        hipLaunchKernelGGL((int8_gemm_persistent_kernel<BM, BN, 2, W, NA, NB, EPI, CDT, -1, ADT, false, false, true, decltype(GATHER)::value>),
-                           dim3((unsigned)(nslot * NUM_XCD)), dim3(2 * W * 64), 0, st, a);
+        hipLaunchKernelGGL((int8_gemm_persistent_kernel<BM, BN, WM, WN, NA, NB, EPI, CDT, -1, ADT, false, false, true, decltype(GATHER)::value>),
+                           dim3((unsigned)(nslot * NUM_XCD)), dim3(WM * WN * 64), 0, st, a);
         return hero_launch_status();
     };
-    using T256 = std::integral_constant<int, 256>;
-    using T128 = std::integral_constant<int, 128>;
-    if (rows == 256) return ga.row_index ? go(T256{}, std::true_type{}) : go(T256{}, std::false_type{});
-    if (rows == 128) return ga.row_index ? go(T128{}, std::true_type{}) : go(T128{}, std::false_type{});
+    auto either = [&](auto R) { return ga.row_index ? go(R, std::true_type{}) : go(R, std::false_type{}); };
+    if (tile == GROUPED_256) return either(std::integral_constant<int, GROUPED_256>{});
+    if (tile == GROUPED_256x128) return either(std::integral_constant<int, GROUPED_256x128>{});
+    if (tile == GROUPED_128) return either(std::integral_constant<int, GROUPED_128>{});
     return HERO_ERR_UNSUPPORTED;
 }
 

@@ -10,7 +10,7 @@ from parity import to_np
 
 pytestmark = pytest.mark.gpu
 
-TILES = [None, 1, 17, 18, 21, 22, 24, 128, 256]                                          # the library's choice of a kernel, and each kernel
+TILES = [None, 1, 17, 18, 21, 22, 24, 128, 256, 384]                                          # the library's choice of a kernel, and each kernel
 HP = {"bf16": torch.bfloat16, "f16": torch.float16}
 
 
