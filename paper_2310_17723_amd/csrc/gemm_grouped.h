@@ -183,13 +183,17 @@ inline bool grouped_tile_ok(const GroupedArgs& a) { return grouped_ring_ok(a) &&
 // The choice goes by an estimate of each form's time (us) from what the host knows: a round of tiles takes start + slab times the 128-byte slabs of K, a first one
 // that fills the slots to r only alone + (1 - alone) r of that, a last one between that and its share; the weights of the experts that can have a row come at 5.4 TB/s, and
 // the lesser of the two times shows to 15 %.  Fitted, a form at a time, to 770 problems of 1 to 32768 rows, 2 to 256 experts, every type, drawn at random, weights from memory.  Over 180
-// others the choice takes 1.020 times the best form's time (1.36 at most), over 270 of 40 to 700 rows an expert 1.031 (1.39); by the number of tiles to a CU alone 1.021 and 1.044.
-struct FormTime { int form, bm, bn, slots; float start, slab, alone; };
+// others the choice takes 1.014 times the best form's time (1.33 at most), over 270 of 40 to 700 rows an expert 1.031 (1.39); by the number of tiles to a CU alone 1.021 and 1.044.
+struct FormTime { int form, bm, bn, slots; struct { float start, slab, alone; } few, many; };      // (few: up to 32 rows an expert)
 constexpr FormTime FORM_TIMES[] = {
-    {GROUPED_RING + RING_32x32_K4, 32, 32, 256, 3.92f, 0.096f, 0.80f}, {GROUPED_RING + RING_32x64_K2, 32, 64, 256, 3.60f, 0.182f, 0.85f},
-    {GROUPED_RING + RING_64x64_K2, 64, 64, 256, 3.96f, 0.224f, 0.75f}, {GROUPED_RING + RING_64x64, 64, 64, 768, 2.93f, 0.693f, 0.36f},
-    {GROUPED_RING + RING_128x64, 128, 64, 512, 3.71f, 0.692f, 0.43f},  {GROUPED_128, 128, 128, 512, 4.23f, 1.191f, 0.43f},
-    {GROUPED_256, 256, 256, 256, 9.93f, 1.513f, 0.73f},                {GROUPED_256x128, 256, 128, 256, 5.70f, 0.928f, 1.00f}};
+    {GROUPED_RING + RING_32x32_K4, 32, 32, 256, {3.94f, 0.098f, 0.78f}, {3.92f, 0.096f, 0.80f}},
+    {GROUPED_RING + RING_32x64_K2, 32, 64, 256, {3.80f, 0.186f, 0.81f}, {3.60f, 0.182f, 0.85f}},
+    {GROUPED_RING + RING_64x64_K2, 64, 64, 256, {4.05f, 0.219f, 0.76f}, {3.96f, 0.224f, 0.75f}},
+    {GROUPED_RING + RING_64x64, 64, 64, 768, {4.89f, 0.458f, 0.49f}, {2.93f, 0.693f, 0.36f}},
+    {GROUPED_RING + RING_128x64, 128, 64, 512, {4.93f, 0.492f, 0.58f}, {3.71f, 0.692f, 0.43f}},
+    {GROUPED_128, 128, 128, 512, {3.67f, 1.054f, 0.48f}, {4.23f, 1.191f, 0.43f}},
+    {GROUPED_256, 256, 256, 256, {}, {9.93f, 1.513f, 0.73f}},
+    {GROUPED_256x128, 256, 128, 256, {}, {5.70f, 0.928f, 1.00f}}};
 inline int grouped_form(const GroupedArgs& a) {
     if (!grouped_ring_ok(a)) return GROUPED_ANY;
     const bool tile_ok = grouped_tile_ok(a);
@@ -211,15 +215,16 @@ inline int grouped_form(const GroupedArgs& a) {
     const float slabs = (float)(a.g.K / (2 * BK)), stream = (float)active * (float)N * (float)a.g.K / 5.4e6f;
     int best = GROUPED_ANY;
     float least = INFINITY;
+    const bool few = R / active <= 32;
     for (const FormTime& f : FORM_TIMES) {
-        if (f.form >= GROUPED_128 && !tile_ok) continue;
-        if (f.bm == 256 && R / active <= 32) continue;              // (rows that are too few for their tiles, whatever the estimate)
+        if ((f.form >= GROUPED_128 && !tile_ok) || (f.bm == 256 && few)) continue;
+        const float start = few ? f.few.start : f.many.start, slab = few ? f.few.slab : f.many.slab, alone = few ? f.few.alone : f.many.alone;
         float time = INFINITY;
         for (int q = f.bm == 256 ? 0 : 3; q < 4; ++q) {             // (best_height())
             const float r = tiles(f.bm / 4 * (q + 1), f.bn) / (float)f.slots;
             if (f.form < GROUPED_RING + RING_64x64 && r > 1) continue;      // K groups: one round
-            const float rounds = r <= 1 ? f.alone + (1 - f.alone) * r : r + 0.6f * f.alone * (ceilf(r) - r);
-            const float t = rounds * (f.start + f.slab * slabs) * (f.bm == 256 ? GROUPED_COST[q] * 0.01f : 1.0f);
+            const float rounds = r <= 1 ? alone + (1 - alone) * r : r + 0.6f * alone * (ceilf(r) - r);
+            const float t = rounds * (start + slab * slabs) * (f.bm == 256 ? GROUPED_COST[q] * 0.01f : 1.0f);
             time = t < time ? t : time;
         }
         time = time > stream ? time + 0.15f * stream : stream + 0.15f * time;
