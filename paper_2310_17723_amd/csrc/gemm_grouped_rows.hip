@@ -45,7 +45,7 @@ __global__ __launch_bounds__(ROW_WAVES * 64, 4) void grouped_rows_kernel(Grouped
 #pragma unroll
     for (int c = 0; c < CT; ++c) pw[c] = g.Bt + (int64_t)t.e * a.expert_stride + (int64_t)min(n0 + c * 16 + r16, g.N - 1) * g.ldb + piece;
 
-    const int steps = (g.K + 127) >> 7, half = (g.K & 64) ? steps - 1 : -1;      // (the last step may be half a one)
+    const int steps = (g.K >> 7) + ((g.K >> 6) & 1), half = (g.K & 64) ? steps - 1 : -1;      // (the last step may be half a one; K goes up to 2^31 - 64)
     v4i fa[DEPTH][TM][2], fw[DEPTH][CT][2];
     auto load = [&](int s, v4i (&xa)[TM][2], v4i (&xw)[CT][2]) {
         if (s >= steps) return;                                     // (uniform)

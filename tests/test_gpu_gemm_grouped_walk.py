@@ -127,3 +127,24 @@ def test_three_tiles_and_more_to_a_workgroup(hero, tile, fmt, gathered):
 
 def test_weights_and_results_beyond_4_gb_in_tiles_of_256_by_128(hero):
     G.test_weights_and_results_beyond_4_gb(hero, 384)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3", "bf16"])
+def test_the_longest_rows(hero, fmt):
+    """K of 2^31 - 64 bytes: a number of bytes, a little more of which 32 bits do not hold."""
+    K, dt = (2 ** 31 - 64) // DTYPE[fmt].itemsize, DTYPE[fmt]
+    A, W = (torch.zeros(K, dtype=torch.uint8 if dt.itemsize == 1 else dt, device="cuda").view(dt) for _ in range(2))
+    at = [0, 1, K // 3, K // 2, K - 33, K - 2, K - 1]
+    for i, k in enumerate(at):                                            # (single elements, through the type's own conversion)
+        A[k:k + 1] = torch.tensor([i + 1.0]).to(dt).cuda()
+        W[k:k + 1] = torch.tensor([2.0]).to(dt).cuda()
+    off, want = torch.tensor([0, 1], dtype=torch.int32, device="cuda"), 2.0 * sum(range(1, len(at) + 1))
+    for tile in (None, 1):
+        out = torch.zeros((1, 4), dtype=torch.bfloat16, device="cuda")
+        kw = dict(C_out=out[:, :1], tile=tile)
+        if fmt == "bf16":
+            hero.hero_hp_gemm_grouped(A[None], W[None, None], off, **kw)
+        else:
+            fn = hero.hero_int8_gemm_grouped if fmt == "i8" else hero.hero_fp8_gemm_grouped
+            fn(A[None], W[None, None], off, b_col_scale=torch.ones((1, 1), device="cuda"), **kw)
+        assert out[0].tolist() == [want, 0, 0, 0]
