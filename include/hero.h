@@ -532,7 +532,8 @@ hero_status hero_layer_fwd_kv(const hero_layer_desc* desc, const hero_layer_weig
  *   row_token int32 [T*top_k]; offsets int32 [E+1]: all are written whole.
  *   workspace: hero_moe_route_workspace_bytes(T, E, top_k) bytes (0 for few tokens), 256-byte aligned, else HERO_ERR_WORKSPACE.  Pure scratch:
  *            calls that may overlap on the GPU need their own.
- * Constraints: 1 <= E <= 512, 1 <= top_k <= 16, top_k <= E; T * top_k < 2^31.  T == 0: offsets are written, all 0.
+ * Constraints: 1 <= E <= 512, 1 <= top_k <= 16, top_k <= E; T * top_k < 2^31, T <= 2^28 - 16 (what a launch holds; else HERO_ERR_SHAPE).  T == 0: offsets are
+ * written, all 0.
  * The results depend on the arguments alone (no order of atomics shows in them). */
 size_t hero_moe_route_workspace_bytes(int64_t T, int64_t E, int64_t top_k);
 hero_status hero_moe_route(const void* logits, hero_dtype dt, int64_t ldl, int64_t T, int64_t E, int64_t top_k, int renorm,

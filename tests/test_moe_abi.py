@@ -31,6 +31,11 @@ def test_routes_that_are_refused(lib, kw, status):
     assert _route(lib, **kw) == status
 
 
+def test_more_tokens_than_a_launch_holds(lib):
+    for T in (2 ** 28 - 15, 2 ** 28, 2 ** 31 - 1):
+        assert _route(lib, T=T, k=1, ws=P, n=1 << 50) == SHAPE
+
+
 def test_scratch_of_the_router(lib):
     size = lib.hero_moe_route_workspace_bytes
     assert size(1, 8, 2) == size(64, 512, 16) == 0
