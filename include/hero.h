@@ -577,6 +577,8 @@ hero_status hero_hp_gemm_grouped(const void* A, int64_t lda, int64_t MA, const i
 
 /* The weighted sum of every token's rows:  out[t] = residual[t] + sum_j weight[t][j] * y[slot[t][j]], in fp32 (the choices in their
  * order, the residual last), rounded once; a choice whose slot lies outside [0, R) is left out, whatever its weight.
+ *   The rows y are 16 bits, as the second linear leaves them: each has been rounded once before the sum, which is rounded once more (the dense layer, whose
+ *   second linear adds the residual itself, rounds once).
  *   y [R,D], residual [T,D] or NULL (= 0), out [T,D] in dt (HERO_BF16 / HERO_F16), leading dimensions ldy, ldr, ldo; out may be the residual
  *   itself (ldo == ldr).  slot int32 [T,top_k], weight f32 [T,top_k].
  * Constraints: D and the leading dimensions multiples of 8, base pointers 16-byte aligned, 1 <= top_k <= 16; T * D such that a launch holds it

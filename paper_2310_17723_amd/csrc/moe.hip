@@ -322,6 +322,9 @@ struct CombineArgs {
 // A thread adds 8 values of one token: the slots and weights of up to four choices, then their rows, then the sums, so that one wait covers the
 // loads of each kind (a choice after the other: 32 tokens x 4 x 1024 4.7 us, 1 x 2 x 768 2.2).  Bound by HBM: the rows, the residual and the result
 // once, 16384 tokens x 2 x 4096 in 99 us, 5.4 TB/s, a large copy's rate.
+// y is in 16 bits, half the bytes of fp32 on both sides of this kernel, which is nothing but bytes: every row is rounded before the weighted sum and the sum
+// after.  Root mean square error of a whole MLP (BF16) relative to its result, rows in fp32 / this: 32 tokens x 4 of 16 experts x 1024 x 4096 1.66e-3 / 1.84e-3,
+// 4096 x 2 of 8 x 4096 x 16384 1.66e-3 / 1.95e-3 (1.66e-3 is the rounding of the result alone).
 template <int DT, int K>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
