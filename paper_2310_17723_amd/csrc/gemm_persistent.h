@@ -141,7 +141,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
         if constexpr (GATHER) {
             ia = g.A + range_start(s);
 #pragma unroll
-            for (int u = 0; u < A_UNITS; ++u)                    // (units beyond a tile of odd height are not loaded)
+            for (int u = 0; u < A_UNITS; ++u)                    // (behind the tile's last row: that row again, as its number was fetched again)
                 oa[u] = source(row_number[p * BM + min(lrow + u * (NWAVE * 16), BM - 1)]) * (uint32_t)g.lda + lc;
         } else {
             ia = g.A + (int64_t)t.m0 * g.lda + range_start(s);
@@ -460,7 +460,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void int8_gemm_persistent_kernel(t
             }
         };
         if constexpr (GROUPED) {
-            // (in quarters of a wave's fragments; a loop for each, chosen once per tile)
+            // (in quarters of a wave's fragments, halves where it has two: E4M3's of 32 rows in tiles of 256 x 128 and 128 x 128, which so multiply 128 and 64
+            // rows at a time; a loop for each, chosen once per tile)
             constexpr int Q = CI >= 4 ? CI / 4 : 1, QUARTERS = CI / Q, UNIT_ROWS = WM * Q * (WIDE ? 32 : 16);
             constexpr int THREE = (QUARTERS > 3) ? 3 * Q : CI, TWO = (QUARTERS > 2) ? 2 * Q : CI;
             const int quarters = (tile.end - m0 + UNIT_ROWS - 1) / UNIT_ROWS;
