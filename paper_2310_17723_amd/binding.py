@@ -1,5 +1,9 @@
 """ctypes binding of libhero.so: same names as the C ABI, torch tensors in place of raw
-pointers.  Argument marshalling only."""
+pointers.  Argument marshalling only.
+
+stream=: the torch.cuda.Stream that a call is enqueued on, None for the current one.  Results that a call makes (no out= or the like) are
+memory of the CURRENT stream, as torch.empty gives it, also where stream= is another one: such a caller lets `stream` wait for the current
+stream before the call, and the current stream for `stream` before the results are used or let go of (or passes results of its own)."""
 from __future__ import annotations
 
 import ctypes as C
@@ -540,7 +544,8 @@ class Hero:
     # wrong run only where something is.  us of host time, a check for each tensor by functions of its own -> so: route 7.1 -> 4.7, sum 7.9 -> 5.0, product 11.8 -> 8.0.)
     def hero_moe_route(self, logits, top_k, renorm=True, out=None, workspace=None, stream=None) -> MoeRouting:
         """The top_k experts of every token (logits [T,E] f32 / bf16 / f16) and the order of their rows.  workspace: uint8 tensor
-        (hero_moe_route_workspace_bytes), made here if it is None and needed; out: a MoeRouting to write into (moe_routing)."""
+        (hero_moe_route_workspace_bytes), made here if it is None and needed (memory of the call's stream); out: a MoeRouting to write into
+        (moe_routing); made here if it is None, memory of the current stream: with another stream= the caller orders the two."""
         T, E = logits.shape
         if out is None:
             out = self.moe_routing(T, E, top_k, logits.device)
@@ -612,8 +617,9 @@ class Hero:
                                out_col_scale=None, out_dtype=None, C_out=None, stream=None, tile=None):
         """Rows offsets[e] .. offsets[e+1] - 1 (int32 [E+1] on the device) of A [R,K] int8, or of A[row_index] (int32 [R]), times W[e]; W
         [E,N,K] int8.  a_row_scale f32 [A's rows] or None; b_col_scale, bias, out_col_scale f32 [E,N].  Returns C [R,N]: bf16 (or
-        out_dtype float16) or, for the REQUANT epilogues, int8; rows from offsets[E] on are not written.  tile=<code> -> the test hook
-        hero_gemm_grouped_tile (include/hero_debug.h: the kernel forced)."""
+        out_dtype float16) or, for the REQUANT epilogues, int8; rows from offsets[E] on are not written.  C made here is memory of the current
+        stream: with another stream= the caller orders the two.  tile=<code> -> the test hook hero_gemm_grouped_tile (include/hero_debug.h: the
+        kernel forced)."""
         if A.dtype is not torch.int8 or W.dtype is not torch.int8:
             raise ValueError("rows and weights are int8")
         return self._gemm_grouped8(self.lib.hero_int8_gemm_grouped, I8, A, W, offsets, row_index, a_row_scale, b_col_scale, bias, epi, out_col_scale,
@@ -642,7 +648,8 @@ class Hero:
 
     def hero_moe_combine(self, y, slot, weight, residual=None, out=None, stream=None):
         """out[t] = residual[t] + sum_j weight[t][j] y[slot[t][j]]; y [R,D], residual, out [T,D] bf16 / f16 (out may be the residual itself);
-        slot int32, weight f32 [T,top_k]; slots outside [0, R) are left out."""
+        slot int32, weight f32 [T,top_k]; slots outside [0, R) are left out.  A result made here is memory of the current stream: with another
+        stream= the caller orders the two."""
         R, D = y.shape
         T, k = slot.shape
         dt, dev = y.dtype, y.get_device()
