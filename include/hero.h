@@ -556,9 +556,10 @@ hero_status hero_moe_route(const void* logits, hero_dtype dt, int64_t ldl, int64
  *        no residual (hero_moe_combine adds it).
  * Constraints: E <= 512; R < 2^23; K % 64 == 0; lda, ldb, expert_stride multiples of 16, ldc of 4; base pointers of A, Bt, C 16-byte aligned;
  * R * N such that a launch holds it (else HERO_ERR_SHAPE).  R == 0, N == 0 or E == 0 is a no-op.
- * Which kernel runs is chosen by R, E, N and K; results of 8-bit integer operands do not depend on it.  E4M3 and 16-bit operands: the order in which a
- * row's products are added (fp32) depends on the kernel and on where the row's tile lies, so on the numbers of rows of all experts: the same call
- * gives the same bits again, but the same row between other rows, or twice in one call, may differ by the rounding of its sum.
+ * Which kernel runs is chosen by R (taken as the number of rows: room for many more than there are costs time), E, N and K; results of 8-bit
+ * integer operands do not depend on it.  E4M3 and 16-bit operands: the order in which a row's products are added (fp32) depends on the kernel and
+ * on where the row's tile lies, so on the numbers of rows of all experts: the same call gives the same bits again, but the same row between other
+ * rows, or twice in one call, may differ by the rounding of its sum.
  * hero_fp8_gemm_grouped: the same with OCP E4M3 operands (hero_fp8_gemm; 8-bit results are HERO_F8E4M3).
  * hero_hp_gemm_grouped: 16-bit operands (hero_hp_gemm): C = act(A Bt[e]^T + bias[e]) in dt; K % 32 == 0, lda, ldb, expert_stride
  * multiples of 8. */

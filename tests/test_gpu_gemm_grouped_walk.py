@@ -148,3 +148,23 @@ def test_the_longest_rows(hero, fmt):
             fn = hero.hero_int8_gemm_grouped if fmt == "i8" else hero.hero_fp8_gemm_grouped
             fn(A[None], W[None, None], off, b_col_scale=torch.ones((1, 1), device="cuda"), **kw)
         assert out[0].tolist() == [want, 0, 0, 0]
+
+
+@pytest.mark.parametrize("tile", G.TILES)
+def test_rows_gathered_from_between_2_and_4_gb(hero, tile):
+    """Byte offsets of 32 bits, the uppermost of which is set: they are no negative numbers.  (As much memory of the test's own lies in front of the rows.)"""
+    MA, K, N = 2 ** 20 - 3, 4096, 48
+    room = torch.zeros((2 ** 19 + MA, K), dtype=torch.int8, device="cuda")
+    room[:2 ** 19] = 1
+    A = room[2 ** 19:]
+    index = torch.tensor([0, MA - 1, 2 ** 19, 2 ** 19 - 1, 700_001, MA - 2, 77], dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(7)
+    A[index.long()] = torch.randint(-127, 128, (7, K), generator=g, device="cuda", dtype=torch.int8)
+    W = torch.randint(-127, 128, (2, N, K), generator=g, device="cuda", dtype=torch.int8)
+    rs = torch.ones(MA, device="cuda")
+    rs[index.long()] = torch.arange(1.0, 8.0, device="cuda")
+    off, cs = torch.tensor([0, 3, 7], dtype=torch.int32, device="cuda"), torch.full((2, N), 1e-4, device="cuda")
+    got = hero.hero_int8_gemm_grouped(A, W, off, row_index=index, a_row_scale=rs, b_col_scale=cs, tile=tile).double()
+    for e, (a, b) in enumerate(((0, 3), (3, 7))):
+        y = A[index[a:b].long()].double() @ W[e].double().t() * rs[index[a:b].long()].double()[:, None] * cs[e].double()
+        assert bool(((got[a:b] - y).abs() <= (2.0 ** -8 + 2.0 ** -20) * y.abs()).all())      # one rounding to BF16, a few of fp32
